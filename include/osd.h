@@ -350,6 +350,133 @@ int osd_sample(const void* p_logits, int64_t p_row_stride,
                void* stream);
 
 /*
+ * The record of a row of logits: its k largest logits, and the mass of all
+ * the others.  It is what a draft model that proposes from its top logits
+ * needs to hand on, and what a replay buffer keeps of the teacher in place of
+ * the row (Algorithm 1 stores the target's distribution at the error index; a
+ * row of 32128 bf16 logits is 64256 bytes, its record with k = 64 388).
+ *
+ *   ids   [k] int32  token ids, largest logit first, the lowest id first among
+ *                    equal logits (zeros of both signs are equal); -1 in slots
+ *                    past the row's finite logits
+ *   top   [k] dtype  their logits, -inf in slots without a token
+ *   rest  fp32       log(sum over the tokens outside the record of
+ *                    exp((x_j - top_0) / T)), -inf if they have no mass:
+ *                    relative to the first slot's logit, at a temperature T
+ *
+ * A row with a NaN or +inf logit, or without a finite one, has the empty
+ * record: ids -1, top -inf, rest -inf.
+ *
+ * osd_topk -- the record of each row and, with tokens_out, a token drawn
+ * from it: rank r is the smallest whose running sum of exp(top_r / T), in slot
+ * order, exceeds u * their total (a proposal y ~ q with q the softmax over
+ * the record; Algorithm 1's proposal step with a truncated draft).
+ *
+ * logits        [N, V] dtype rows, row n at element offset n * row_stride
+ *               (row_stride >= V)
+ * k             1 .. min(V, OSD_MAX_TOPK)
+ * temperature   T > 0; or T == 0, where the token is slot 0's (the argmax)
+ *               and rest_out must be NULL
+ * u             [N] float uniforms in [0, 1); NULL without tokens_out or at
+ *               T == 0
+ * ids_out       out [N, k] int32
+ * top_out       out [N, k] dtype
+ * rest_out      out [N] fp32, nullable
+ * tokens_out    out [N] int32, nullable; -1 for an empty record
+ * workspace     NULL, or at least osd_topk_workspace_bytes(N, k) bytes,
+ *               16-byte aligned, zero before the first call; every call leaves
+ *               it zero.  Calls that may overlap need their own.  With one, a
+ *               few long rows are split over several workgroups.  The ids,
+ *               logits and tokens are the same either way, rest to within fp32
+ *               rounding
+ *
+ * Errors: OSD_ERR_INVALID_ARG for sizes or k out of range, a bad dtype, T < 0,
+ * inf or NaN, rest_out at T == 0, a needed pointer NULL or a row stride < V;
+ * OSD_ERR_UNSUPPORTED for V > osd_max_vocab(dtype); OSD_ERR_WORKSPACE for a
+ * workspace that is too small or misaligned; OSD_ERR_DEVICE if the launch
+ * fails.  Nothing is enqueued on an error.
+ */
+#define OSD_MAX_TOPK 256
+size_t osd_topk_workspace_bytes(int N, int k);
+int osd_topk(const void* logits, int64_t row_stride, int dtype, int N, int V, int k, float temperature,
+             const float* u, int32_t* ids_out, void* top_out, float* rest_out, int32_t* tokens_out,
+             void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * osd_distill_topk_loss_grad -- osd_distill_loss_grad from teacher records.
+ * The record's tokens are k buckets and all other tokens one more; over these
+ *   p = softmax(top_1 / tau, .., top_k / tau, rest)      (teacher)
+ *   q = the student's softmax(s / tau), the others summed
+ * and D is Eq. 3's divergence between p and q:
+ *   FKL  KL(p || q)          gradient of token j in bucket b  q_j (1 - p_b / q_b) / tau
+ *   RKL  KL(q || p)                     q_j (log(q_b / p_b) - D) / tau
+ *   JSD  beta KL(p || m) + (1 - beta) KL(q || m),  m = beta p + (1 - beta) q
+ *                                       (1 - beta) q_j (log(q_b / m_b) - KL(q || m)) / tau
+ * (0 log 0 = 0; a token with q_j = 0 outside the record has gradient 0).  With a record that
+ * holds the whole row this is osd_distill_loss_grad.
+ *
+ * teacher_ids   [.., k] int32, teacher_top [.., k] dtype, teacher_rest [..]
+ *               fp32: records as osd_topk writes them (rest at T = tau).  The
+ *               record of row (b, i) is number b * teacher_batch_rows + i (pass
+ *               K + 1 to distil the first K of each sequence's K + 1 target
+ *               rows).  The first slot holds the largest logit.  teacher_rest
+ *               NULL: the teacher is its record alone (p of the last bucket is
+ *               0); RKL, infinite there, is refused
+ * student_logits  row (b, i) starts at element b * student_batch_stride + i*V
+ * mask, kind, beta, tau, loss_out, row_loss_out   as osd_distill_loss_grad
+ * grad_out      out [B, K, V] in `dtype`, contiguous, nullable: the gradient
+ *               of sum(mask * D); rows with mask 0 are written as 0.  It may be
+ *               the student rows themselves (the same address, rows without
+ *               gaps); any other overlap with them is refused.  Outputs must not
+ *               overlap the other inputs
+ * workspace     osd_distill_topk_workspace_bytes(B, K) zero-initialised bytes
+ *
+ * A row whose record is empty, names a token outside [0, V) (-1: an empty slot)
+ * or one token twice, or holds a NaN or +inf, and a student row with a NaN, +inf or
+ * no finite logit, gives D = NaN and a gradient of NaN.  Equal calls give equal
+ * bits.
+ *
+ * Errors as osd_distill_loss_grad, and OSD_ERR_INVALID_ARG for k outside
+ * 1 .. min(V, OSD_MAX_TOPK), teacher_batch_rows < K with B > 1, RKL without
+ * teacher_rest.
+ */
+size_t osd_distill_topk_workspace_bytes(int B, int K);
+int osd_distill_topk_loss_grad(const int32_t* teacher_ids, const void* teacher_top, const float* teacher_rest,
+                               int64_t teacher_batch_rows, int k, const void* student_logits,
+                               int64_t student_batch_stride, int dtype, int B, int K, int V, const uint8_t* mask,
+                               int kind, float beta, float tau, float* loss_out, float* row_loss_out,
+                               void* grad_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * osd_verify_topk -- osd_verify for proposals drawn from the draft's record
+ * (osd_topk with the same T): q is the softmax over the record's slots and 0
+ * elsewhere, p the target's over the whole row, so the emitted tokens follow
+ * the target exactly although the draft is truncated.  Acceptance, first
+ * rejection, correction and bonus token as osd_verify (a proposal outside its
+ * record has q = 0: accepted where p > 0).
+ *
+ * draft_ids     [B, K, k] int32, draft_top [B, K, k] dtype: the record that
+ *               proposal i was drawn from (rest is not needed)
+ * temperature   T > 0 (at T == 0 the draft's probabilities play no part: use
+ *               osd_verify)
+ * workspace     osd_verify_topk_workspace_bytes(B, K) zero-initialised bytes
+ * the others    as osd_verify
+ *
+ * accepted_len is -1 as in osd_verify, and where the record of a position that
+ * is tested is empty, names a token outside [0, V) (-1: an empty slot) or one
+ * token twice, or holds a NaN or +inf.
+ *
+ * Decisions are taken in fp64 (exponentials to 1e-12): they agree with an exact
+ * computation except within about 1e-11 of probability mass of an edge.
+ */
+size_t osd_verify_topk_workspace_bytes(int B, int K);
+int osd_verify_topk(const void* target_logits, const int32_t* draft_ids, const void* draft_top, int k, int dtype,
+                    int B, int K, int V, const int32_t* draft_tokens, const int32_t* draft_len,
+                    const float* u_accept, const float* u_resample, float temperature, int32_t* accepted_len,
+                    int32_t* out_tokens, uint8_t* reject_mask, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/*
  * Vocabulary-sharded verification.  When the target and draft LM heads are
  * split by vocabulary over G ranks (tensor parallelism), rank g holds columns
  * [v_begin_g, v_begin_g + V_g) of every logit row, and no rank sees a whole

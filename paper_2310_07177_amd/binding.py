@@ -21,6 +21,7 @@ OSD_FKL, OSD_RKL, OSD_JSD = 0, 1, 2
 OSD_MAX_K = 16
 OSD_MAX_SHARDS = 64
 OSD_MAX_TREE_NODES = 64
+OSD_MAX_TOPK = 256
 # Byte sizes of the sharded verification's records (osd_shard_row_stats,
 # osd_shard_mass in include/osd.h); the binding keeps them as uint8 tensors.
 SHARD_ROW_STATS_BYTES = 40
@@ -31,7 +32,8 @@ EXPORTS = ("osd_max_vocab", "osd_status_string", "osd_verify_workspace_bytes", "
            "osd_distill_workspace_bytes", "osd_distill_loss_grad", "osd_verify_distill_workspace_bytes",
            "osd_verify_distill", "osd_verify_distill_rejected", "osd_verify_tree_workspace_bytes", "osd_verify_tree",
            "osd_sample_workspace_bytes", "osd_sample", "osd_shard_verify_stats", "osd_shard_verify_mass",
-           "osd_shard_verify_draw")
+           "osd_shard_verify_draw", "osd_topk_workspace_bytes", "osd_topk", "osd_distill_topk_workspace_bytes",
+           "osd_distill_topk_loss_grad", "osd_verify_topk_workspace_bytes", "osd_verify_topk")
 
 _lib = None
 _lock = threading.Lock()
@@ -95,6 +97,20 @@ def lib():
             L.osd_shard_verify_draw.restype = i32
             L.osd_shard_verify_draw.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, f32,
                                                 vp, vp, vp, vp, vp]
+            L.osd_topk_workspace_bytes.restype = sz
+            L.osd_topk_workspace_bytes.argtypes = [i32, i32]
+            L.osd_topk.restype = i32
+            L.osd_topk.argtypes = [vp, i64, i32, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, sz, vp]
+            L.osd_distill_topk_workspace_bytes.restype = sz
+            L.osd_distill_topk_workspace_bytes.argtypes = [i32, i32]
+            L.osd_distill_topk_loss_grad.restype = i32
+            L.osd_distill_topk_loss_grad.argtypes = [vp, vp, vp, i64, i32, vp, i64, i32, i32, i32, i32, vp, i32, f32,
+                                                     f32, vp, vp, vp, vp, sz, vp]
+            L.osd_verify_topk_workspace_bytes.restype = sz
+            L.osd_verify_topk_workspace_bytes.argtypes = [i32, i32]
+            L.osd_verify_topk.restype = i32
+            L.osd_verify_topk.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, f32, vp, vp, vp, vp,
+                                          sz, vp]
             _lib = L
     return _lib
 
@@ -513,4 +529,165 @@ def osd_shard_verify_draw(target_shard, draft_shard, draft_tokens, u_resample, t
                                      _ptr(rmask), _stream_handle(dev))
     if st != OSD_OK:
         raise OsdError("osd_shard_verify_draw", st)
+    return acc, toks, rmask
+
+
+def _check_same_device(dev, *ts):
+    """Every tensor given lives on the GPU `dev`."""
+    for t in ts:
+        if t is not None and (not t.is_cuda or t.device != dev):
+            raise ValueError("every tensor argument must live on one GPU")
+
+
+def _on_device(dev, fn, *args):
+    """fn(*args) with `dev` as the current device (a launch goes to the current
+    device's queues)."""
+    torch = _torch()
+    if torch._C._cuda_getDevice() == dev.index:
+        return fn(*args)
+    with torch.cuda.device(dev):
+        return fn(*args)
+
+
+def _check_out(t, shape, dtype, name):
+    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+
+
+def osd_topk(logits, k, temperature=1.0, u=None, rest=True, tokens=None, out=None):
+    """The record of each row of logits through the C ABI: its k largest
+    logits with their ids, the log mass of the others relative to the first
+    slot's, and a token drawn from the record.
+
+    logits: [N, V] bf16 or fp32 GPU tensor with contiguous rows (any row
+    stride, e.g. a slice [:, i, :] of a [B, K, V] tensor).  u: [N] float32
+    uniforms; given, or with tokens=True (the argmax at T == 0), a token is
+    drawn.  Returns (ids [N, k] int32, top [N, k] like logits, rest [N]
+    float32 or None, tokens [N] int32 or None) as new (or the given `out`)
+    tensors; pass rest=False at T == 0."""
+    torch = _torch()
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be a [N, V] tensor with contiguous rows")
+    N, V = logits.shape
+    dev = logits.device
+    _check_same_device(dev, logits, u)
+    if u is not None:
+        _check_out(u, (N,), torch.float32, "u")
+    if tokens is None:
+        tokens = u is not None
+    k = int(k)
+    if out is None:
+        out = (torch.empty(N, k, dtype=torch.int32, device=dev),
+               torch.empty(N, k, dtype=logits.dtype, device=dev),
+               torch.empty(N, dtype=torch.float32, device=dev) if rest else None,
+               torch.empty(N, dtype=torch.int32, device=dev) if tokens else None)
+    ids, top, rst, toks = out
+    _check_same_device(dev, *out)
+    _check_out(ids, (N, k), torch.int32, "ids")
+    _check_out(top, (N, k), logits.dtype, "top")
+    _check_out(rst, (N,), torch.float32, "rest")
+    _check_out(toks, (N,), torch.int32, "tokens")
+    L = lib()
+    ws = workspace("topk", L.osd_topk_workspace_bytes(N, k), dev)
+    st = _on_device(dev, L.osd_topk, _ptr(logits), logits.stride(0) if N > 1 else V, _dtype_code(logits), N, V, k,
+                    float(temperature), _ptr(u), _ptr(ids), _ptr(top), _ptr(rst), _ptr(toks), _ptr(ws), ws.numel(),
+                    _stream_handle(dev))
+    if st != OSD_OK:
+        raise OsdError("osd_topk", st)
+    return ids, top, rst, toks
+
+
+def osd_distill_topk_loss_grad(teacher_ids, teacher_top, teacher_rest, student_logits, kind, beta=0.5, tau=1.0,
+                               mask=None, grad=True, row_loss=True, out=None):
+    """Distillation divergence and gradient against teacher records through
+    the C ABI.
+
+    teacher_ids [B, Kt, k] int32, teacher_top [B, Kt, k] and teacher_rest
+    [B, Kt] float32 or None: records as osd_topk returns them, Kt >= K (the
+    first K of each sequence are distilled, so a [B, K+1] target's records
+    serve as they are).  student_logits [B, K, V] with rows one after another
+    (any batch stride).  Returns (loss [2] float32 = {mean, sum}, row_loss
+    [B, K] float32 or None, grad [B, K, V] or None)."""
+    torch = _torch()
+    if student_logits.dim() != 3 or teacher_ids.dim() != 3:
+        raise ValueError("student_logits must be [B, K, V], teacher_ids [B, Kt, k]")
+    B, K, V = student_logits.shape
+    Kt, k = teacher_ids.shape[1:]
+    dev = student_logits.device
+    _check_same_device(dev, student_logits, teacher_ids, teacher_top, teacher_rest, mask)
+    s = student_logits
+    if (V > 1 and s.stride(2) != 1) or (K > 1 and s.stride(1) != V):
+        raise ValueError("the student's rows must lie one after another")
+    if Kt < K or teacher_ids.shape[0] != B:
+        raise ValueError("teacher records must be [B, Kt, k] with Kt >= K")
+    if teacher_top.dtype != s.dtype:
+        raise TypeError("teacher_top and student logits must share a dtype")
+    _check_out(teacher_ids, (B, Kt, k), torch.int32, "teacher_ids")
+    _check_out(teacher_top, (B, Kt, k), s.dtype, "teacher_top")
+    _check_out(teacher_rest, (B, Kt), torch.float32, "teacher_rest")
+    _check_out(mask, (B, K), torch.uint8, "mask")
+    kind_code = KINDS[kind] if isinstance(kind, str) else int(kind)
+    if out is None:
+        out = (torch.empty(2, dtype=torch.float32, device=dev),
+               torch.empty(B, K, dtype=torch.float32, device=dev) if row_loss else None,
+               torch.empty(B, K, V, dtype=s.dtype, device=dev) if grad else None)
+    loss, rows, g = out
+    _check_same_device(dev, *out)
+    _check_out(loss, (2,), torch.float32, "loss")
+    _check_out(rows, (B, K), torch.float32, "row_loss")
+    _check_out(g, (B, K, V), s.dtype, "grad")
+    L = lib()
+    ws = workspace("distill_topk", L.osd_distill_topk_workspace_bytes(B, K), dev)
+    st = _on_device(dev, L.osd_distill_topk_loss_grad, _ptr(teacher_ids), _ptr(teacher_top), _ptr(teacher_rest), Kt, k,
+                    _ptr(s), s.stride(0) if B > 1 else K * V, _dtype_code(s), B, K, V, _ptr(mask), kind_code,
+                    float(beta), float(tau), _ptr(loss), _ptr(rows), _ptr(g), _ptr(ws), ws.numel(),
+                    _stream_handle(dev))
+    if st != OSD_OK:
+        raise OsdError("osd_distill_topk_loss_grad", st)
+    return loss, rows, g
+
+
+def osd_verify_topk(target_logits, draft_ids, draft_top, draft_tokens, u_accept, u_resample, temperature,
+                    draft_len=None, out=None):
+    """Verification of proposals drawn from the draft's records through the
+    C ABI.
+
+    target_logits [B, K+1, V]; draft_ids [B, K, k] int32 and draft_top
+    [B, K, k]: the records (osd_topk at the same temperature) that
+    draft_tokens [B, K] int32 were drawn from; the other arguments and the
+    results as osd_verify, temperature > 0."""
+    torch = _torch()
+    if target_logits.dim() != 3 or draft_ids.dim() != 3:
+        raise ValueError("target_logits must be [B, K+1, V], draft_ids [B, K, k]")
+    B, K1, V = target_logits.shape
+    K, k = K1 - 1, draft_ids.shape[2]
+    dev = target_logits.device
+    _check_same_device(dev, target_logits, draft_ids, draft_top, draft_tokens, u_accept, u_resample, draft_len)
+    if not target_logits.is_contiguous():
+        raise ValueError("tensor arguments must be contiguous")
+    if draft_top.dtype != target_logits.dtype:
+        raise TypeError("target logits and draft_top must share a dtype")
+    _check_out(draft_ids, (B, K, k), torch.int32, "draft_ids")
+    _check_out(draft_top, (B, K, k), target_logits.dtype, "draft_top")
+    _check_out(draft_tokens, (B, K), torch.int32, "draft_tokens")
+    _check_out(u_accept, (B, K), torch.float32, "u_accept")
+    _check_out(u_resample, (B,), torch.float32, "u_resample")
+    _check_out(draft_len, (B,), torch.int32, "draft_len")
+    if out is None:
+        out = (torch.empty(B, dtype=torch.int32, device=dev),
+               torch.empty(B, K + 1, dtype=torch.int32, device=dev),
+               torch.empty(B, K, dtype=torch.uint8, device=dev))
+    acc, toks, rmask = out
+    _check_same_device(dev, *out)
+    _check_out(acc, (B,), torch.int32, "accepted_len")
+    _check_out(toks, (B, K + 1), torch.int32, "out_tokens")
+    _check_out(rmask, (B, K), torch.uint8, "reject_mask")
+    L = lib()
+    ws = workspace("verify_topk", L.osd_verify_topk_workspace_bytes(B, K), dev)
+    st = _on_device(dev, L.osd_verify_topk, _ptr(target_logits), _ptr(draft_ids), _ptr(draft_top), k,
+                    _dtype_code(target_logits), B, K, V, _ptr(draft_tokens), _ptr(draft_len), _ptr(u_accept),
+                    _ptr(u_resample), float(temperature), _ptr(acc), _ptr(toks), _ptr(rmask), _ptr(ws), ws.numel(),
+                    _stream_handle(dev))
+    if st != OSD_OK:
+        raise OsdError("osd_verify_topk", st)
     return acc, toks, rmask

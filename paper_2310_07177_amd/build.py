@@ -15,7 +15,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libosd.so")
 PROBE_LIB = os.path.join(HERE, "libosd_probe.so")
 SOURCES = ["osd_api.hip", "verify.hip", "distill.hip", "verify_greedy.hip", "distill_stream.hip", "verify_distill.hip",
-           "sample.hip", "verify_shard.hip", "verify_tree.hip"]
+           "sample.hip", "verify_shard.hip", "verify_tree.hip", "topk.hip", "distill_topk.hip", "verify_topk.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -647,3 +647,173 @@ int osd_verify_tree(const void* target_logits, const void* draft_logits, int dty
 }
 
 }  // extern "C"
+
+// ---------------------------------------------------------------------------
+// The record of a row's top logits: made, distilled from, verified against.
+// ---------------------------------------------------------------------------
+namespace {
+
+struct DistillTopkWs {
+    size_t done, partials, total;
+};
+DistillTopkWs distill_topk_layout(int B, int K) {
+    DistillTopkWs w;
+    const int64_t rows = int64_t(B) * K;
+    const size_t groups = size_t(rows < osd::kMaxDistillTopkGroups ? rows : osd::kMaxDistillTopkGroups);
+    w.done = 0;
+    w.partials = kAlign;
+    w.total = w.partials + round_up(groups * 8, kAlign);
+    return w;
+}
+
+bool record_ok(int k, int V) { return k >= 1 && k <= OSD_MAX_TOPK && k <= V; }
+
+// Whether the bytes [a, a + na) and [b, b + nb) meet.
+bool meets(const void* a, uint64_t na, const void* b, uint64_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + nb && y < x + na;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t osd_topk_workspace_bytes(int N, int k) {
+    if (N <= 0 || k <= 0 || k > OSD_MAX_TOPK) return 0;
+    return 256;
+}
+
+int osd_topk(const void* logits, int64_t row_stride, int dtype, int N, int V, int k, float temperature,
+             const float* u, int32_t* ids_out, void* top_out, float* rest_out, int32_t* tokens_out,
+             void* workspace, size_t workspace_bytes, void* stream) {
+    if (dtype != OSD_F32 && dtype != OSD_BF16) return OSD_ERR_INVALID_ARG;
+    if (N <= 0 || V <= 0 || !record_ok(k, V)) return OSD_ERR_INVALID_ARG;
+    if (V > osd_max_vocab(dtype)) return OSD_ERR_UNSUPPORTED;
+    if (!(temperature >= 0.0f) || isinf(temperature)) return OSD_ERR_INVALID_ARG;
+    if (!logits || row_stride < V || !ids_out || !top_out) return OSD_ERR_INVALID_ARG;
+    if (temperature == 0.0f && rest_out) return OSD_ERR_INVALID_ARG;
+    if (temperature > 0.0f && tokens_out && !u) return OSD_ERR_INVALID_ARG;
+    if (workspace && (workspace_bytes < osd_topk_workspace_bytes(N, k) ||
+                      (reinterpret_cast<uintptr_t>(workspace) & 15u)))
+        return OSD_ERR_WORKSPACE;
+    osd::TopkLaunch L;
+    L.x = logits;
+    L.stride = row_stride;
+    L.dtype = dtype;
+    L.N = N;
+    L.V = V;
+    L.k = k;
+    L.temperature = temperature;
+    L.u = u;
+    L.ids = ids_out;
+    L.top = top_out;
+    L.rest = rest_out;
+    L.tokens = tokens_out;
+    L.workspace = workspace;
+    L.stream = static_cast<hipStream_t>(stream);
+    L.cus = device_cus(L.stream);
+    return osd::launch_topk(L) == hipSuccess ? OSD_OK : OSD_ERR_DEVICE;
+}
+
+size_t osd_distill_topk_workspace_bytes(int B, int K) {
+    if (B <= 0 || K <= 0) return 0;
+    if (int64_t(B) * int64_t(K) > 0x7FFFFFFFll) return 0;
+    return distill_topk_layout(B, K).total;
+}
+
+int osd_distill_topk_loss_grad(const int32_t* teacher_ids, const void* teacher_top, const float* teacher_rest,
+                               int64_t teacher_batch_rows, int k, const void* student_logits,
+                               int64_t student_batch_stride, int dtype, int B, int K, int V, const uint8_t* mask,
+                               int kind, float beta, float tau, float* loss_out, float* row_loss_out,
+                               void* grad_out, void* workspace, size_t workspace_bytes, void* stream) {
+    if (dtype != OSD_F32 && dtype != OSD_BF16) return OSD_ERR_INVALID_ARG;
+    if (B <= 0 || K <= 0 || V <= 0 || !record_ok(k, V)) return OSD_ERR_INVALID_ARG;
+    if (int64_t(B) * int64_t(K) > 0x7FFFFFFFll) return OSD_ERR_INVALID_ARG;
+    if (V > osd_max_vocab(dtype)) return OSD_ERR_UNSUPPORTED;
+    if (kind != OSD_FKL && kind != OSD_RKL && kind != OSD_JSD) return OSD_ERR_INVALID_ARG;
+    if (!(tau > 0.0f) || isinf(tau)) return OSD_ERR_INVALID_ARG;
+    if (!(beta >= 0.0f && beta <= 1.0f)) return OSD_ERR_INVALID_ARG;
+    if (!teacher_ids || !teacher_top || !student_logits || !loss_out) return OSD_ERR_INVALID_ARG;
+    // KL(q || p) needs the teacher's mass wherever the student has some.
+    if (kind == OSD_RKL && !teacher_rest) return OSD_ERR_INVALID_ARG;
+    if (B > 1 && (teacher_batch_rows < K || student_batch_stride < int64_t(K) * V)) return OSD_ERR_INVALID_ARG;
+    const int64_t eb = dtype == OSD_BF16 ? 2 : 4, rows = int64_t(K) * V * eb;
+    // The gradient may take the student rows' own place, each row in its own.
+    if (grad_out && !(grad_out == student_logits && (B == 1 || student_batch_stride == int64_t(K) * V)) &&
+        meets(grad_out, uint64_t(B) * rows, student_logits, uint64_t((B - 1) * student_batch_stride * eb + rows)))
+        return OSD_ERR_INVALID_ARG;
+    const DistillTopkWs ws = distill_topk_layout(B, K);
+    if (!workspace || workspace_bytes < ws.total || (reinterpret_cast<uintptr_t>(workspace) & 15u))
+        return OSD_ERR_WORKSPACE;
+    osd::DistillTopkLaunch L;
+    L.ids = teacher_ids;
+    L.top = teacher_top;
+    L.rest = teacher_rest;
+    L.teacher_rows = teacher_batch_rows;
+    L.k = k;
+    L.student = student_logits;
+    L.student_stride = student_batch_stride;
+    L.dtype = dtype;
+    L.B = B;
+    L.K = K;
+    L.V = V;
+    L.mask = mask;
+    L.kind = kind;
+    L.beta = beta;
+    L.tau = tau;
+    L.loss_out = loss_out;
+    L.row_loss_out = row_loss_out;
+    L.grad_out = grad_out;
+    char* w = static_cast<char*>(workspace);
+    L.done_counter = reinterpret_cast<uint32_t*>(w + ws.done);
+    L.partials = reinterpret_cast<double*>(w + ws.partials);
+    L.stream = static_cast<hipStream_t>(stream);
+    L.cus = device_cus(L.stream);
+    return osd::launch_distill_topk(L) == hipSuccess ? OSD_OK : OSD_ERR_DEVICE;
+}
+
+size_t osd_verify_topk_workspace_bytes(int B, int K) {
+    if (B <= 0 || K <= 0 || K > OSD_MAX_K) return 0;
+    if (int64_t(B) * int64_t(K + 1) > 0x7FFFFFFFll) return 0;
+    return round_up(size_t(B) * size_t(K + 1) * sizeof(osd::VerifyTopkRow), kAlign);
+}
+
+int osd_verify_topk(const void* target_logits, const int32_t* draft_ids, const void* draft_top, int k, int dtype,
+                    int B, int K, int V, const int32_t* draft_tokens, const int32_t* draft_len,
+                    const float* u_accept, const float* u_resample, float temperature, int32_t* accepted_len,
+                    int32_t* out_tokens, uint8_t* reject_mask, void* workspace, size_t workspace_bytes,
+                    void* stream) {
+    if (dtype != OSD_F32 && dtype != OSD_BF16) return OSD_ERR_INVALID_ARG;
+    if (B <= 0 || K <= 0 || V <= 0 || K > OSD_MAX_K || !record_ok(k, V)) return OSD_ERR_INVALID_ARG;
+    if (!sizes_ok(B, K, V, dtype)) return OSD_ERR_UNSUPPORTED;
+    if (!(temperature > 0.0f) || isinf(temperature)) return OSD_ERR_INVALID_ARG;
+    if (!target_logits || !draft_ids || !draft_top || !draft_tokens || !u_accept || !u_resample || !accepted_len ||
+        !out_tokens)
+        return OSD_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < osd_verify_topk_workspace_bytes(B, K) ||
+        (reinterpret_cast<uintptr_t>(workspace) & 15u))
+        return OSD_ERR_WORKSPACE;
+    osd::VerifyTopkLaunch L;
+    L.target = target_logits;
+    L.ids = draft_ids;
+    L.top = draft_top;
+    L.k = k;
+    L.dtype = dtype;
+    L.B = B;
+    L.K = K;
+    L.V = V;
+    L.tokens = draft_tokens;
+    L.draft_len = draft_len;
+    L.u_accept = u_accept;
+    L.u_resample = u_resample;
+    L.temperature = temperature;
+    L.accepted_len = accepted_len;
+    L.out_tokens = out_tokens;
+    L.reject_mask = reject_mask;
+    L.rows = static_cast<osd::VerifyTopkRow*>(workspace);
+    L.stream = static_cast<hipStream_t>(stream);
+    L.cus = device_cus(L.stream);
+    return osd::launch_verify_topk(L) == hipSuccess ? OSD_OK : OSD_ERR_DEVICE;
+}
+
+}  // extern "C"

@@ -222,4 +222,76 @@ struct ShardLaunch {
 };
 hipError_t launch_verify_shard(const ShardLaunch& L);
 
+// The record of a row's top logits (topk.hip).
+struct TopkLaunch {
+    const void* x;
+    int64_t stride;  // elements
+    int dtype;
+    int N, V, k;
+    float temperature;
+    const float* u;
+    int32_t* ids;
+    void* top;
+    float* rest;
+    int32_t* tokens;
+    int cus;
+    void* workspace;  // null, or topk_workspace_bytes(N, k) bytes
+    hipStream_t stream;
+};
+hipError_t launch_topk(const TopkLaunch& L);
+
+// Distillation from teacher records (distill_topk.hip).
+struct DistillTopkLaunch {
+    const int32_t* ids;
+    const void* top;
+    const float* rest;
+    int64_t teacher_rows;  // record rows between sequences
+    int k;
+    const void* student;
+    int64_t student_stride;  // elements between sequences
+    int dtype;
+    int B, K, V;
+    const uint8_t* mask;
+    int kind;
+    float beta, tau;
+    float* loss_out;
+    float* row_loss_out;
+    void* grad_out;
+    double* partials;        // [min(B*K, kMaxDistillTopkGroups)] zero on entry and exit
+    uint32_t* done_counter;  // [1] zero on entry and exit
+    int cus;
+    hipStream_t stream;
+};
+// Workgroups of one launch at most.
+constexpr int kMaxDistillTopkGroups = 8192;
+hipError_t launch_distill_topk(const DistillTopkLaunch& L);
+
+// Verification against draft records (verify_topk.hip): what is kept of one
+// target row, by cell.
+constexpr int kMaxCells = 64;
+struct VerifyTopkRow {
+    double sum[kMaxCells];
+    float top[kMaxCells];
+};
+struct VerifyTopkLaunch {
+    const void* target;
+    const int32_t* ids;
+    const void* top;
+    int k;
+    int dtype;
+    int B, K, V;
+    const int32_t* tokens;
+    const int32_t* draft_len;
+    const float* u_accept;
+    const float* u_resample;
+    float temperature;
+    int32_t* accepted_len;
+    int32_t* out_tokens;
+    uint8_t* reject_mask;
+    VerifyTopkRow* rows;  // [B*(K+1)]
+    int cus;
+    hipStream_t stream;
+};
+hipError_t launch_verify_topk(const VerifyTopkLaunch& L);
+
 }  // namespace osd

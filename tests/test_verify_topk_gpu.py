@@ -1,0 +1,249 @@
+"""osd_verify_topk against the 64-bit reference: every output exactly (a
+sequence with a decision within 1e-9 of a border is counted and left out), and
+a speculative step that makes, draws from, verifies and distils records."""
+import numpy as np
+import pytest
+
+from oracle import topk_ref
+from tests._helpers import to_device
+from tests._topk_helpers import as_dtype, rows, uniforms
+from tests.test_topk_gpu import host
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def osd():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU")
+    import paper_2310_07177_amd as m
+    m.lib()
+    return m
+
+
+def inputs(B, K, V, k, dtype, T, seed, noise=1.0, kind="normal"):
+    t = rows(kind, B * (K + 1), V, seed, dtype).reshape(B, K + 1, V)
+    with np.errstate(over="ignore", invalid="ignore"):
+        d = (rows("normal", B * K, V, seed + 1) / 3 * noise).reshape(B, K, V)
+        d = d + np.where(np.abs(t[:, :K]) < 1e4, t[:, :K], 0)
+    t, d = as_dtype(t, dtype), as_dtype(d, dtype)
+    rec = topk_ref.topk(d.reshape(B * K, V), k, T, uniforms(B * K, seed + 2))
+    ids = rec["ids"]
+    top = np.take_along_axis(d.reshape(B * K, V), ids.astype(np.int64), 1)
+    return dict(t=t, ids=ids.reshape(B, K, k), top=top.reshape(B, K, k), y=rec["tokens"].reshape(B, K),
+                ua=uniforms((B, K), seed + 3), ur=uniforms(B, seed + 4))
+
+
+def call(osd, x, T, dl=None):
+    return osd.osd_verify_topk(*(to_device(x[n]) for n in ("t", "ids", "top", "y", "ua", "ur")), T,
+                               draft_len=to_device(dl))
+
+
+def check(got, x, T, dl, label):
+    acc, toks, rmask = (host(t) for t in got)
+    wa, wt, wm, margin = topk_ref.verify(x["t"], x["ids"], x["top"], x["y"], x["ua"], x["ur"], T, dl)
+    sure = margin > 1e-9
+    bad = (acc != wa) | (toks != wt).any(1) | (rmask != wm).any(1)
+    bad &= sure
+    assert not bad.any(), (f"{label}: {bad.sum()} sequences, first {np.argwhere(bad)[0]}: {acc[bad][0]} "
+                           f"{toks[bad][0]} for {wa[bad][0]} {wt[bad][0]}")
+    return int((~sure).sum())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,k", [(1, 1), (2, 1), (7, 7), (9, 4), (100, 64), (255, 3), (1001, 65), (2048, 256),
+                                 (2049, 16), (4099, 1), (8192, 100), (20011, 33), (32000, 64), (32771, 255)])
+def test_shapes(osd, V, k, dtype):
+    B, K, T = 7, 3, 0.75
+    x = inputs(B, K, V, k, dtype, T, V)
+    assert check(call(osd, x, T), x, T, None, f"V={V} k={k} {dtype}") <= 1
+
+
+@pytest.mark.parametrize("V,k,dtype", [(65536, 100, "f32"), (50257, 20, "f32"), (131072, 256, "bf16"),
+                                       (128256, 64, "bf16"), (100003, 17, "bf16")])
+def test_long_rows(osd, V, k, dtype):
+    B, K, T = 2, 2, 1.0
+    x = inputs(B, K, V, k, dtype, T, V)
+    check(call(osd, x, T), x, T, None, f"V={V} k={k} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K", [1, 2, 5, 16])
+@pytest.mark.parametrize("noise", [0.05, 3.0])
+def test_lengths_and_acceptance(osd, K, noise, dtype):
+    """Ragged and out-of-range lengths; drafts near the target and far off."""
+    B, V, k, T = 60, 1003, 50, 1.0
+    x = inputs(B, K, V, k, dtype, T, 100 + K, noise)
+    dl = (np.arange(B) % (K + 2)).astype(np.int32)
+    left = check(call(osd, x, T, dl), x, T, dl, f"K={K} ragged") + check(call(osd, x, T), x, T, None, f"K={K}")
+    assert left <= 1
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["ties", "equal", "lowest", "masked", "masked_lowest", "ascending", "block", "peak",
+                                  "wide", "bad"])
+@pytest.mark.parametrize("V", [777, 40003])
+def test_target_kinds(osd, kind, V, dtype):
+    B, K, k, T = 6, 3, 40, 1.0
+    x = inputs(B, K, V, k, dtype, T, 7, kind=kind)
+    x["ur"][0] = 0.0
+    x["ur"][1] = np.float32(1 - 2.0 ** -24)
+    x["ua"][2] = 0.0
+    x["ua"][3] = np.float32(1 - 2.0 ** -24)
+    check(call(osd, x, T), x, T, None, f"{kind} V={V} {dtype}")
+
+
+def test_first_and_last_tokens(osd):
+    """u = 0 draws the first token with mass, the largest u the last ones; the
+    residual of a draft with all of the target's mass."""
+    B, K, V, k, T = 4, 1, 5000, 8, 1.0
+    t = np.full((B, 2, V), -np.inf, np.float32)
+    t[:, :, [3, 2500, 4990]] = np.array([0.0, 0.5, 1.0], np.float32)
+    ids = np.full((B, K, k), -1, np.int32)
+    top = np.full((B, K, k), -np.inf, np.float32)
+    ids[:, :, 0], top[:, :, 0] = 4990, 1.0
+    x = dict(t=t, ids=ids, top=top, y=np.full((B, K), 4990, np.int32),
+             ua=np.full((B, K), 1 - 2.0 ** -24, np.float32), ur=np.array([0, 1 - 2.0 ** -24, 0.3, 0.6], np.float32))
+    acc, toks, _ = (host(o) for o in call(osd, x, T))
+    assert acc.tolist() == [0] * 4 and toks[:2, 0].tolist() == [3, 2500]
+    check(call(osd, x, T), x, T, None, "sparse")
+    x["ua"][:] = 0.0
+    check(call(osd, x, T), x, T, None, "bonus")
+
+
+def test_bad_records_tokens_and_rows(osd):
+    B, K, V, k, T = 12, 3, 3000, 30, 1.0
+    for accept in (0.0, 1 - 2.0 ** -24):
+        x = inputs(B, K, V, k, "f32", T, 55)
+        x["ua"][:] = accept
+        x["ids"][0, 0, 3] = x["ids"][0, 0, 9]
+        x["ids"][1, 2, 3] = V
+        x["ids"][2, 1, 3] = -5
+        x["top"][3, 1, 0] = np.nan
+        x["top"][4, 1, 0] = np.inf
+        x["ids"][5, 2] = -1
+        x["y"][6, 2] = V
+        x["y"][7, 0] = -1
+        x["t"][8, 3] = -np.inf
+        x["t"][9, 1, 5] = np.nan
+        x["ids"][10, 0, 4:] = -1  # a short record is one
+        check(call(osd, x, T), x, T, None, f"bad accept={accept}")
+
+
+def test_proposal_outside_its_record(osd):
+    x = inputs(5, 2, 1000, 10, "f32", 1.0, 66)
+    x["y"][:, 0] = [j for j in range(1000) if j not in x["ids"][:, 0]][:5]
+    acc = host(call(osd, x, 1.0)[0])
+    assert (acc >= 1).all()
+    check(call(osd, x, 1.0), x, 1.0, None, "outside")
+
+
+@pytest.mark.parametrize("B", [1, 64, 400])
+def test_batches_repeat(osd, B):
+    """Calls of several sizes in a row on one workspace give equal bits."""
+    import torch
+    K, V, k, T = 4, 8001, 64, 1.0
+    x = inputs(min(B, 16), K, V, k, "bf16", T, 77)
+    x = {n: np.concatenate([a] * (-(-B // len(a))))[:B] for n, a in x.items()}
+    a = call(osd, x, T)
+    first = {n: v[:16] for n, v in x.items()}
+    check([t[:16] for t in a], first, T, None, f"B={B}")
+    b = call(osd, first, T)
+    assert all(torch.equal(p[:min(B, 16)], q) for p, q in zip(a, b))
+    c = call(osd, x, T)
+    assert all(torch.equal(p, q) for p, q in zip(a, c))
+
+
+def test_whole_row_record_is_osd_verify(osd):
+    """k = V: osd_verify's outcome (its own fp32 margin, 1e-6, left out)."""
+    B, K, V, T = 50, 3, 200, 1.0
+    g = rows("normal", B * K, V, 88)
+    t, d = rows("normal", B * (K + 1), V, 89).reshape(B, K + 1, V), g.reshape(B, K, V)
+    rec = topk_ref.topk(g, V, T, uniforms(B * K, 90))
+    x = dict(t=t, ids=rec["ids"].reshape(B, K, V), top=rec["top"].astype(np.float32).reshape(B, K, V),
+             y=rec["tokens"].reshape(B, K), ua=uniforms((B, K), 91), ur=uniforms(B, 92))
+    a = [host(o) for o in call(osd, x, T)]
+    b = [host(o) for o in osd.osd_verify(to_device(t), to_device(d), to_device(x["y"]), to_device(x["ua"]),
+                                         to_device(x["ur"]), T)]
+    margin = topk_ref.verify(t, x["ids"], x["top"], x["y"], x["ua"], x["ur"], T)[3]
+    sure = margin > 1e-6
+    assert sure.sum() > 45
+    assert all(np.array_equal(p[sure], q[sure]) for p, q in zip(a, b))
+
+
+def test_guard_bands_and_workspace(osd):
+    import ctypes
+    import torch
+    from paper_2310_07177_amd import binding
+    for B, K, V, k in [(1, 1, 5, 3), (7, 3, 1001, 20), (3, 16, 4099, 64)]:
+        x = inputs(B, K, V, k, "bf16", 1.0, 99)
+        d = [to_device(x[n]) for n in ("t", "ids", "top", "y", "ua", "ur")]
+        sizes = [B * 4, B * (K + 1) * 4, B * K]
+        bufs = [torch.full((z + 8192,), 0x5A, dtype=torch.uint8, device="cuda") for z in sizes]
+        ws = torch.zeros(osd.lib().osd_verify_topk_workspace_bytes(B, K) + 4096, dtype=torch.uint8, device="cuda")
+        ws[-4096:] = 0x5A
+        p = lambda t, o=0: ctypes.c_void_p(t.data_ptr() + o)
+        st = osd.lib().osd_verify_topk(p(d[0]), p(d[1]), p(d[2]), k, binding.OSD_BF16, B, K, V, p(d[3]), None, p(d[4]),
+                                       p(d[5]), 1.0, *(p(b, 4096) for b in bufs), p(ws), ws.numel() - 4096, None)
+        assert st == 0
+        torch.cuda.synchronize()
+        assert (ws[-4096:] == 0x5A).all()
+        for b, z in zip(bufs, sizes):
+            assert (b[:4096] == 0x5A).all() and (b[4096 + z:] == 0x5A).all()
+
+
+def test_graph(osd):
+    import torch
+    B, K, V, k, T = 6, 4, 9001, 64, 1.0
+    xs = [inputs(B, K, V, k, "bf16", T, 200 + i) for i in range(3)]
+    names = ("t", "ids", "top", "y", "ua", "ur")
+    held = [to_device(xs[0][n]).clone() for n in names]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        osd.osd_verify_topk(*held, T)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = osd.osd_verify_topk(*held, T)
+    for i in (1, 2, 0, 1):
+        for h, n in zip(held, names):
+            h.copy_(to_device(xs[i][n]))
+        eager = osd.osd_verify_topk(*held, T)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, eager))
+        check(out, xs[i], T, None, f"replay {i}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_speculative_step_on_records(osd, dtype):
+    """A step as it is used: K proposals drawn from the draft's records,
+    verification against them, the records of the target rows kept, and the
+    draft distilled from these at each first rejection."""
+    import torch
+    B, K, V, k, T = 9, 4, 12007, 64, 1.0
+    t = as_dtype(rows("normal", B * (K + 1), V, 300), dtype).reshape(B, K + 1, V)
+    d = as_dtype(topk_ref.values(t[:, :K]).astype(np.float32) + rows("normal", B * K, V, 301).reshape(B, K, V) / 4,
+                 dtype)
+    ud, ua, ur = uniforms((K, B), 302), uniforms((B, K), 303), uniforms(B, 304)
+    dt, dd = to_device(t), to_device(d)
+    ids = torch.empty(B, K, k, dtype=torch.int32, device="cuda")
+    top = torch.empty(B, K, k, dtype=dd.dtype, device="cuda")
+    y = torch.empty(B, K, dtype=torch.int32, device="cuda")
+    for i in range(K):  # the draft's autoregressive steps
+        ids[:, i], top[:, i], _, y[:, i] = osd.osd_topk(dd[:, i, :], k, T, to_device(ud[i]), rest=False)
+    acc, toks, rmask = osd.osd_verify_topk(dt, ids, top, y, to_device(ua), to_device(ur), T)
+    ti, tt, tr, _ = osd.osd_topk(dt.view(-1, V), k, T)
+    loss, rl, g = osd.osd_distill_topk_loss_grad(ti.view(B, K + 1, k), tt.view(B, K + 1, k), tr.view(B, K + 1), dd,
+                                                 "fkl", 0.5, T, mask=rmask)
+    x = dict(t=t, ids=host(ids), top=host(top), y=host(y), ua=ua, ur=ur)
+    rec = topk_ref.topk(d.transpose(1, 0, 2).reshape(K * B, V), k, T, ud.reshape(-1))
+    assert np.array_equal(x["y"], rec["tokens"].reshape(K, B).T)
+    check((acc, toks, rmask), x, T, None, "step")
+    from tests.test_distill_topk_gpu import check as check_distill
+    from tests.test_distill_topk_gpu import record
+    fi, ft, fr = record(t[:, :K].reshape(B * K, V), k, T)
+    check_distill((loss, rl, g), fi, ft, fr, d.reshape(B * K, V), "fkl", 0.5, T, host(rmask), "step")
