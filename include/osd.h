@@ -460,14 +460,17 @@ int osd_distill_topk_loss_grad(const int32_t* teacher_ids, const void* teacher_t
  * temperature   T > 0 (at T == 0 the draft's probabilities play no part: use
  *               osd_verify)
  * workspace     osd_verify_topk_workspace_bytes(B, K) zero-initialised bytes
+ *               (counters among them are left zero; the rest keeps scratch that
+ *               later calls need not find cleared, at any B, K, V)
  * the others    as osd_verify
  *
  * accepted_len is -1 as in osd_verify, and where the record of a position that
  * is tested is empty, names a token outside [0, V) (-1: an empty slot) or one
  * token twice, or holds a NaN or +inf.
  *
- * Decisions are taken in fp64 (exponentials to 1e-12): they agree with an exact
- * computation except within about 1e-11 of probability mass of an edge.
+ * Tests agree with an exact computation except where u lies within about 1e-8
+ * (relative) of p(y)/q(y), draws except within about 1e-11 of probability mass of
+ * an edge: a draw whose point lies near an edge is decided in fp64.
  */
 size_t osd_verify_topk_workspace_bytes(int B, int K);
 int osd_verify_topk(const void* target_logits, const int32_t* draft_ids, const void* draft_top, int k, int dtype,

@@ -267,12 +267,22 @@ constexpr int kMaxDistillTopkGroups = 8192;
 hipError_t launch_distill_topk(const DistillTopkLaunch& L);
 
 // Verification against draft records (verify_topk.hip): what is kept of one
-// target row, by cell.
-constexpr int kMaxCells = 64;
+// target row in the workspace.  Only the arrivals have to be zero between calls;
+// they lie at one place in records of one size, so no call's data reaches
+// another's.
+constexpr int kMaxCells = 32;
 struct VerifyTopkRow {
-    double sum[kMaxCells];
-    float top[kMaxCells];
+    double sum[kMaxCells];     // by cell: exponentials relative to
+    float top[kMaxCells];      //          the largest logit
+    float slot[OSD_MAX_TOPK];  // the row's logits at its record's tokens
+    double q_sum;              // the record's softmax: normaliser (0: no record)
+    double q_token;            // the proposal's exponential
+    float q_top;               // the largest logit
+    float t_token;             // the row's logit at the proposal, NaN if out of range
+    uint32_t arrivals;         // (row 0) workgroups of the sequence
+    uint32_t pad[25];
 };
+static_assert(sizeof(VerifyTopkRow) == 1536, "whole cache lines");
 struct VerifyTopkLaunch {
     const void* target;
     const int32_t* ids;

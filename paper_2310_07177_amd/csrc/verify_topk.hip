@@ -5,14 +5,27 @@
 // target's softmax over the whole row, proposal y_i is accepted when
 // u q(y_i) < p(y_i), and the first rejection at row a draws from max(0, p - q)
 // (Appendix A.1, Eq. 5).  p and max(0, p - q) differ at the record's tokens only,
-// so the masses of a row's cells (256 chunks: 2048 bf16 or 1024 fp32 logits), known
+// so the masses of a row's cells (256 chunks, 2048 bf16 or
+// 1024 fp32 logits; in rows of more than 32 of these twice as many), known
 // from the sums that normalise p, need no more than the record's corrections to
 // place the draw in a cell, and one cell of row a is read again.
 //
-//   cells   one wave per cell of every row 0 .. k_b: its largest logit and the
-//           fp64 sum of exponentials relative to it
-//   decide  one workgroup per sequence: normalisers, tests, first rejection,
-//           corrections, the draw
+// One launch.  Workgroups of four waves: a wave takes one cell of a row 0 .. k_b
+// (its largest logit and the sum of exponentials relative to it), or the record
+// of one position (its normaliser, the proposal's q, the target's logits at its
+// tokens).  They post what they found in the workspace, and the last of a sequence
+// to arrive decides and draws.
+//
+// Precision: the cells' sums take v_exp_f32 and are summed in fp64 from eight
+// terms up.  With relative errors d_j of the terms the running mass C at a token is
+// off by (1 - C) sum p_j d_j over the tokens before it less C times the same over
+// those after: at most half the largest error of terms that carry mass, 6e-8, and
+// (the errors are of either sign) 5e-9 on average and 2.5e-8 at most over
+// simulated rows of 8000 to 128000 logits.  A draw whose point lies within
+// kUnsure of an edge of its token's interval is decided again on fp64 exponentials
+// of the whole row (1e-12); that is one draw in some hundred.  fp64 exponentials
+// throughout took three times as long for the cells (B = 64, K = 8, V = 32128
+// bf16: 20.6 us for them alone).
 #include "osd.h"
 #include "osd_device.hpp"
 #include "osd_internal.hpp"
@@ -23,7 +36,11 @@ namespace osd {
 namespace {
 
 constexpr int kW = 256, kNW = kW / kWave;
-constexpr int kCellChunks = 256;  // chunks of a cell: one wave, four a lane
+constexpr int kSlots = OSD_MAX_TOPK / kWave;
+constexpr int kSlotPad = 8;       // (the row's last chunk reads up to 7 elements before its own)
+constexpr int kTable = 1024;      // places for the ids of a record (at most 256)
+constexpr double kUnsure = 6.0e-8;
+// Workgroups per launch (a grid stays below 2^32 work-items).
 constexpr int64_t kMaxGrid = int64_t(1) << 22;
 
 struct VerifyTopkArgs {
@@ -31,7 +48,9 @@ struct VerifyTopkArgs {
     const int32_t* ids;
     const char* top;
     int k;
-    int B, K, V, cells;
+    int K, V, cells;
+    int groups;      // workgroups for the cells of one row
+    int records;     // workgroups for the records of one sequence
     const int32_t* tokens;
     const int32_t* draft_len;
     const float* u_accept;
@@ -41,341 +60,533 @@ struct VerifyTopkArgs {
     int32_t* accepted_len;
     int32_t* out_tokens;
     uint8_t* reject_mask;
-    int64_t first;
+    int64_t first;   // first sequence of this launch
 };
+
+// What the workgroups of a sequence post, at the device-wide coherence point.
+__device__ inline void post(double* p, double v) {
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ inline void post(float* p, float v) {
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename T>
+__device__ inline T posted(const T* p) {
+    return __hip_atomic_load(const_cast<T*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 
 template <typename Fmt>
 __device__ inline chunk_t row_chunk(const char* row, int ch, const RowCut<Fmt>& cut, int V) {
     if (V < Fmt::kPerChunk) return ch == 0 ? load_short<Fmt>(row, V) : pad_chunk<Fmt>();
-    return pad_lead<Fmt>(load_off(row, cut.off(ch)), cut.lead(ch));
+    return load_off(row, cut.off(ch));
 }
 
-template <typename Fmt>
-__global__ __launch_bounds__(kW) void cells_kernel(VerifyTopkArgs a) {
-    constexpr int EPC = Fmt::kPerChunk, kPer = kCellChunks / kWave;
-    const int lane = threadIdx.x & (kWave - 1), wid = threadIdx.x / kWave;
-    const int64_t unit = (a.first + blockIdx.x) * kNW + wid;
-    const int64_t row = unit / a.cells;
-    const int cell = int(unit - row * a.cells);
-    const int64_t b = row / (a.K + 1);
-    const int i = int(row - b * (a.K + 1));
-    if (b >= a.B) return;
-    const int kb = a.draft_len ? a.draft_len[b] : a.K;
-    if (i > kb || kb < 1 || kb > a.K) return;
-    const RowCut<Fmt> cut(a.V);
-    const char* x = a.target + row * a.V * Fmt::kBytes;
-    chunk_t c[kPer];
+// A cell is kPer chunks a lane of one wave.
+template <typename Fmt, int kPer>
+__device__ inline void load_cell(chunk_t (&c)[kPer], const char* row, int cell, const RowCut<Fmt>& cut, int V) {
+    const int lane = threadIdx.x & (kWave - 1), ch0 = cell * kPer * kWave + lane;
 #pragma unroll
-    for (int r = 0; r < kPer; ++r) c[r] = row_chunk<Fmt>(x, cell * kCellChunks + r * kWave + lane, cut, a.V);
-    float m = kNegInf;
+    for (int r = 0; r < kPer; ++r) c[r] = row_chunk<Fmt>(row, ch0 + r * kWave, cut, V);
+}
+
+// One cell by one wave: its largest logit, and the sum of exponentials relative
+// to it (0 where there is no finite one).
+template <typename Fmt, int kPer, bool EXACT>
+__device__ inline void cell_sum(chunk_t (&c)[kPer], int cell, const RowCut<Fmt>& cut, double c2, float& m, double& S) {
+    constexpr int EPC = Fmt::kPerChunk;
+    const int lane = threadIdx.x & (kWave - 1), ch0 = cell * kPer * kWave + lane;
+    if ((cell + 1) * kPer * kWave > cut.nfull) {  // the row's end
+#pragma unroll
+        for (int r = 0; r < kPer; ++r) c[r] = pad_lead<Fmt>(c[r], cut.lead(ch0 + r * kWave));
+    }
+    m = kNegInf;
 #pragma unroll
     for (int r = 0; r < kPer; ++r)
 #pragma unroll
         for (int e = 0; e < EPC; ++e) m = max_nan(m, Fmt::get(c[r], e));
+    opaque<kPer>(c);
     m = wave_max_nan(m);
-    double S = 0.0;
-    if (is_finite(m)) {
+    S = 0.0;
+    if (!is_finite(m)) return;
+    const float scale = float(c2);
 #pragma unroll
-        for (int r = 0; r < kPer; ++r)
+    for (int r = 0; r < kPer; ++r) {
+        if constexpr (EXACT) {
 #pragma unroll
-            for (int e = 0; e < EPC; ++e) S += exp2_f64((double(Fmt::get(c[r], e)) - double(m)) * a.c2);
+            for (int e = 0; e < EPC; ++e) {
+                S += exp2_f64((double(Fmt::get(c[r], e)) - double(m)) * c2);
+                if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // few registers
+            }
+            continue;
+        }
+        float e8[EPC];
+#pragma unroll
+        for (int e = 0; e < EPC; ++e) e8[e] = exp2_fast((Fmt::get(c[r], e) - m) * scale);
+#pragma unroll
+        for (int w = 1; w < EPC; w <<= 1)
+#pragma unroll
+            for (int e = 0; e < EPC; e += 2 * w) e8[e] = e8[e] + e8[e + w];
+        S += double(e8[0]);
+        __builtin_amdgcn_sched_barrier(0);
     }
     S = wave_sum(S);
-    if (lane == 0) {
-        a.rows[row].sum[cell] = S;
-        a.rows[row].top[cell] = m;
-    }
 }
 
-struct DecideLds {
-    double sum[OSD_MAX_K + 1];          // rows: normaliser
-    float top[OSD_MAX_K + 1];           //       largest logit, NaN if unusable
-    double qy[OSD_MAX_K];
-    int bad[OSD_MAX_K];                 // records that are none
-    double q[OSD_MAX_TOPK];
-    int id[OSD_MAX_TOPK];
-    uint64_t fixed[kMaxCells];          // corrections by cell, 2^-62
-    double cum[kMaxCells];              // mass up to and with each cell
-    double dense[kCellChunks * 8];      // q over the tokens of one cell
-    double wave[kNW];
-    int hit[kNW], last[kNW];
-    int32_t table[kNW][1024];           // ids seen, by wave
-    int stop, invalid;
+struct VerifyTopkLds {
+    union {
+        int32_t table[kNW][kTable];            // ids seen, by wave
+        uint16_t slot[512 * 8];                // 1 + the slot of each token of one cell, or 0
+    };
+    double row_sum[OSD_MAX_K + 1];             // target rows: normaliser
+    float row_top[OSD_MAX_K + 1];              //              largest logit, NaN or -inf if unusable
+    int verdict[OSD_MAX_K + 1];                // 0 accepted, 1 stop here, 2 invalid
+    int id[OSD_MAX_TOPK];                      // the record at the first rejection: token (-1: none),
+    double q[OSD_MAX_TOPK];                    // q, and
+    double e[OSD_MAX_TOPK];                    // the target's exponential
+    uint64_t fixed[kMaxCells];                 // corrections by cell, 2^-62
+    double sum[kMaxCells];                     // the drawn row's cells
+    double wave[kNW], low, high;
+    int hit[kNW], last, token;
+    int stop, invalid, is_last;
 };
 
-// Slot i = j * 64 + lane of the record of one position, by one wave: its
-// probability in q[j] (id -1: 0), and whether the record is one.
+// Totals over each half of the wave, in all its lanes.
+__device__ inline double half_sum(double v) {
+    v = dpp_add_step<kDppRowShr1, 0xF>(v);
+    v = dpp_add_step<kDppRowShr2, 0xF>(v);
+    v = dpp_add_step<kDppRowShr4, 0xF>(v);
+    v = dpp_add_step<kDppRowShr8, 0xF>(v);
+    v = dpp_add_step<kDppRowBcast15, 0xA>(v);
+    const double lo = readlane_f64(v, 31), hi = readlane_f64(v, 63);
+    return (threadIdx.x & 32) ? hi : lo;
+}
+__device__ inline float half_max_nan(float x) {
+    uint32_t k = order_key(x);
+    k = dpp_umax_step<kDppRowShr1, 0xF>(k);
+    k = dpp_umax_step<kDppRowShr2, 0xF>(k);
+    k = dpp_umax_step<kDppRowShr4, 0xF>(k);
+    k = dpp_umax_step<kDppRowShr8, 0xF>(k);
+    k = dpp_umax_step<kDppRowBcast15, 0xA>(k);
+    const uint32_t lo = readlane_u32(k, 31), hi = readlane_u32(k, 63);
+    return key_float((threadIdx.x & 32) ? hi : lo);  // (the largest key is a NaN's pattern too)
+}
+
+// The record of one position by one wave, posted: the softmax's reference and
+// normaliser (0: no record), the proposal's q, the target's logits at the
+// record's tokens and at the proposal.
 template <typename Fmt>
-__device__ inline bool record_softmax(const VerifyTopkArgs& a, int64_t pos, int32_t* table, int (&id)[4],
-                                      double (&q)[4]) {
+__device__ inline void post_record(const VerifyTopkArgs& a, int64_t b, int i, int32_t* table, VerifyTopkRow& out) {
     const int lane = threadIdx.x & (kWave - 1);
-    float x[4], m = kNegInf;
+    const int64_t pos = b * a.K + i;
+    const char* row = a.target + (b * (a.K + 1) + i) * a.V * Fmt::kBytes;
+    const int y = a.tokens[pos];
+    int id[kSlots];
+    float x[kSlots], m = kNegInf;
     bool ok = true;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int i = j * kWave + lane;
-        id[j] = i < a.k ? a.ids[pos * a.k + i] : -1;
-        x[j] = kNegInf;
+    for (int j = 0; j < kSlots; ++j) {
+        const int s = j * kWave + lane;
+        id[j] = s < a.k ? a.ids[pos * a.k + s] : -1;
+        x[j] = s < a.k ? Fmt::load_one(a.top + pos * a.k * Fmt::kBytes, s) : kNegInf;
+    }
+#pragma unroll
+    for (int j = 0; j < kSlots; ++j) {
+        const int s = j * kWave + lane;
         if (id[j] < -1 || id[j] >= a.V) {
             ok = false;
             id[j] = -1;
         }
         if (id[j] >= 0) {
-            x[j] = Fmt::load_one(a.top + pos * a.k * Fmt::kBytes, i);
-            if (!(x[j] < -kNegInf)) ok = false;
+            ok = ok && x[j] < -kNegInf;
+            post(&out.slot[s], Fmt::load_one(row, id[j]));
+        } else {
+            x[j] = kNegInf;
         }
         m = fmaxf(m, x[j]);
     }
     m = wave_max(m);
     ok = ok && m > kNegInf;
-    double s = 0.0;
+    double q[kSlots], s = 0.0, mine = 0.0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < kSlots; ++j) {
         q[j] = x[j] > kNegInf ? exp2_f64((double(x[j]) - double(m)) * a.c2) : 0.0;
         s += q[j];
+        if (id[j] == y) mine += q[j];
     }
     s = wave_sum(s);
+    mine = wave_sum(mine);
+    // An id twice: its place in the table is taken by an equal one.
 #pragma unroll
-    for (int j = 0; j < 4; ++j) q[j] = q[j] / s;
-    // An id twice: its place in the table of ids (1024 places for at most 256
-    // ids) is taken by an equal one.
-    int place[4];
+    for (int t = 0; t < kTable / kWave; ++t) table[t * kWave + lane] = -1;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        place[j] = -1;
+    for (int j = 0; j < kSlots; ++j) {
         if (id[j] < 0) continue;
         int h = int((uint32_t(id[j]) * 2654435761u) >> 22);
-        for (int t = 0; t < 1024; ++t) {
+        for (int t = 0; t < kTable; ++t) {
             const int old = atomicCAS(&table[h], -1, id[j]);
-            if (old == -1) {
-                place[j] = h;
-                break;
-            }
+            if (old == -1) break;
             if (old == id[j]) {
                 ok = false;
                 break;
             }
-            h = (h + 1) & 1023;
+            h = (h + 1) & (kTable - 1);
         }
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (place[j] >= 0) table[place[j]] = -1;
-    return __ballot(!ok) == 0;
+    ok = __ballot(!ok) == 0;
+    if (lane == 0) {
+        const float t = y >= 0 && y < a.V ? Fmt::load_one(row, y) : __builtin_nanf("");
+        post(&out.q_top, m);
+        post(&out.q_sum, ok ? s : 0.0);
+        post(&out.q_token, mine);
+        post(&out.t_token, t);
+    }
 }
 
-template <typename Fmt>
-__global__ __launch_bounds__(kW) void decide_kernel(VerifyTopkArgs a) {
-    constexpr int EPC = Fmt::kPerChunk;
-    __shared__ DecideLds s;
+// The drawn row, in every thread.
+struct Draw {
+    const char* row;
+    double top, sum, inv;  // largest logit, normaliser and its reciprocal
+    double point;     // in probability mass
+    double cum;       // lane c: mass up to and with cell c
+    uint64_t lives;   // cells with mass
+    bool with_q;      // the residual, or p alone
+};
+
+// The smallest token whose running mass exceeds the point; the last one with mass
+// if rounding put the point past it (-1: none has).  sure: the point is further than kUnsure
+// from both edges of the token's interval.
+template <typename Fmt, int kPer, bool EXACT>
+__device__ __forceinline__ int find_token(const VerifyTopkArgs& a, const Draw& d, VerifyTopkLds& s, bool& sure) {
+    constexpr int EPC = Fmt::kPerChunk, kCell = kPer * kWave, kEach = kCell / kW, kTokens = kCell * EPC;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = tid / kWave;
-    const int64_t b = a.first + blockIdx.x;
-    const int K = a.K;
-    const int kb = a.draft_len ? a.draft_len[b] : K;
-    const int32_t* y = a.tokens + b * K;
-    for (int i = lane; i < 1024; i += kWave) s.table[wid][i] = -1;
-    if (tid < kMaxCells) s.fixed[tid] = 0;
-    if (tid == 0) s.invalid = 0;
-    __syncthreads();
-    if (tid < K && tid < kb && (y[tid] < 0 || y[tid] >= a.V)) s.invalid = 1;
-    __syncthreads();
-    bool invalid = kb < 1 || kb > K || s.invalid;
-    int acc = 0, extra = -1;
-    if (!invalid) {
-        for (int i = wid; i <= kb; i += kNW) {
-            const VerifyTopkRow& r = a.rows[b * (K + 1) + i];
-            const float m = lane < a.cells ? r.top[lane] : kNegInf;
-            const float top = wave_max_nan(m);
-            const double v = lane < a.cells && is_finite(m) ? r.sum[lane] : 0.0;
-            const double sum = wave_sum(v * exp2_f64((double(m) - double(top)) * a.c2));
-            if (lane == 0) {
-                s.top[i] = top;
-                s.sum[i] = sum;
-            }
-            if (i < kb) {
-                int id[4];
-                double q[4];
-                const bool ok = record_softmax<Fmt>(a, b * K + i, s.table[wid], id, q);
-                const int want = y[i];
-                double mine = 0.0;
+    const RowCut<Fmt> cut(a.V);
+    const float scale = float(a.c2), top = float(d.top);
+    // The first cell that may hold the point (the sums of the cells and of their
+    // elements differ by rounding), then upwards; down from there only if rounding
+    // put the point past the last token.
+    const uint64_t from = __ballot((d.lives >> lane & 1) && d.cum > d.point - 1e-14);
+    int cell = from ? __builtin_ctzll(from) : 63 - __builtin_clzll(d.lives);
+    const int start = cell;
+    bool up = true;
+    sure = false;
+    while (true) {
+        const int ch0 = cell * kCell + tid * kEach;
+        chunk_t c[kEach];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) mine += id[j] == want ? q[j] : 0.0;
-                mine = wave_sum(mine);
-                if (lane == 0) {
-                    s.qy[i] = mine;
-                    s.bad[i] = !ok;
+        for (int n = 0; n < kEach; ++n) c[n] = row_chunk<Fmt>(d.row, ch0 + n, cut, a.V);
+        double base = cell > 0 ? readlane_f64(d.cum, cell - 1) : 0.0;
+        const bool mine = d.with_q && tid < a.k && s.id[tid] / kTokens == cell && s.id[tid] >= 0;
+        const int at = mine ? s.id[tid] - cell * kTokens : 0;
+        if (mine) s.slot[kSlotPad + at] = uint16_t(tid + 1);
+        if (tid == 0) s.last = -1;
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < kEach; ++n) c[n] = pad_lead<Fmt>(c[n], cut.lead(ch0 + n));
+        // The masses of the thread's tokens times the normaliser: of p, then without the record's part
+        // (few threads hold any of it).  In fp64 they are taken again when needed.
+        float w[EXACT ? 1 : kEach * EPC];
+        if constexpr (!EXACT) {
+#pragma unroll
+            for (int n = 0; n < kEach; ++n) {
+                const int first = cut.token((ch0 + n) * EPC);
+                const uint16_t* slots = s.slot + (first - cell * kTokens + kSlotPad);
+                int slot[EPC], any = 0;
+#pragma unroll
+                for (int e = 0; e < EPC; ++e) {
+                    slot[e] = slots[e];
+                    any |= slot[e];
+                    w[n * EPC + e] = exp2_fast((Fmt::get(c[n], e) - top) * scale);
+                }
+                if (any) {
+#pragma unroll
+                    for (int e = 0; e < EPC; ++e)
+                        if (slot[e]) w[n * EPC + e] = float(fmax(double(w[n * EPC + e]) - s.q[slot[e] - 1] * d.sum, 0.0));
                 }
             }
         }
+        // f(token, mass) for the thread's tokens in order.
+        const auto each = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+            for (int n = 0; n < kEach; ++n) {
+                const int first = cut.token((ch0 + n) * EPC);
+#pragma unroll
+                for (int e = 0; e < EPC; ++e) {
+                    if constexpr (EXACT) {
+                        const float t = Fmt::get(c[n], e);
+                        if (t > kNegInf) {
+                            double p = exp2_f64((double(t) - d.top) * a.c2) * d.inv;
+                            const int slot = s.slot[first + e - cell * kTokens + kSlotPad];
+                            if (slot) p = fmax(p - s.q[slot - 1], 0.0);
+                            f(first + e, p);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);  // few registers
+                    } else {
+                        f(first + e, double(w[n * EPC + e]) * d.inv);
+                    }
+                }
+            }
+        };
+        double run = 0.0;
+        int lastpos = -1;
+        each([&](int token, double p) __attribute__((always_inline)) {
+            run += p;
+            if (p > 0.0) lastpos = token;
+        });
+        const double upto = wave_scan_add(run);
+        if (lane == kWave - 1) s.wave[wid] = upto;
+        if (lastpos >= 0 && __ballot(lastpos >= 0) >> lane == 1) atomicMax(&s.last, lastpos);
         __syncthreads();
-        if (wid == 0) {
-            // Lane i: the test of position i.
-            bool bad = false, reject = false;
-            if (lane <= kb) bad = !is_finite(s.top[lane]);
-            if (lane < kb && !bad) {
-                bad = s.bad[lane] != 0;
-                const float t = Fmt::load_one(a.target + ((b * (K + 1) + lane) * a.V) * Fmt::kBytes, y[lane]);
-                const double py = exp2_f64((double(t) - double(s.top[lane])) * a.c2) / s.sum[lane];
-                reject = !(double(a.u_accept[b * K + lane]) * s.qy[lane] < (t > kNegInf ? py : 0.0));
-            }
-            const uint64_t stops = __ballot(lane <= kb && (bad || reject || lane == kb));
-            const int at = __builtin_ctzll(stops);
-            const uint64_t bads = __ballot(bad);
-            if (lane == 0) {
-                s.stop = at;
-                s.invalid = int((bads >> at) & 1);
-            }
+        for (int i = 0; i < wid; ++i) base += s.wave[i];
+        base += upto - run;
+        const uint64_t past = __ballot(run > 0.0 && base + run > d.point);
+        if (lane == 0) s.hit[wid] = past ? wid * kWave + __builtin_ctzll(past) : 0x7FFFFFFF;
+        __syncthreads();
+        int hit = s.hit[0];
+        for (int i = 1; i < kNW; ++i) hit = min(hit, s.hit[i]);
+        if (tid == hit) {  // the first thread whose tokens reach past the point
+            int token = -1;
+            double low = 0.0, high = 0.0;
+            each([&](int t, double p) __attribute__((always_inline)) {
+                if (token < 0 && p > 0.0) {
+                    low = base;
+                    high = base + p;
+                    if (high > d.point) token = t;
+                }
+                base += p;
+            });
+            s.token = token >= 0 ? token : lastpos;
+            s.low = low;
+            s.high = high;
         }
         __syncthreads();
-        acc = s.stop;
-        invalid = s.invalid != 0;
+        if (mine) s.slot[kSlotPad + at] = 0;
+        if (up && hit != 0x7FFFFFFF) {
+            // (An edge at 0 is exact.)
+            sure = s.high - d.point > kUnsure && (d.point - s.low > kUnsure || s.low == 0.0);
+            return s.token;
+        }
+        const int last = s.last;
+        const uint64_t more = d.lives & ~((2ull << cell) - 1);
+        if (up && more) {
+            cell = __builtin_ctzll(more);
+        } else {
+            if (last >= 0) return last;
+            if (up) cell = start;
+            up = false;
+            const uint64_t fewer = d.lives & ((1ull << cell) - 1);
+            if (!fewer) return -1;
+            cell = 63 - __builtin_clzll(fewer);
+        }
+        __syncthreads();
     }
+}
+
+// The last workgroup of a sequence: the tests, the first rejection, the draw.
+template <typename Fmt, int kPer>
+__device__ __forceinline__ void decide(const VerifyTopkArgs& a, int64_t b, int kb, VerifyTopkLds& s) {
+    constexpr int EPC = Fmt::kPerChunk, kTokens = kPer * kWave * EPC;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = tid / kWave;
+    const int K = a.K;
+    VerifyTopkRow* rows = a.rows + b * (K + 1);
+    const int32_t* y = a.tokens + b * K;
+    const int token = lane < kb ? y[lane] : 0;  // position lane's proposal
+    // Half a wave per row, two rows after another; all that was posted of them is
+    // requested at once.
+    constexpr int kBatch = 2, kRows = 2 * kNW;
+    const int cell = lane & 31;
+#pragma unroll 1
+    for (int i0 = 2 * wid + (lane >> 5); i0 - (lane >> 5) <= kb; i0 += kBatch * kRows) {
+        float m[kBatch], t[kBatch], u[kBatch];
+        double v[kBatch], qs[kBatch], qt[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int i = min(i0 + j * kRows, kb);
+            const VerifyTopkRow& r = rows[i];
+            const bool rec = i < kb;
+            m[j] = cell < a.cells ? posted(&r.top[cell]) : kNegInf;
+            v[j] = cell < a.cells ? posted(&r.sum[cell]) : 0.0;
+            qs[j] = rec ? posted(&r.q_sum) : 1.0;
+            qt[j] = rec ? posted(&r.q_token) : 0.0;
+            t[j] = rec ? posted(&r.t_token) : 0.0f;
+            u[j] = rec ? a.u_accept[b * K + i] : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int i = i0 + j * kRows;
+            const float top = half_max_nan(m[j]);
+            const double sum = half_sum(v[j] * exp2_f64((double(m[j]) - double(top)) * a.c2));
+            int verdict = 1;
+            if (!is_finite(top) || t[j] != t[j] || !(qs[j] > 0.0))
+                verdict = 2;
+            else if (i < kb) {  // u q / q_sum < p / sum
+                const double p = t[j] > kNegInf ? exp2_f64((double(t[j]) - double(top)) * a.c2) : 0.0;
+                verdict = double(u[j]) * qt[j] * sum < p * qs[j] ? 0 : 1;
+            }
+            // (A proposal outside the vocabulary, wherever it is, is caught below.)
+            if (cell == 0 && i <= kb) {
+                s.row_top[i] = top;
+                s.row_sum[i] = sum;
+                s.verdict[i] = verdict;
+            }
+        }
+    }
+    if (tid < kMaxCells) s.fixed[tid] = 0;
+    for (int i = tid; i < (kSlotPad + kTokens + 8) / 2; i += kW) reinterpret_cast<uint32_t*>(s.slot)[i] = 0u;
+    __syncthreads();
+    const int v = lane <= kb ? s.verdict[lane] : 1;
+    const int acc = __builtin_ctzll(__ballot(v != 0));
+    bool invalid = __ballot(token < 0 || token >= a.V) != 0 || __builtin_amdgcn_readlane(v, acc) == 2;
+    int extra = -1;
     if (!invalid) {
         const bool rejected = acc < kb;
-        const int64_t row = b * (K + 1) + acc;
-        const char* x = a.target + row * a.V * Fmt::kBytes;
-        const RowCut<Fmt> cut(a.V);
-        const double top = double(s.top[acc]), inv = 1.0 / s.sum[acc];
-        const auto place = [&](int id) {  // element of the row in chunk order
-            const int ch = id / EPC;
-            return id + (ch >= cut.nfull ? cut.dup : 0);
+        const VerifyTopkRow& r = rows[acc];
+        Draw d;
+        d.row = a.target + (b * (K + 1) + acc) * a.V * Fmt::kBytes;
+        d.top = double(s.row_top[acc]);
+        d.sum = s.row_sum[acc];
+        d.inv = 1.0 / d.sum;
+        // Slot s by thread s: q, and what of p it takes away from its cell.
+        const auto correct = [&] {
+            if (s.id[tid] >= 0)
+                atomicAdd(reinterpret_cast<unsigned long long*>(&s.fixed[s.id[tid] / kTokens]),
+                          (unsigned long long)(fmin(s.e[tid] * d.inv, s.q[tid]) * 0x1p62));
         };
-        const auto prob = [&](float t) {
-            return t > kNegInf ? exp2_f64((double(t) - top) * a.c2) * inv : 0.0;
-        };
-        if (rejected && wid == 0) {
-            int id[4];
-            double q[4];
-            record_softmax<Fmt>(a, b * K + acc, s.table[0], id, q);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int i = j * kWave + lane;
-                s.id[i] = id[j];
-                s.q[i] = q[j];
-                if (id[j] < 0) continue;
-                const double both = fmin(prob(Fmt::load_one(x, id[j])), q[j]);
-                atomicAdd(reinterpret_cast<unsigned long long*>(&s.fixed[place(id[j]) / (kCellChunks * EPC)]),
-                          (unsigned long long)(both * 0x1p62));
-            }
+        const float m = cell < a.cells ? posted(&r.top[cell]) : kNegInf;
+        double S = cell < a.cells ? posted(&r.sum[cell]) : 0.0;
+        if (rejected && tid < a.k) {
+            const int64_t pos = b * K + acc;
+            const int id = a.ids[pos * a.k + tid];
+            const float x = Fmt::load_one(a.top + pos * a.k * Fmt::kBytes, tid), t = posted(&r.slot[tid]);
+            const double ref = double(posted(&r.q_top)), qs = posted(&r.q_sum);
+            s.id[tid] = id;
+            s.q[tid] = x > kNegInf ? exp2_f64((double(x) - ref) * a.c2) / qs : 0.0;
+            s.e[tid] = id >= 0 && t > kNegInf ? exp2_f64((double(t) - d.top) * a.c2) : 0.0;
+            correct();
         }
+        const double u = double(a.u_resample[b]);
         __syncthreads();
-        // Lane c of every wave: cell c.
-        const VerifyTopkRow& r = a.rows[row];
-        const float m = lane < a.cells ? r.top[lane] : kNegInf;
-        double mass = 0.0;
-        if (lane < a.cells && is_finite(m)) mass = r.sum[lane] * exp2_f64((double(m) - top) * a.c2) * inv;
-        const bool live = mass > 0.0;
-        const double left = fmax(mass - double(s.fixed[lane]) * 0x1p-62, 0.0);
-        double cum = wave_scan_add(left);
-        bool with_q = rejected;
-        if (readlane_f64(cum, kWave - 1) <= 0.0) {  // rounding left nothing: from p
-            cum = wave_scan_add(mass);
-            with_q = false;
-        }
-        const double Z = readlane_f64(cum, kWave - 1);
-        const double point = double(a.u_resample[b]) * Z;
-        const uint64_t lives = __ballot(live);
-        // The first cell that may hold the point (the sums of the cells and of
-        // their elements differ by rounding), then upwards; down from there only
-        // if rounding put the point past the last token.
-        const uint64_t from = __ballot(live && cum > point - 1e-14);
-        int cell = from ? __builtin_ctzll(from) : 63 - __builtin_clzll(lives);
-        const int start = cell;
-        bool up = true;
-        while (true) {
-            double base = cell > 0 ? readlane_f64(cum, cell - 1) : 0.0;
+        const double weight = exp2_f64((double(m) - d.top) * a.c2);
+        const auto masses = [&] {  // lane c < 32 of every wave: cell c
+            const double mass = lane < kMaxCells ? S * weight * d.inv : 0.0;
+            d.lives = __ballot(mass > 0.0);
+            d.with_q = rejected;
+            d.cum = wave_scan_add(fmax(mass - double(s.fixed[cell]) * 0x1p-62, 0.0));
+            if (readlane_f64(d.cum, kWave - 1) <= 0.0) {  // rounding left nothing: from p
+                d.cum = wave_scan_add(mass);
+                d.with_q = false;
+            }
+            d.point = u * readlane_f64(d.cum, kWave - 1);
+        };
+        masses();
+        bool sure;
+        extra = find_token<Fmt, kPer, false>(a, d, s, sure);
+        if (!sure) {  // again with fp64 exponentials
             __syncthreads();
-            for (int i = tid; i < kCellChunks * EPC; i += kW) s.dense[i] = 0.0;
-            __syncthreads();
-            if (with_q && tid < a.k && s.id[tid] >= 0) {
-                const int at = place(s.id[tid]) - cell * kCellChunks * EPC;
-                if (at >= 0 && at < kCellChunks * EPC) s.dense[at] = s.q[tid];
+            if (tid < kMaxCells) {
+                s.fixed[tid] = 0;
+                s.sum[tid] = 0.0;
             }
             __syncthreads();
-            const int ch = cell * kCellChunks + tid;
-            const chunk_t c = row_chunk<Fmt>(x, ch, cut, a.V);
-            double e[EPC], run = 0.0;
-#pragma unroll
-            for (int j = 0; j < EPC; ++j) {
-                e[j] = fmax(prob(Fmt::get(c, j)) - s.dense[tid * EPC + j], 0.0);
-                run += e[j];
-            }
-            const double upto = wave_scan_add(run);
-            if (lane == kWave - 1) s.wave[wid] = upto;
-            __syncthreads();
-            for (int w = 0; w < wid; ++w) base += s.wave[w];
-            base += upto - run;
-            int hit = 0x7FFFFFFF, lastpos = -1;
-#pragma unroll
-            for (int j = 0; j < EPC; ++j) {
-                base += e[j];
-                if (e[j] > 0.0) lastpos = cut.token(ch * EPC + j);
-                if (e[j] > 0.0 && base > point && hit == 0x7FFFFFFF) hit = cut.token(ch * EPC + j);
-            }
-            const uint64_t any = __ballot(hit != 0x7FFFFFFF), pos = __ballot(lastpos >= 0);
-            const int h = any ? __shfl(hit, __builtin_ctzll(any), kWave) : 0x7FFFFFFF;
-            const int l = pos ? __shfl(lastpos, 63 - __builtin_clzll(pos), kWave) : -1;
-            if (lane == 0) {
-                s.hit[wid] = h;
-                s.last[wid] = l;
+            const RowCut<Fmt> cut(a.V);
+#pragma unroll 1
+            for (int c = wid; c < a.cells; c += kNW) {
+                chunk_t x[kPer];
+                float top;
+                double sum;
+                load_cell<Fmt, kPer>(x, d.row, c, cut, a.V);
+                cell_sum<Fmt, kPer, true>(x, c, cut, a.c2, top, sum);
+                if (lane == 0) s.sum[c] = sum;
             }
             __syncthreads();
-            int found = 0x7FFFFFFF, lastfound = -1;
-            for (int w = 0; w < kNW; ++w) {
-                found = min(found, s.hit[w]);
-                lastfound = max(lastfound, s.last[w]);
-            }
-            if (up) {
-                if (found != 0x7FFFFFFF) {
-                    extra = found;
-                    break;
-                }
-                if (lastfound >= 0) extra = lastfound;
-                const uint64_t more = lives & ~((2ull << cell) - 1);
-                if (cell < 63 && more) {
-                    cell = __builtin_ctzll(more);
-                    continue;
-                }
-                if (extra >= 0) break;
-                up = false;
-                cell = start;
-            } else if (lastfound >= 0) {
-                extra = lastfound;
-                break;
-            }
-            const uint64_t fewer = lives & ((1ull << cell) - 1);
-            if (!fewer) break;
-            cell = 63 - __builtin_clzll(fewer);
+            S = s.sum[cell];
+            d.sum = half_sum(S * weight);
+            d.inv = 1.0 / d.sum;
+            if (rejected && tid < a.k) correct();
+            __syncthreads();
+            masses();
+            extra = find_token<Fmt, kPer, true>(a, d, s, sure);
         }
         invalid = extra < 0;
     }
     if (tid <= K) {
         const int64_t o = b * (K + 1) + tid;
-        a.out_tokens[o] = invalid || tid > acc ? -1 : (tid == acc ? extra : y[tid]);
+        a.out_tokens[o] = invalid || tid > acc ? -1 : (tid == acc ? extra : token);
         if (tid == 0) a.accepted_len[b] = invalid ? -1 : acc;
         if (a.reject_mask && tid < K) a.reject_mask[b * K + tid] = !invalid && tid == acc && acc < kb ? 1 : 0;
     }
 }
 
-template <typename Fmt>
-hipError_t launch_fmt(const VerifyTopkLaunch& L, VerifyTopkArgs a) {
-    const int chunks = (L.V + Fmt::kPerChunk - 1) / Fmt::kPerChunk;
-    a.cells = (chunks + kCellChunks - 1) / kCellChunks;
-    if (a.cells > kMaxCells) return hipErrorInvalidValue;
-    const int64_t groups = (int64_t(a.B) * (a.K + 1) * a.cells + kNW - 1) / kNW;
-    for (int64_t f = 0; f < groups; f += kMaxGrid) {
-        a.first = f;
-        const unsigned g = unsigned(groups - f < kMaxGrid ? groups - f : kMaxGrid);
-        const hipError_t e = launch_kernel(&cells_kernel<Fmt>, dim3(g), dim3(kW), 0, L.stream, a);
-        if (e != hipSuccess) return e;
+template <typename Fmt, int kPer>
+__global__ __launch_bounds__(kW, kPer == 4 ? 5 : 4) void verify_topk_kernel(VerifyTopkArgs a) {
+    __shared__ VerifyTopkLds s;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const int wid = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int K = a.K;
+    const uint32_t per = uint32_t(a.records + (K + 1) * a.groups);
+    const uint32_t seq = blockIdx.x / per, unit = blockIdx.x - seq * per;
+    const int64_t b = a.first + seq;
+    const int kb = a.draft_len ? a.draft_len[b] : K;
+    if (kb < 1 || kb > K) {
+        if (unit == 0 && tid <= K) {
+            a.out_tokens[b * (K + 1) + tid] = -1;
+            if (tid == 0) a.accepted_len[b] = -1;
+            if (a.reject_mask && tid < K) a.reject_mask[b * K + tid] = 0;
+        }
+        return;
     }
-    for (int64_t f = 0; f < a.B; f += kMaxGrid) {
+    VerifyTopkRow* rows = a.rows + b * (K + 1);
+    if (unit < uint32_t(a.records)) {
+        const int i = int(unit) * kNW + wid;
+        if (i < kb) post_record<Fmt>(a, b, i, s.table[wid], rows[i]);
+    } else {
+        const uint32_t u = unit - uint32_t(a.records);
+        const int i = int(u / uint32_t(a.groups)), g = int(u - uint32_t(i) * uint32_t(a.groups));
+        if (i > kb) return;
+        const RowCut<Fmt> cut(a.V);
+        const char* x = a.target + (b * (K + 1) + i) * a.V * Fmt::kBytes;
+        const int cell = g * kNW + wid;
+        if (cell < a.cells) {
+            chunk_t c[kPer];
+            float m;
+            double S;
+            load_cell<Fmt, kPer>(c, x, cell, cut, a.V);
+            cell_sum<Fmt, kPer, false>(c, cell, cut, a.c2, m, S);
+            if (lane == 0) {
+                post(&rows[i].sum[cell], S);
+                post(&rows[i].top[cell], m);
+            }
+        }
+    }
+    // A wave's posts are in place before the workgroup's arrival is issued.
+    wait_memory();
+    __syncthreads();
+    if (tid == 0) s.is_last = arrive(&rows[0].arrivals) == uint32_t(a.records + (kb + 1) * a.groups) - 1;
+    __syncthreads();
+    if (!s.is_last) return;
+    if (tid == 0) __hip_atomic_store(&rows[0].arrivals, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    decide<Fmt, kPer>(a, b, kb, s);
+}
+
+template <typename Fmt, int kPer>
+hipError_t launch_cells(const VerifyTopkLaunch& L, VerifyTopkArgs a, int chunks) {
+    a.cells = (chunks + kPer * kWave - 1) / (kPer * kWave);
+    if (a.cells > kMaxCells) return hipErrorInvalidValue;
+    a.records = (a.K + kNW - 1) / kNW;
+    a.groups = (a.cells + kNW - 1) / kNW;
+    const int64_t per = a.records + int64_t(a.K + 1) * a.groups, most = kMaxGrid / per;
+    for (int64_t f = 0; f < L.B; f += most) {
         a.first = f;
-        const unsigned g = unsigned(a.B - f < kMaxGrid ? a.B - f : kMaxGrid);
-        const hipError_t e = launch_kernel(&decide_kernel<Fmt>, dim3(g), dim3(kW), 0, L.stream, a);
+        const unsigned g = unsigned((L.B - f < most ? L.B - f : most) * per);
+        const hipError_t e = launch_kernel(&verify_topk_kernel<Fmt, kPer>, dim3(g), dim3(kW), 0, L.stream, a);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
+}
+
+template <typename Fmt>
+hipError_t launch_fmt(const VerifyTopkLaunch& L, const VerifyTopkArgs& a) {
+    const int chunks = (L.V + Fmt::kPerChunk - 1) / Fmt::kPerChunk;
+    return chunks <= kMaxCells * 4 * kWave ? launch_cells<Fmt, 4>(L, a, chunks) : launch_cells<Fmt, 8>(L, a, chunks);
 }
 
 }  // namespace
@@ -386,7 +597,6 @@ hipError_t launch_verify_topk(const VerifyTopkLaunch& L) {
     a.ids = L.ids;
     a.top = static_cast<const char*>(L.top);
     a.k = L.k;
-    a.B = L.B;
     a.K = L.K;
     a.V = L.V;
     a.tokens = L.tokens;
