@@ -680,7 +680,7 @@ extern "C" {
 
 size_t osd_topk_workspace_bytes(int N, int k) {
     if (N <= 0 || k <= 0 || k > OSD_MAX_TOPK) return 0;
-    return 256;
+    return osd::topk_layout(N, k).total;
 }
 
 int osd_topk(const void* logits, int64_t row_stride, int dtype, int N, int V, int k, float temperature,
@@ -693,8 +693,8 @@ int osd_topk(const void* logits, int64_t row_stride, int dtype, int N, int V, in
     if (!logits || row_stride < V || !ids_out || !top_out) return OSD_ERR_INVALID_ARG;
     if (temperature == 0.0f && rest_out) return OSD_ERR_INVALID_ARG;
     if (temperature > 0.0f && tokens_out && !u) return OSD_ERR_INVALID_ARG;
-    if (workspace && (workspace_bytes < osd_topk_workspace_bytes(N, k) ||
-                      (reinterpret_cast<uintptr_t>(workspace) & 15u)))
+    if (workspace ? workspace_bytes < osd_topk_workspace_bytes(N, k) || (reinterpret_cast<uintptr_t>(workspace) & 15u)
+                  : osd::topk_needs_workspace(V, per_chunk(dtype)))
         return OSD_ERR_WORKSPACE;
     osd::TopkLaunch L;
     L.x = logits;

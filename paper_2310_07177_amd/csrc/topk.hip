@@ -1,20 +1,32 @@
 // topk.hip -- the record of a row's top logits, and a token drawn from it
 // (gfx950).
 //
-// Method: a workgroup holds a row in registers.  Each thread takes the maximum
-// of its elements; the k-th largest of the threads' maxima (to 16 bits of the
-// ordered key) is at most the k-th largest logit, since k threads hold an element
-// that large, so the elements at or above it, the candidates, are all the record
-// can hold.  There are few more than k of them (a thread rarely holds two): they
-// are collected in LDS and ranked by counting, for each, the candidates before
-// it, so the record does not depend on the order of their arrival.  A row with
+// Method: one workgroup streams a row once.  Each thread keeps, for each of up to
+// sixteen groups of its chunks, the largest logit and the sum of exponentials.  The
+// k-th largest of the threads' maxima (to 16 bits of the ordered key, by a
+// histogram of one wave) is at most the k-th largest logit, since k threads met an
+// element that large; so the elements at or above it, the candidates, are all the
+// record can hold, and there are few more than k of them.  Each wave looks through the
+// groups of its threads that reach the threshold once more, an element a lane, and
+// picks the candidates; these are grouped by key and ranked within their group by
+// counting, so the record does not depend on the order of their arrival.  A row with
 // more candidates than LDS holds (many equal logits, or the largest ones side by
-// side) gets the exact k-th (logit, id) by bisection first.
+// side) gets the exact k-th (logit, id) by bisection over the row first.
 //
-// The mass of the tokens outside the record is summed over the elements below
-// the threshold, then the candidates that were not taken: nothing is subtracted,
-// so it keeps its relative accuracy however small it is.  The draw sums fp64
-// exponentials of the record's logits.
+// The mass of the tokens outside the record is the sum over the groups below the
+// threshold, what the others hold besides candidates, and the candidates that were
+// not taken: nothing is subtracted, so it keeps its relative accuracy however small
+// it is.  The draw sums fp64 exponentials of the record's logits.
+//
+// What bounds it in bulk is instruction issue: a row of 64 KB arrives at a CU in 2.7
+// us, in which its four SIMDs issue some 6500 vector instructions, and the sweep
+// over 32128 logits takes 2700 (unpacking, one multiply-add, exponential and add an
+// element, maxima two elements an instruction).  So everything else is kept to few
+// waves and few instructions: rows held in registers (two sweeps, half the waves
+// a CU) with the candidates collected from them and ranked by comparing all pairs
+// took twice as many instructions, and 2048 rows of 128256 bf16 logits 232 us.
+#include <utility>
+
 #include "osd.h"
 #include "osd_device.hpp"
 #include "osd_internal.hpp"
@@ -24,7 +36,10 @@
 namespace osd {
 namespace {
 
-constexpr int kCap = 1024;  // candidates that LDS holds
+constexpr int kCap = 1024;   // candidates that LDS holds
+constexpr int kQueue = 128;  // groups of one wave's queue
+constexpr int kBins = 256;   // 16-bit keys of one histogram
+constexpr int kAhead = 8;    // chunks a thread requests ahead
 // Workgroups per launch (a grid stays below 2^32 work-items).
 constexpr int64_t kMaxGrid = int64_t(1) << 21;
 
@@ -43,66 +58,257 @@ struct TopkArgs {
 
 template <int W>
 struct TopkLds {
+    union {
+        int queue[W / kWave][kQueue];  // groups to look through, by wave
+        uint64_t sorted[kCap];         // the candidates in order
+    };
     uint64_t cand[kCap];
-    uint64_t sorted[kCap];
-    uint32_t digit[4][16];
-    uint32_t count[2];
+    uint32_t key[W];             // the threads' maxima
+    uint32_t bin[kBins];         // counts, then where each bin's candidates begin
+    uint32_t fill[kBins];
     double sum[W / kWave];
-    uint32_t ncand;
-    uint32_t maxkey;
+    uint32_t maxkey, tkey, ncand, count;
 };
 
 // Candidates come first: larger logit, then lower id.
 __device__ inline uint64_t composite(uint32_t key, int token) { return (uint64_t(key) << 32) | uint32_t(~token); }
 
-template <typename Fmt, int W, int CPT>
-__global__ __launch_bounds__(W, 4) void topk_row_kernel(TopkArgs a) {
-    constexpr int EPC = Fmt::kPerChunk, NW = W / kWave;
-    __shared__ TopkLds<W> s;
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = tid / kWave;
-    const int64_t n = a.first + blockIdx.x;
-    const int k = a.k;
-    const HeldRow<Fmt, W, CPT> held(a.V);
-    chunk_t c[CPT];
-    held.load(c, a.x + n * a.stride, a.V, tid);
-    if (tid < 64) s.digit[tid / 16][tid % 16] = 0u;
-    if (tid == 0) {
-        s.ncand = 0u;
-        s.maxkey = 0u;
+// Inclusive scan of 32-bit counts over the wave.
+template <int CTRL, int ROWS>
+__device__ inline uint32_t dpp_count_step(uint32_t v) {
+    return v + dpp_sum_src<CTRL, ROWS>(v);
+}
+__device__ inline uint32_t wave_scan_count(uint32_t v) {
+    v = dpp_count_step<kDppRowShr1, 0xF>(v);
+    v = dpp_count_step<kDppRowShr2, 0xF>(v);
+    v = dpp_count_step<kDppRowShr4, 0xF>(v);
+    v = dpp_count_step<kDppRowShr8, 0xF>(v);
+    v = dpp_count_step<kDppRowBcast15, 0xA>(v);
+    v = dpp_count_step<kDppRowBcast31, 0xC>(v);
+    return v;
+}
+__device__ inline uint32_t wave_max_key(uint32_t k) {
+    k = dpp_umax_step<kDppRowShr1, 0xF>(k);
+    k = dpp_umax_step<kDppRowShr2, 0xF>(k);
+    k = dpp_umax_step<kDppRowShr4, 0xF>(k);
+    k = dpp_umax_step<kDppRowShr8, 0xF>(k);
+    k = dpp_umax_step<kDppRowBcast15, 0xA>(k);
+    k = dpp_umax_step<kDppRowBcast31, 0xC>(k);
+    return readlane_u32(k, kWave - 1);
+}
+// A value that every lane holds.
+__device__ inline uint32_t uniform(uint32_t v) { return uint32_t(__builtin_amdgcn_readfirstlane(int(v))); }
+// The lane's place among those of a ballot.
+__device__ inline uint32_t lanes_below(uint64_t ballot) {
+    return __builtin_amdgcn_mbcnt_hi(uint32_t(ballot >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(ballot), 0u));
+}
+
+// The candidates in order, by the whole workgroup: grouped by the 256 16-bit
+// keys from the largest down (the last group holds all below), and each
+// ranked within its group by counting.  (cand is complete; barriers inside and
+// at the end.)
+template <int kW>
+__device__ __forceinline__ void sort_candidates(TopkLds<kW>& s, int nc, uint32_t maxkey) {
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const auto group = [&](uint64_t v) { return min((maxkey >> 16) - uint32_t(v >> 48), uint32_t(kBins - 1)); };
+    if (tid < kBins) s.bin[tid] = s.fill[tid] = 0u;
+    __syncthreads();
+    for (int i = tid; i < nc; i += kW) atomicAdd(&s.bin[group(s.cand[i])], 1u);
+    __syncthreads();
+    if (tid < kWave) {
+        uint32_t* bins = &s.bin[lane * 4];
+        const uint32_t b0 = bins[0], b1 = bins[1], b2 = bins[2], b3 = bins[3];
+        const uint32_t before = wave_scan_count(b0 + b1 + b2 + b3) - (b0 + b1 + b2 + b3);
+        bins[0] = before;
+        bins[1] = before + b0;
+        bins[2] = before + b0 + b1;
+        bins[3] = before + b0 + b1 + b2;
     }
     __syncthreads();
-    held.pad(c, tid);
+    // (In `sorted` for now in any order within a group.)
+    for (int i = tid; i < nc; i += kW) {
+        const uint64_t v = s.cand[i];
+        const uint32_t g = group(v);
+        s.sorted[s.bin[g] + atomicAdd(&s.fill[g], 1u)] = v;
+    }
+    __syncthreads();
+    constexpr int kMost = kCap / kW;
+    uint64_t v[kMost];
+    int rank[kMost];
+#pragma unroll
+    for (int j = 0; j < kMost; ++j) {
+        const int i = tid + j * kW;
+        rank[j] = -1;
+        if (i >= nc) continue;
+        v[j] = s.sorted[i];
+        const uint32_t g = group(v[j]);
+        const int first = int(s.bin[g]), last = first + int(s.fill[g]);
+        rank[j] = first;
+        for (int o = first; o < last; ++o) rank[j] += s.sorted[o] > v[j] ? 1 : 0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kMost; ++j)
+        if (rank[j] >= 0) s.sorted[rank[j]] = v[j];
+    __syncthreads();
+}
 
-    float m = kNegInf;
-    held.each([&](int r) __attribute__((always_inline)) {
+// The largest element of a chunk, NaN if one is.  For bf16 the 16-bit patterns
+// are first compared as f16 numbers, two per packed instruction (see chunks_max):
+// both are sign-magnitude with the exponent above the mantissa; a pattern that is an f16
+// infinity or NaN (a bf16 magnitude of 2^121 or more) leaves an unusable
+// result, and the chunk is decided element by element.
+template <typename Fmt>
+__device__ __forceinline__ float chunk_top(const chunk_t& c) {
+    if constexpr (Fmt::kPerChunk == 8) {
+        typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
+        const auto H = [](uint32_t w) { return __builtin_bit_cast(h2_t, w); };
+        const h2_t h = __builtin_elementwise_maximum(
+            __builtin_elementwise_maximum(__builtin_elementwise_maximum(H(c.x), H(c.y)), H(c.z)), H(c.w));
+        const uint32_t b = __builtin_bit_cast(uint32_t, h);
+        const float lo = __uint_as_float(b << 16), hi = __uint_as_float(b & 0xFFFF0000u);
+        if (__builtin_fabsf(lo) < 0x1p121f && __builtin_fabsf(hi) < 0x1p121f) return fmaxf(lo, hi);
+    }
+    float x = Fmt::get(c, 0);
 #pragma unroll
-        for (int e = 0; e < EPC; ++e) m = max_nan(m, Fmt::get(c[r], e));
-    });
-    const uint32_t mk = order_key(m);
+    for (int e = 1; e < Fmt::kPerChunk; ++e) x = max_nan(x, Fmt::get(c, e));
+    return x;
+}
+
+// f(r) for r = 0 .. N-1 as constants (more steps than the compiler unrolls).
+template <typename F, int... R>
+__device__ __forceinline__ void unrolled(std::integer_sequence<int, R...>, F f) {
+    (f(std::integral_constant<int, R>{}), ...);
+}
+
+// Elements of the row, in chunk order, that `f` is called with: every chunk of the
+// row by the whole workgroup, kAhead of them requested at a time (rare: small
+// code before speed).
+template <typename Fmt, int W, typename F>
+__device__ __forceinline__ void over_row(const char* row, const RowCut<Fmt>& cut, int V, F f) {
+#pragma unroll 1
+    for (int ch = threadIdx.x; ch < cut.nchunks; ch += W) {
+        chunk_t c = V < Fmt::kPerChunk ? load_short<Fmt>(row, V) : load_off(row, cut.off(ch));
+        c = pad_lead<Fmt>(c, cut.lead(ch));
+#pragma unroll
+        for (int e = 0; e < Fmt::kPerChunk; ++e) f(Fmt::get(c, e), cut.token(ch * Fmt::kPerChunk + e));
+    }
+}
+
+template <typename Fmt, int W, int GROUPS, int G>
+__global__ __launch_bounds__(W, W == 1024 ? 4 : 5) void topk_row_kernel(TopkArgs a) {
+    constexpr int EPC = Fmt::kPerChunk, NW = W / kWave, kRounds = GROUPS * G, kKeys = W / kWave;
+    static_assert(W >= kBins && W >= OSD_MAX_TOPK && NW <= 16 && GROUPS <= 16, "");
+    __shared__ TopkLds<W> s;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const int wid = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int64_t n = a.first + blockIdx.x;
+    const int k = a.k;
+    const char* row = a.x + n * a.stride;
+    const RowCut<Fmt> cut(a.V);
+    const int rounds = (cut.nchunks + W - 1) / W;
+    const float c2 = float(a.c2);
+    if (tid == 0) s.ncand = 0u;
+
+    // One sweep: round r is chunk r * W + tid, in group r / G.
+    float gmax[GROUPS], gsum[GROUPS];
+    float ref = kNegInf, shift = 0.0f;  // the sums are relative to 2^shift, shift = ref c2
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+        gmax[g] = kNegInf;
+        gsum[g] = 0.0f;
+    }
     {
-        const float wm = wave_max_nan(m);
-        if (lane == 0) atomicMax(&s.maxkey, order_key(wm));
+        const rsrc_t rs = make_rsrc(row, uint32_t(a.V) * Fmt::kBytes);
+        constexpr int kRing = kRounds < kAhead ? kRounds : kAhead;
+        chunk_t c[kRing];
+        const auto load = [&](int r) __attribute__((always_inline)) {
+            if (r >= rounds) return;
+            int off = (r * W + tid) * 16;
+            if (r == rounds - 1) off = min(off, cut.last_off);
+            c[r % kRing] = a.V < EPC ? load_short<Fmt>(row, a.V)
+                                     : __builtin_bit_cast(chunk_t, __builtin_amdgcn_raw_buffer_load_b128(
+                                                                       rs, off, 0, kStreamAux));
+        };
+#pragma unroll
+        for (int r = 0; r < kRing; ++r) load(r);
+        unrolled(std::make_integer_sequence<int, kRounds>{}, [&](auto step) __attribute__((always_inline)) {
+            constexpr int r = decltype(step)::value;
+            if (r < rounds) {
+                chunk_t x = c[r % kRing];
+                if (r == rounds - 1) x = pad_lead<Fmt>(x, cut.lead(r * W + tid));
+                const float top = chunk_top<Fmt>(x);
+                gmax[r / G] = r % G ? max_nan(gmax[r / G], top) : top;
+                if (a.rest) {
+                    if (!(ref > kNegInf)) {  // the first chunk with a finite logit
+                        ref = top;
+                        shift = top > kNegInf ? fmaxf(top * c2, -1.0e30f) : 0.0f;  // (so low: no mass)
+                    }
+                    float e8[EPC];
+#pragma unroll
+                    for (int e = 0; e < EPC; ++e) e8[e] = exp2_fast(__builtin_fmaf(Fmt::get(x, e), c2, -shift));
+#pragma unroll
+                    for (int w = 1; w < EPC; w <<= 1)
+#pragma unroll
+                        for (int e = 0; e < EPC; e += 2 * w) e8[e] = e8[e] + e8[e + w];
+                    gsum[r / G] = r % G ? gsum[r / G] + e8[0] : e8[0];
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (r + kRing < kRounds) load(r + kRing);
+            }
+        });
     }
-    // The k-th largest maximum, four bits at a time.
-    uint32_t prefix = 0;
+    float m = gmax[0];
 #pragma unroll
-    for (int step = 0; step < 4; ++step) {
-        const int sh = 12 - 4 * step;
-        uint32_t mine = 0;
+    for (int g = 1; g < GROUPS; ++g) m = max_nan(m, gmax[g]);
+    s.key[tid] = order_key(m);
+    __syncthreads();
+    if (wid == 0) {
+        // The k-th largest of the threads' maxima, to the upper 16 bits of its
+        // key: a histogram of the 256 such keys from the largest down (two octaves),
+        // and of the next 256 from the largest below these while they hold fewer
+        // than k.
+        const auto most_below = [&](uint32_t end16) {
+            uint32_t v = 0;
 #pragma unroll
-        for (int d = 1; d < 16; ++d) {
-            const uint32_t cnt = uint32_t(__popcll(__ballot((mk >> 16) >= (prefix | (uint32_t(d) << sh)))));
-            if (lane == d) mine = cnt;
+            for (int j = 0; j < kKeys; ++j) {
+                const uint32_t key = s.key[j * kWave + lane];
+                v = max(v, (key >> 16) < end16 ? key : 0u);
+            }
+            return wave_max_key(v);
+        };
+        uint32_t most = most_below(0x10000u);
+        if (lane == 0) s.maxkey = most;
+        uint32_t tkey = kKeyNegInf + 1, before = 0;
+#pragma unroll 1
+        while (most > kKeyNegInf) {  // (else fewer than k threads met a finite logit)
+            const uint32_t base = most >> 16;
+            uint32_t* bins = &s.bin[lane * 4];
+            bins[0] = bins[1] = bins[2] = bins[3] = 0u;
+#pragma unroll
+            for (int j = 0; j < kKeys; ++j) {
+                const uint32_t at = base - (s.key[j * kWave + lane] >> 16);
+                if (at < uint32_t(kBins)) atomicAdd(&s.bin[at], 1u);
+            }
+            const uint32_t b0 = bins[0], b1 = bins[1], b2 = bins[2], b3 = bins[3];
+            const uint32_t upto = wave_scan_count(b0 + b1 + b2 + b3) + before;
+            const uint64_t full = __ballot(upto >= uint32_t(k));
+            if (full) {
+                const uint32_t left = upto - b0 - b1 - b2 - b3;
+                const uint32_t j = (left + b0 < uint32_t(k)) + (left + b0 + b1 < uint32_t(k)) +
+                                   (left + b0 + b1 + b2 < uint32_t(k));
+                const int l = __builtin_ctzll(full);
+                tkey = max(tkey, (base - uint32_t(l) * 4 - readlane_u32(j, l)) << 16);
+                break;
+            }
+            before = readlane_u32(upto, kWave - 1);
+            most = most_below(base < uint32_t(kBins) ? 0u : base - uint32_t(kBins) + 1);
         }
-        if (lane < 16) atomicAdd(&s.digit[step][lane], mine);
-        __syncthreads();
-        const uint32_t total = s.digit[step][lane & 15];
-        const int d = __popcll(__ballot(lane >= 1 && lane < 16 && total >= uint32_t(k)));
-        prefix |= uint32_t(d) << sh;
+        if (lane == 0) s.tkey = tkey;
     }
-    const uint32_t maxkey = s.maxkey;
-    const bool empty = maxkey >= kKeyPosInf || maxkey <= kKeyNegInf;  // an infinity, a NaN, no finite logit
-    if (empty) {
+    __syncthreads();
+    const uint32_t maxkey = uniform(s.maxkey);
+    if (maxkey >= kKeyPosInf || maxkey <= kKeyNegInf) {  // an infinity, a NaN, no finite logit
         for (int r = tid; r < k; r += W) {
             a.ids[n * k + r] = -1;
             if constexpr (EPC == 8)
@@ -114,101 +320,108 @@ __global__ __launch_bounds__(W, 4) void topk_row_kernel(TopkArgs a) {
         if (tid == 0 && a.tokens) a.tokens[n] = -1;
         return;
     }
-    // Candidates: logits above tx, and those equal to it up to token ttok.
-    float tx = key_float(max(prefix << 16, kKeyNegInf + 1));
-    int ttok = 0x7FFFFFFF;
-    double S = 0.0;
-    const float c2 = float(a.c2), top = key_float(maxkey);
+    const float top = key_float(maxkey);
     const auto weight = [&](float x) __attribute__((always_inline)) { return exp2_fast((x - top) * c2); };
-    // Collects the candidates; the others among the logits equal to tx are
-    // added to S.
-    const auto collect = [&]() __attribute__((always_inline)) {
-        if (!(m >= tx)) return;
-        held.each([&](int r) __attribute__((always_inline)) {
-            asm volatile("" : "+v"(c[r]));
-            if (!(chunk_max<Fmt>(c[r]) >= tx)) return;
+    // Candidates: logits above tx, and those equal to it up to token ttok.
+    float tx = key_float(uniform(s.tkey));
+    int ttok = 0x7FFFFFFF;
+    // The thread's groups to look through: those that reach the threshold, and all
+    // of them where the sums may have left fp32's range (a later chunk more than
+    // 2^100 above the first) or the shift its precision.
+    uint32_t flags = 0;
 #pragma unroll
-            for (int e = 0; e < EPC; ++e) {
-                const float x = Fmt::get(c[r], e);
-                if (!(x >= tx)) continue;
-                const int tok = held.token(r, e, opaque_tid());
-                if (x > tx || tok <= ttok) {
-                    const uint32_t p = atomicAdd(&s.ncand, 1u);
-                    if (p < uint32_t(kCap)) s.cand[p] = composite(order_key(x), tok);
-                } else if (a.rest) {
-                    S += double(weight(x));
+    for (int g = 0; g < GROUPS; ++g) flags |= uint32_t(gmax[g] >= tx) << g;
+    const uint32_t every = (1u << ((rounds + G - 1) / G)) - 1u;
+    if (a.rest && ((m - ref) * c2 > 100.0f || __builtin_fabsf(top) * c2 > 65536.0f)) flags = every;
+    int nc = 0;
+    double S = 0.0;
+#pragma unroll 1
+    for (int pass = 0;; ++pass) {
+        S = 0.0;
+        int* queue = s.queue[wid];
+        const uint32_t mine = uint32_t(__popc(flags)), upto = wave_scan_count(mine);
+        const int total = int(readlane_u32(upto, kWave - 1));
+#pragma unroll 1
+        for (int first = 0; first < total; first += kQueue) {
+            int at = int(upto - mine) - first;
+            for (uint32_t f = flags; f; f &= f - 1, ++at)
+                if (uint32_t(at) < uint32_t(kQueue)) queue[at] = (__builtin_ctz(f) * G) * W + tid;  // its first chunk
+            const int elements = min(total - first, kQueue) * G * EPC;
+            constexpr int kStep = 4;  // elements a lane requests at once
+#pragma unroll 1
+            for (int i0 = lane; i0 - lane < elements; i0 += kStep * kWave) {
+                float x[kStep];
+                int token[kStep];
+#pragma unroll
+                for (int j = 0; j < kStep; ++j) {
+                    const int i = i0 + j * kWave;
+                    x[j] = kNegInf;
+                    if (i < elements) {
+                        token[j] = (queue[i / (G * EPC)] + (i / EPC) % G * W) * EPC + i % EPC;
+                        if (token[j] < a.V) x[j] = Fmt::load_one(row, token[j]);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < kStep; ++j) {
+                    const bool in = x[j] > tx || (x[j] == tx && token[j] <= ttok);
+                    const uint64_t ins = __ballot(in);
+                    if (ins) {
+                        uint32_t p = 0;
+                        if (lane == 0) p = atomicAdd(&s.ncand, uint32_t(__popcll(ins)));
+                        p = readlane_u32(p, 0) + lanes_below(ins);
+                        if (in && p < uint32_t(kCap)) s.cand[p] = composite(order_key(x[j]), token[j]);
+                    }
+                    if (a.rest && !in) S += double(weight(x[j]));
                 }
             }
-        });
-    };
-    collect();
-    __syncthreads();
-    if (s.ncand > uint32_t(kCap)) {
+        }
+        __syncthreads();
+        nc = int(uniform(s.ncand));
+        if (nc <= kCap || pass) break;
         // Bisection for the largest key that k logits reach, then for the id up
         // to which its equals fill the record: `lo` always has k, `hi` has not.
         uint64_t lo = composite(order_key(tx), 0x7FFFFFFF), hi = composite(maxkey, 0) + 1;
-        int flip = 0;
 #pragma unroll 1
         while (hi - lo > 1) {
             const uint64_t mid = lo + (hi - lo) / 2;
-            const uint32_t mkey = uint32_t(mid >> 32), mtok = ~uint32_t(mid);
+            const float mx = key_float(uint32_t(mid >> 32));
+            const uint32_t mtok = ~uint32_t(mid);
+            if (tid == 0) s.count = 0u;
+            __syncthreads();
             uint32_t v = 0;
-            held.each([&](int r) __attribute__((always_inline)) {
-                asm volatile("" : "+v"(c[r]));
-#pragma unroll
-                for (int e = 0; e < EPC; ++e) {
-                    const uint32_t key = order_key(Fmt::get(c[r], e));
-                    v += key > mkey || (key == mkey && uint32_t(held.token(r, e, opaque_tid())) <= mtok) ? 1u : 0u;
-                }
+            over_row<Fmt, W>(row, cut, a.V, [&](float x, int token) __attribute__((always_inline)) {
+                v += uint32_t(int(x > mx) | (int(x == mx) & int(uint32_t(token) <= mtok)));
             });
+            v = readlane_u32(wave_scan_count(v), kWave - 1);
+            if (lane == 0) atomicAdd(&s.count, v);
             __syncthreads();
-            if (tid == 0) s.count[flip] = 0u;
-            __syncthreads();
-            atomicAdd(&s.count[flip], v);
-            __syncthreads();
-            if (s.count[flip] >= uint32_t(k))
+            if (uniform(s.count) >= uint32_t(k))
                 lo = mid;
             else
                 hi = mid;
-            flip ^= 1;
+            __syncthreads();
         }
         tx = key_float(uint32_t(lo >> 32));
         ttok = int(~uint32_t(lo));
-        __syncthreads();
         if (tid == 0) s.ncand = 0u;
-        S = 0.0;
         __syncthreads();
-        collect();
-        __syncthreads();
+        // (Groups below the new threshold keep their sums.)
+        if (flags != every || !a.rest) {
+            flags = 0;
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) flags |= uint32_t(gmax[g] >= tx) << g;
+        }
     }
-    const int nc = int(s.ncand);
-    for (int i = tid; i < nc; i += W) {
-        const uint64_t me = s.cand[i];
-        int rank = 0;
-        for (int j = 0; j < nc; ++j) rank += s.cand[j] > me ? 1 : 0;
-        s.sorted[rank] = me;
-    }
-    // The mass outside: logits below the threshold, relative to the row's
-    // largest.
+    // The mass outside, relative to the row's largest logit.
     if (a.rest) {
-        held.each([&](int r) __attribute__((always_inline)) {
-            asm volatile("" : "+v"(c[r]));
-            float e8[EPC];
+        float t = 0.0f;
 #pragma unroll
-            for (int e = 0; e < EPC; ++e) {
-                const float x = Fmt::get(c[r], e);
-                e8[e] = x < tx ? weight(x) : 0.0f;
-            }
-#pragma unroll
-            for (int w = 1; w < EPC; w <<= 1)
-#pragma unroll
-                for (int e = 0; e < EPC; e += 2 * w) e8[e] = e8[e] + e8[e + w];
-            S += double(e8[0]);
-        });
+        for (int g = 0; g < GROUPS; ++g) t += (flags >> g) & 1u ? 0.0f : gsum[g];
+        if (t > 0.0f) S += double(t) * exp2_f64(double(shift) - double(top) * double(c2));
         S = wave_sum(S);
         if (lane == 0) s.sum[wid] = S;
     }
-    __syncthreads();
+    sort_candidates<W>(s, nc, maxkey);
     for (int r = tid; r < k; r += W) {
         const uint64_t v = s.sorted[r];
         const bool in = r < nc;
@@ -221,13 +434,12 @@ __global__ __launch_bounds__(W, 4) void topk_row_kernel(TopkArgs a) {
     }
     if (wid == 0 && a.rest) {
         double t = lane < NW ? s.sum[lane] : 0.0;
-        for (int r = k + lane; r < nc; r += kWave)
-            t += double(weight(key_float(uint32_t(s.sorted[r] >> 32))));
+        for (int r = k + lane; r < nc; r += kWave) t += double(weight(key_float(uint32_t(s.sorted[r] >> 32))));
         t = wave_sum(t);
-        if (lane == 0) a.rest[n] = t > 0.0 ? float(log2_pos(t) * kLn2) : kNegInf;
+        if (lane == 0) a.rest[n] = t > 0.0 ? float(log2_f64(t) * kLn2) : kNegInf;
     }
     if (wid == NW - 1 && a.tokens) {
-        const int held = nc < k ? nc : k;
+        const int held = min(nc, k);
         if (a.c2 == 0.0) {
             if (lane == 0) a.tokens[n] = int(~uint32_t(s.sorted[0]));
             return;
@@ -258,27 +470,35 @@ __global__ __launch_bounds__(W, 4) void topk_row_kernel(TopkArgs a) {
     }
 }
 
-template <typename Fmt, int W, int CPT>
+template <typename Fmt, int W, int GROUPS, int G>
 hipError_t launch_tile(const TopkLaunch& L, TopkArgs a) {
     for (int64_t f = 0; f < L.N; f += kMaxGrid) {
         a.first = f;
         const unsigned g = unsigned(L.N - f < kMaxGrid ? L.N - f : kMaxGrid);
-        const hipError_t e = launch_kernel(&topk_row_kernel<Fmt, W, CPT>, dim3(g), dim3(W), 0, L.stream, a);
+        const hipError_t e = launch_kernel(&topk_row_kernel<Fmt, W, GROUPS, G>, dim3(g), dim3(W), 0, L.stream, a);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
 
 template <typename Fmt>
-hipError_t launch_fmt(const TopkLaunch& L, TopkArgs a) {
+hipError_t launch_fmt(const TopkLaunch& L, const TopkArgs& a) {
     const int chunks = (L.V + Fmt::kPerChunk - 1) / Fmt::kPerChunk;
-    if (chunks <= 256) return launch_tile<Fmt, 256, 1>(L, a);
-    if (chunks <= 1024) return launch_tile<Fmt, 256, 4>(L, a);
-    if (chunks <= 2048) return launch_tile<Fmt, 512, 4>(L, a);
-    if (chunks <= 4096) return launch_tile<Fmt, 512, 8>(L, a);
-    if (chunks <= 8192) return launch_tile<Fmt, 1024, 8>(L, a);
-    if (chunks <= 16384) return launch_tile<Fmt, 1024, 16>(L, a);
-    return hipErrorInvalidValue;
+    if (chunks <= 256) return launch_tile<Fmt, 256, 1, 1>(L, a);
+    if (chunks <= 1024) return launch_tile<Fmt, 256, 4, 1>(L, a);
+    if (chunks > 16384) return hipErrorInvalidValue;
+    if (L.N <= L.cus) {
+        if (chunks <= 4096) return launch_tile<Fmt, 1024, 4, 1>(L, a);
+        return launch_tile<Fmt, 1024, 16, 1>(L, a);
+    }
+    if (L.N <= 3 * L.cus || chunks > 8192) {
+        if (chunks <= 4096) return launch_tile<Fmt, 512, 8, 1>(L, a);
+        if (chunks <= 8192) return launch_tile<Fmt, 512, 16, 1>(L, a);
+        return launch_tile<Fmt, 512, 16, 2>(L, a);
+    }
+    if (chunks <= 2048) return launch_tile<Fmt, 256, 8, 1>(L, a);
+    if (chunks <= 4096) return launch_tile<Fmt, 256, 16, 1>(L, a);
+    return launch_tile<Fmt, 256, 16, 2>(L, a);
 }
 
 }  // namespace

@@ -65,6 +65,26 @@ __device__ inline uint32_t order_key(float x) { return x == x ? float_key(x + 0.
 constexpr uint32_t kKeyNegInf = 0x007FFFFFu;
 constexpr uint32_t kKeyPosInf = 0xFF800000u;
 
+// The elements of chunks, in one sweep over a held row.  For bf16 the shift and
+// the mask that unpack a pair are opaque, anew in each sweep: the unpacked values
+// of one sweep are then not kept for the next, which would double the registers
+// of a row.  (An opaque copy of the chunks themselves did that in places.)
+template <typename Fmt>
+struct Sweep {
+    uint32_t shift = 16u, mask = 0xFFFF0000u;
+    __device__ __forceinline__ Sweep() {
+        if constexpr (Fmt::kPerChunk == 8) asm volatile("" : "+s"(shift), "+s"(mask));
+    }
+    __device__ __forceinline__ float get(const chunk_t& c, int e) const {
+        if constexpr (Fmt::kPerChunk == 8) {
+            const uint32_t w = (e >> 1) == 0 ? c.x : (e >> 1) == 1 ? c.y : (e >> 1) == 2 ? c.z : c.w;
+            return __uint_as_float((e & 1) ? w & mask : w << shift);
+        } else {
+            return Fmt::get(c, e);
+        }
+    }
+};
+
 // A row of any length and alignment held in registers: chunk r * W + tid in
 // round r of its `rounds` rounds (at most CPT).  Every round is a basic block of
 // its own (a scalar branch: rounds past the row cost nothing), which also keeps the

@@ -26,6 +26,7 @@ def topk(**kw):
     (dict(T=-1.0), -1), (dict(T=NAN), -1), (dict(T=INF), -1), (dict(T=0.0), -1),  # rest at T == 0
     (dict(V=1 << 20, stride=1 << 20), -2), (dict(dtype=0, V=65537, stride=65537), -2),
     (dict(ws=FAKE, wsb=8), -4), (dict(ws=ODD, wsb=1 << 30), -4),
+    (dict(V=32769, stride=32769), -4), (dict(dtype=0, V=16385, stride=16385), -4),  # split rows need one
 ])
 def test_topk_rejects_bad_arguments(kw, status):
     assert topk(**kw) == status
