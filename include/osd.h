@@ -428,6 +428,8 @@ int osd_topk(const void* logits, int64_t row_stride, int dtype, int N, int V, in
  *               gaps); any other overlap with them is refused.  Outputs must not
  *               overlap the other inputs
  * workspace     osd_distill_topk_workspace_bytes(B, K) zero-initialised bytes
+ *               (counters among them are left zero; the rest keeps scratch that
+ *               later calls need not find cleared, at any B, K, V, k)
  *
  * A row whose record is empty, names a token outside [0, V) (-1: an empty slot)
  * or one token twice, or holds a NaN or +inf, and a student row with a NaN, +inf or

@@ -216,7 +216,8 @@ struct LdsCache {
 // in row order (D = 0 for masked-out rows) and posts the partial at the
 // device-wide coherence point; the last workgroup to finish adds the
 // partials in workgroup order, counts the mask, writes the loss and zeroes
-// what it read.  The result depends only on the grid size.
+// what it read.  The result depends only on the grid size.  (Or G workgroups of
+// a larger grid post, numbered by `post`.)
 // What the tail needs, staged in LDS at kernel start so that none of it stays
 // in registers across the row loop.
 struct LossTail {
@@ -229,7 +230,7 @@ struct LossTail {
 };
 
 template <int W>
-__device__ inline void finish_loss(const LossTail& a, const double* s_part) {
+__device__ inline void finish_loss(const LossTail& a, const double* s_part, uint32_t post = blockIdx.x) {
     __shared__ int s_last;
     __shared__ double s_sum[W / kWave], s_cnt[W / kWave];
     // Thread indices recomputed from an opaque copy: values derived from them
@@ -240,7 +241,7 @@ __device__ inline void finish_loss(const LossTail& a, const double* s_part) {
     const int G = a.G;
     __syncthreads();
     if (tid == 0) {
-        __hip_atomic_exchange(&a.row_ws[blockIdx.x], s_part[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_exchange(&a.row_ws[post], s_part[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         s_last = int(arrive(a.done)) == G - 1;  // after the post completed
     }
     __syncthreads();

@@ -653,16 +653,19 @@ int osd_verify_tree(const void* target_logits, const void* draft_logits, int dty
 // ---------------------------------------------------------------------------
 namespace {
 
+// What has to be zero between calls lies at one place whatever the sizes.
 struct DistillTopkWs {
-    size_t done, partials, total;
+    size_t done, partials, parts, x, total;
 };
 DistillTopkWs distill_topk_layout(int B, int K) {
     DistillTopkWs w;
     const int64_t rows = int64_t(B) * K;
-    const size_t groups = size_t(rows < osd::kMaxDistillTopkGroups ? rows : osd::kMaxDistillTopkGroups);
+    const size_t split = size_t(rows < osd::kDistillTopkSplitRows ? rows : osd::kDistillTopkSplitRows);
     w.done = 0;
     w.partials = kAlign;
-    w.total = w.partials + round_up(groups * 8, kAlign);
+    w.parts = w.partials + osd::kMaxDistillTopkGroups * sizeof(double);
+    w.x = w.parts + (osd::kDistillTopkParts + split * osd::kDistillTopkLongest) * sizeof(osd::DistillTopkPart);
+    w.total = round_up(w.x + split * OSD_MAX_TOPK * sizeof(float), kAlign);
     return w;
 }
 
@@ -767,6 +770,8 @@ int osd_distill_topk_loss_grad(const int32_t* teacher_ids, const void* teacher_t
     char* w = static_cast<char*>(workspace);
     L.done_counter = reinterpret_cast<uint32_t*>(w + ws.done);
     L.partials = reinterpret_cast<double*>(w + ws.partials);
+    L.parts = reinterpret_cast<osd::DistillTopkPart*>(w + ws.parts);
+    L.split_x = reinterpret_cast<float*>(w + ws.x);
     L.stream = static_cast<hipStream_t>(stream);
     L.cus = device_cus(L.stream);
     return osd::launch_distill_topk(L) == hipSuccess ? OSD_OK : OSD_ERR_DEVICE;

@@ -265,6 +265,15 @@ inline bool topk_needs_workspace(int V, int per_chunk) { return V > kTopkRowChun
 hipError_t launch_topk(const TopkLaunch& L);
 
 // Distillation from teacher records (distill_topk.hip).
+// Rows split over workgroups, at most.  A part is what one workgroup found; kDistillTopkParts of
+// them, and kDistillTopkLongest more a row, suffice (distill_topk.hip, segments).
+constexpr int kDistillTopkSplitRows = 512;
+constexpr int kDistillTopkParts = 1024;
+constexpr int kDistillTopkLongest = 10;
+struct DistillTopkPart {
+    double sum;  // of the segment's others' exponentials, relative to
+    float top;   // the largest of them
+};
 struct DistillTopkLaunch {
     const int32_t* ids;
     const void* top;
@@ -283,10 +292,12 @@ struct DistillTopkLaunch {
     void* grad_out;
     double* partials;        // [min(B*K, kMaxDistillTopkGroups)] zero on entry and exit
     uint32_t* done_counter;  // [1] zero on entry and exit
+    DistillTopkPart* parts;  // [kDistillTopkParts + rows * kDistillTopkLongest]
+    float* split_x;          // [rows, OSD_MAX_TOPK], rows = min(B*K, kDistillTopkSplitRows)
     int cus;
     hipStream_t stream;
 };
-// Workgroups of one launch at most.
+// Workgroups of one launch at most (rows in one each).
 constexpr int kMaxDistillTopkGroups = 8192;
 hipError_t launch_distill_topk(const DistillTopkLaunch& L);
 

@@ -85,6 +85,31 @@ struct Sweep {
     }
 };
 
+// Stores chunk ch of the row at the descriptor's base (whole: it is known to have no
+// padding).
+template <typename Fmt>
+__device__ __forceinline__ void store_chunk(const RowCut<Fmt>& cut, rsrc_t rs, int ch, bool whole, const chunk_t& c) {
+    if (whole || ch < cut.nfull) {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(__attribute__((ext_vector_type(4))) int, c), rs,
+                                               ch * 16, 0, kStreamAux);
+        return;
+    }
+    if (ch >= cut.nchunks) return;
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+    int lead = cut.dup;
+    asm volatile("" : "+v"(lead));  // compared here, not hoisted (see pad_lead)
+#pragma unroll
+    for (int e = 0; e < Fmt::kPerChunk; ++e) {
+        if (e < lead) continue;
+        const int off = cut.last_off + e * Fmt::kBytes;
+        if constexpr (Fmt::kPerChunk == 8)
+            __builtin_amdgcn_raw_buffer_store_b16(static_cast<unsigned short>(w[e >> 1] >> (16 * (e & 1))), rs, off, 0,
+                                                  0);
+        else
+            __builtin_amdgcn_raw_buffer_store_b32(w[e], rs, off, 0, 0);
+    }
+}
+
 // A row of any length and alignment held in registers: chunk r * W + tid in
 // round r of its `rounds` rounds (at most CPT).  Every round is a basic block of
 // its own (a scalar branch: rounds past the row cost nothing), which also keeps the
@@ -135,28 +160,34 @@ struct HeldRow {
     __device__ int token(int r, int e, int tid) const {
         return cut.token((r * W + tid) * Fmt::kPerChunk + e);
     }
-    // Stores a chunk of the row at the descriptor's base.
     __device__ __forceinline__ void store(rsrc_t rs, int r, const chunk_t& c, int tid) const {
-        const int ch = r * W + tid;
-        if (r < rounds - 1 || ch < cut.nfull) {
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(__attribute__((ext_vector_type(4))) int, c), rs,
-                                                   ch * 16, 0, kStreamAux);
-            return;
-        }
-        if (ch >= cut.nchunks) return;
-        const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-        int lead = cut.dup;
-        asm volatile("" : "+v"(lead));  // compared here, not hoisted (see pad_lead)
+        store_chunk(cut, rs, r * W + tid, r < rounds - 1, c);
+    }
+};
+
+// W * CPT chunks of a row from chunk `start` on, in a workgroup of W threads' registers: every
+// round is loaded, past the row's end its last chunk, padded.
+template <typename Fmt, int W, int CPT>
+struct HeldSegment {
+    RowCut<Fmt> cut;
+    int start;
+    bool whole;  // no padding in it
+    __device__ HeldSegment(int V, int start) : cut(V), start(start), whole(start + CPT * W <= cut.nfull) {}
+    template <int AUX>
+    __device__ __forceinline__ void load(chunk_t (&c)[CPT], const void* row, int V, int tid) const {
+        const rsrc_t rs = make_rsrc(row, uint32_t(V) * Fmt::kBytes);
 #pragma unroll
-        for (int e = 0; e < Fmt::kPerChunk; ++e) {
-            if (e < lead) continue;
-            const int off = cut.last_off + e * Fmt::kBytes;
-            if constexpr (Fmt::kPerChunk == 8)
-                __builtin_amdgcn_raw_buffer_store_b16(static_cast<unsigned short>(w[e >> 1] >> (16 * (e & 1))), rs, off,
-                                                      0, 0);
-            else
-                __builtin_amdgcn_raw_buffer_store_b32(w[e], rs, off, 0, 0);
-        }
+        for (int r = 0; r < CPT; ++r)
+            c[r] = __builtin_bit_cast(chunk_t, __builtin_amdgcn_raw_buffer_load_b128(
+                                                   rs, min((start + r * W + tid) * 16, cut.last_off), 0, AUX));
+    }
+    __device__ __forceinline__ void pad(chunk_t (&c)[CPT], int tid) const {
+        if (whole) return;
+#pragma unroll
+        for (int r = 0; r < CPT; ++r) c[r] = pad_lead<Fmt>(c[r], cut.lead(start + r * W + tid));
+    }
+    __device__ __forceinline__ void store(rsrc_t rs, int r, const chunk_t& c, int tid) const {
+        store_chunk(cut, rs, start + r * W + tid, whole, c);
     }
 };
 

@@ -105,6 +105,34 @@ def test_long_rows(osd, V, k, dtype, kind):
     check(got, ids, top, rest, s, kind, beta, tau, None, f"V={V} k={k} {kind} {dtype}")
 
 
+@pytest.mark.parametrize("V,k,dtype,B", [(12289, 33, "bf16", 200), (30011, 64, "bf16", 200), (50257, 64, "bf16", 200),
+                                         (128256, 256, "bf16", 150), (5003, 200, "f32", 300), (9001, 64, "f32", 300),
+                                         (32003, 20, "f32", 200), (65536, 100, "f32", 150)])
+def test_many_rows_each_as_if_alone(osd, V, k, dtype, B):
+    """Five rows over and over, so that there are many: each repeat has the bits
+    of the first, and those are right; without the gradient too."""
+    import torch
+    n, tau = 5, 1.0
+    t = as_dtype(rows("normal", n, V, V + 2), dtype)
+    s = as_dtype(rows("normal", n, V, V + 3), dtype)
+    ids, top, rest = record(t, k, tau)
+    d = [to_device(a) for a in (ids, top, rest, s)]
+    for kind in ("fkl", "rkl", "jsd"):
+        ids_d, top_d, rest_d, s_d = (x.repeat((B // n,) + (1,) * (x.dim() - 1)) for x in d)
+        args = (ids_d.view(B, 1, k), top_d.view(B, 1, k), rest_d.view(B, 1), s_d.view(B, 1, V), kind, 0.5, tau)
+        loss, rl, g = osd.osd_distill_topk_loss_grad(*args)
+        assert torch.equal(rl.view(-1, n), rl[:n].view(1, n).expand(B // n, n))
+        assert torch.equal(g.view(-1, n, V), g[:n].view(1, n, V).expand(B // n, n, V))
+        alone = loss.clone()
+        alone[1] = alone[1] * n / B
+        check((alone, rl[:n], g[:n]), ids, top, rest, s, kind, 0.5, tau, None, f"V={V} k={k} {kind} {dtype} B={B}")
+        loss, rl, g = osd.osd_distill_topk_loss_grad(*args, grad=False)
+        alone = loss.clone()
+        alone[1] = alone[1] * n / B
+        assert torch.equal(rl.view(-1, n), rl[:n].view(1, n).expand(B // n, n))
+        check((alone, rl[:n], None), ids, top, rest, s, kind, 0.5, tau, None, f"no grad V={V} k={k} {kind} {dtype}")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("kind", ["fkl", "rkl", "jsd"])
 @pytest.mark.parametrize("B", [1, 37, 700])
@@ -125,10 +153,11 @@ def test_masks_and_row_counts(osd, B, kind, dtype):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("student", ["ties", "equal", "lowest", "masked", "masked_lowest", "peak", "bad"])
 @pytest.mark.parametrize("kind", ["fkl", "rkl", "jsd"])
-def test_student_kinds(osd, student, kind, dtype):
+@pytest.mark.parametrize("V", [3001, 12007])
+def test_student_kinds(osd, V, student, kind, dtype):
     """Masked vocabularies (-inf, the type's lowest), rows of equal logits,
     rows without a softmax."""
-    B, K, V, k, tau, beta = 5, 1, 3001, 33, 1.0, 0.5
+    B, K, k, tau, beta = 5, 1, 33, 1.0, 0.5
     t = as_dtype(rows("normal", B, V, 6), dtype)
     s = as_dtype(rows(student, B, V, 7, dtype), dtype)
     ids, top, rest = record(t, k, tau)
@@ -142,12 +171,13 @@ def test_student_kinds(osd, student, kind, dtype):
     check(got, ids, top, rest, s, kind, beta, tau, None, f"{student} {kind} {dtype}")
 
 
+@pytest.mark.parametrize("V", [2003, 12007])
 @pytest.mark.parametrize("kind", ["fkl", "rkl", "jsd"])
-def test_teacher_kinds_and_bad_records(osd, kind):
+def test_teacher_kinds_and_bad_records(osd, kind, V):
     """Rows whose teacher is masked to fewer tokens than slots, uniform, or has
     no record; records with an id twice, out of range, NaN, +inf, an empty first
     slot."""
-    V, k, tau, beta = 2003, 40, 1.0, 0.5
+    k, tau, beta = 40, 1.0, 0.5
     for tk in ("masked", "lowest", "equal", "bad"):
         t, s = as_dtype(rows(tk, 6, V, 8, "f32"), "f32"), as_dtype(rows("normal", 6, V, 9), "f32")
         if tk == "masked":
@@ -278,21 +308,60 @@ def test_guard_bands(osd):
         es = d[3].element_size()
         sizes = [8, n * 4, n * V * es]
         bufs = [torch.full((z + 8192,), 0x5A, dtype=torch.uint8, device="cuda") for z in sizes]
-        ws = torch.zeros(osd.lib().osd_distill_topk_workspace_bytes(B, K), dtype=torch.uint8, device="cuda")
+        size = osd.lib().osd_distill_topk_workspace_bytes(B, K)
+        ws = torch.zeros(size + 8192, dtype=torch.uint8, device="cuda")
+        ws[:4096] = ws[4096 + size:] = 0x5A
         p = lambda x, o=0: ctypes.c_void_p(x.data_ptr() + o)
         st = osd.lib().osd_distill_topk_loss_grad(
             p(d[0]), p(d[1]), p(d[2]), K, k, p(d[3]), K * V, binding.OSD_BF16 if es == 2 else binding.OSD_F32, B, K,
-            V, None, 2, 0.5, 1.0, p(bufs[0], 4096), p(bufs[1], 4096), p(bufs[2], 4096), p(ws), ws.numel(), None)
+            V, None, 2, 0.5, 1.0, p(bufs[0], 4096), p(bufs[1], 4096), p(bufs[2], 4096), p(ws, 4096), size, None)
         assert st == 0
         torch.cuda.synchronize()
-        assert not ws.any(), "the workspace is left zero"
-        for b, z in zip(bufs, sizes):
+        for b, z in zip(bufs + [ws], sizes + [size]):
             assert (b[:4096] == 0x5A).all() and (b[4096 + z:] == 0x5A).all()
 
 
-def test_graph(osd):
+def test_one_workspace_at_many_sizes(osd):
+    """What a call leaves in the workspace does not reach later calls of other
+    sizes, rows split over workgroups or not."""
+    import ctypes
     import torch
-    B, K, V, k = 9, 4, 5003, 32
+    from paper_2310_07177_amd import binding
+    shapes = [(4, 3, 32003, 64, "bf16"), (1, 1, 70001, 8, "bf16"), (3, 1, 1001, 20, "f32"), (31, 20, 2500, 256, "f32"),
+              (2, 3, 50257, 256, "f32"), (1, 2, 300, 300 - 44, "bf16"), (40, 10, 9001, 33, "bf16")]
+    calls = []
+    for B, K, V, k, dtype in shapes:
+        n = B * K
+        t, s = as_dtype(rows("normal", n, V, 51), dtype), as_dtype(rows("normal", n, V, 52), dtype)
+        ids, top, rest = record(t, k, 1.0)
+        d = [to_device(a) for a in (ids, top, rest, s)]
+        out = [torch.empty(z, dtype=torch.uint8, device="cuda") for z in (8, n * 4, n * V * d[3].element_size())]
+        calls.append((B, K, V, k, d, out))
+    size = max(osd.lib().osd_distill_topk_workspace_bytes(B, K) for B, K, *_ in shapes)
+
+    def run(call, ws):
+        B, K, V, k, d, out = call
+        p = lambda x: ctypes.c_void_p(x.data_ptr())
+        st = osd.lib().osd_distill_topk_loss_grad(
+            p(d[0]), p(d[1]), p(d[2]), K, k, p(d[3]), K * V,
+            binding.OSD_BF16 if d[3].element_size() == 2 else binding.OSD_F32, B, K, V, None, 2, 0.5, 1.0, p(out[0]),
+            p(out[1]), p(out[2]), p(ws), ws.numel(), None)
+        assert st == 0
+        torch.cuda.synchronize()
+        return [o.clone() for o in out]
+
+    want = [run(c, torch.zeros(size, dtype=torch.uint8, device="cuda")) for c in calls]
+    ws = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    for _ in range(2):
+        for c, w in zip(calls, want):
+            for g, x in zip(run(c, ws), w):
+                assert (g == x).all(), c[:4]
+
+
+@pytest.mark.parametrize("V", [5003, 20011])
+def test_graph(osd, V):
+    import torch
+    B, K, k = 9, 4, 32
     data = []
     for i in range(3):
         t, s = as_dtype(rows("normal", B * K, V, 30 + i), "bf16"), as_dtype(rows("normal", B * K, V, 40 + i), "bf16")
