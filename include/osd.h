@@ -383,22 +383,16 @@ int osd_sample(const void* p_logits, int64_t p_row_stride,
  * top_out       out [N, k] dtype
  * rest_out      out [N] fp32, nullable
  * tokens_out    out [N] int32, nullable; -1 for an empty record
- * workspace     osd_topk_workspace_bytes(N, k) zero-initialised bytes (counters
- *               among them are left zero; the rest keeps scratch that later calls
- *               need not find cleared, at any N, V, k).  May be NULL for rows of up
- *               to 32768 bf16 or 16384 fp32 logits, which one workgroup holds
  *
  * Errors: OSD_ERR_INVALID_ARG for sizes or k out of range, a bad dtype, T < 0,
  * inf or NaN, rest_out at T == 0, a needed pointer NULL or a row stride < V;
- * OSD_ERR_UNSUPPORTED for V > osd_max_vocab(dtype); OSD_ERR_WORKSPACE for a
- * workspace that is missing, too small or misaligned; OSD_ERR_DEVICE if the launch
+ * OSD_ERR_UNSUPPORTED for V > osd_max_vocab(dtype); OSD_ERR_DEVICE if the launch
  * fails.  Nothing is enqueued on an error.
  */
 #define OSD_MAX_TOPK 256
-size_t osd_topk_workspace_bytes(int N, int k);
 int osd_topk(const void* logits, int64_t row_stride, int dtype, int N, int V, int k, float temperature,
              const float* u, int32_t* ids_out, void* top_out, float* rest_out, int32_t* tokens_out,
-             void* workspace, size_t workspace_bytes, void* stream);
+             void* stream);
 
 /*
  * osd_distill_topk_loss_grad -- osd_distill_loss_grad from teacher records.

@@ -32,7 +32,7 @@ EXPORTS = ("osd_max_vocab", "osd_status_string", "osd_verify_workspace_bytes", "
            "osd_distill_workspace_bytes", "osd_distill_loss_grad", "osd_verify_distill_workspace_bytes",
            "osd_verify_distill", "osd_verify_distill_rejected", "osd_verify_tree_workspace_bytes", "osd_verify_tree",
            "osd_sample_workspace_bytes", "osd_sample", "osd_shard_verify_stats", "osd_shard_verify_mass",
-           "osd_shard_verify_draw", "osd_topk_workspace_bytes", "osd_topk", "osd_distill_topk_workspace_bytes",
+           "osd_shard_verify_draw", "osd_topk", "osd_distill_topk_workspace_bytes",
            "osd_distill_topk_loss_grad", "osd_verify_topk_workspace_bytes", "osd_verify_topk")
 
 _lib = None
@@ -97,10 +97,8 @@ def lib():
             L.osd_shard_verify_draw.restype = i32
             L.osd_shard_verify_draw.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, f32,
                                                 vp, vp, vp, vp, vp]
-            L.osd_topk_workspace_bytes.restype = sz
-            L.osd_topk_workspace_bytes.argtypes = [i32, i32]
             L.osd_topk.restype = i32
-            L.osd_topk.argtypes = [vp, i64, i32, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, sz, vp]
+            L.osd_topk.argtypes = [vp, i64, i32, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp]
             L.osd_distill_topk_workspace_bytes.restype = sz
             L.osd_distill_topk_workspace_bytes.argtypes = [i32, i32]
             L.osd_distill_topk_loss_grad.restype = i32
@@ -154,8 +152,8 @@ def _stream_handle(device):
     return _torch()._C._cuda_getCurrentRawStream(device.index)
 
 
-# Zero-initialised workspaces, one per (device, stream, kind): the kernels leave
-# them zeroed, so they are reused across calls on the same stream.  A captured graph
+# Zero-initialised workspaces, one per (device, stream, kind): the kernels leave zero
+# what has to be, so they are reused across calls on the same stream.  A captured graph
 # holds its workspace's address, so one that a larger call supersedes is kept (sizes
 # are powers of two: all of a stream's superseded ones together are smaller than the
 # one in use).  A graph replayed on another stream than the one it was captured on
@@ -550,8 +548,8 @@ def _on_device(dev, fn, *args):
 
 
 def _check_out(t, shape, dtype, name):
-    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous()):
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+    if t is not None and (t.shape != shape or t.dtype != dtype or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape}")
 
 
 def osd_topk(logits, k, temperature=1.0, u=None, rest=True, tokens=None, out=None):
@@ -581,16 +579,16 @@ def osd_topk(logits, k, temperature=1.0, u=None, rest=True, tokens=None, out=Non
                torch.empty(N, k, dtype=logits.dtype, device=dev),
                torch.empty(N, dtype=torch.float32, device=dev) if rest else None,
                torch.empty(N, dtype=torch.int32, device=dev) if tokens else None)
-    ids, top, rst, toks = out
-    _check_same_device(dev, *out)
-    _check_out(ids, (N, k), torch.int32, "ids")
-    _check_out(top, (N, k), logits.dtype, "top")
-    _check_out(rst, (N,), torch.float32, "rest")
-    _check_out(toks, (N,), torch.int32, "tokens")
-    L = lib()
-    ws = workspace("topk", L.osd_topk_workspace_bytes(N, k), dev)
-    st = _on_device(dev, L.osd_topk, _ptr(logits), logits.stride(0) if N > 1 else V, _dtype_code(logits), N, V, k,
-                    float(temperature), _ptr(u), _ptr(ids), _ptr(top), _ptr(rst), _ptr(toks), _ptr(ws), ws.numel(),
+        ids, top, rst, toks = out
+    else:
+        ids, top, rst, toks = out
+        _check_same_device(dev, *out)
+        _check_out(ids, (N, k), torch.int32, "ids")
+        _check_out(top, (N, k), logits.dtype, "top")
+        _check_out(rst, (N,), torch.float32, "rest")
+        _check_out(toks, (N,), torch.int32, "tokens")
+    st = _on_device(dev, lib().osd_topk, _ptr(logits), logits.stride(0) if N > 1 else V, _dtype_code(logits), N, V, k,
+                    float(temperature), _ptr(u), _ptr(ids), _ptr(top), _ptr(rst), _ptr(toks),
                     _stream_handle(dev))
     if st != OSD_OK:
         raise OsdError("osd_topk", st)
@@ -631,11 +629,13 @@ def osd_distill_topk_loss_grad(teacher_ids, teacher_top, teacher_rest, student_l
         out = (torch.empty(2, dtype=torch.float32, device=dev),
                torch.empty(B, K, dtype=torch.float32, device=dev) if row_loss else None,
                torch.empty(B, K, V, dtype=s.dtype, device=dev) if grad else None)
-    loss, rows, g = out
-    _check_same_device(dev, *out)
-    _check_out(loss, (2,), torch.float32, "loss")
-    _check_out(rows, (B, K), torch.float32, "row_loss")
-    _check_out(g, (B, K, V), s.dtype, "grad")
+        loss, rows, g = out
+    else:
+        loss, rows, g = out
+        _check_same_device(dev, *out)
+        _check_out(loss, (2,), torch.float32, "loss")
+        _check_out(rows, (B, K), torch.float32, "row_loss")
+        _check_out(g, (B, K, V), s.dtype, "grad")
     L = lib()
     ws = workspace("distill_topk", L.osd_distill_topk_workspace_bytes(B, K), dev)
     st = _on_device(dev, L.osd_distill_topk_loss_grad, _ptr(teacher_ids), _ptr(teacher_top), _ptr(teacher_rest), Kt, k,
@@ -677,11 +677,13 @@ def osd_verify_topk(target_logits, draft_ids, draft_top, draft_tokens, u_accept,
         out = (torch.empty(B, dtype=torch.int32, device=dev),
                torch.empty(B, K + 1, dtype=torch.int32, device=dev),
                torch.empty(B, K, dtype=torch.uint8, device=dev))
-    acc, toks, rmask = out
-    _check_same_device(dev, *out)
-    _check_out(acc, (B,), torch.int32, "accepted_len")
-    _check_out(toks, (B, K + 1), torch.int32, "out_tokens")
-    _check_out(rmask, (B, K), torch.uint8, "reject_mask")
+        acc, toks, rmask = out
+    else:
+        acc, toks, rmask = out
+        _check_same_device(dev, *out)
+        _check_out(acc, (B,), torch.int32, "accepted_len")
+        _check_out(toks, (B, K + 1), torch.int32, "out_tokens")
+        _check_out(rmask, (B, K), torch.uint8, "reject_mask")
     L = lib()
     ws = workspace("verify_topk", L.osd_verify_topk_workspace_bytes(B, K), dev)
     st = _on_device(dev, L.osd_verify_topk, _ptr(target_logits), _ptr(draft_ids), _ptr(draft_top), k,

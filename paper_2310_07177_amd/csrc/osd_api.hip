@@ -681,14 +681,8 @@ bool meets(const void* a, uint64_t na, const void* b, uint64_t nb) {
 
 extern "C" {
 
-size_t osd_topk_workspace_bytes(int N, int k) {
-    if (N <= 0 || k <= 0 || k > OSD_MAX_TOPK) return 0;
-    return osd::topk_layout(N, k).total;
-}
-
 int osd_topk(const void* logits, int64_t row_stride, int dtype, int N, int V, int k, float temperature,
-             const float* u, int32_t* ids_out, void* top_out, float* rest_out, int32_t* tokens_out,
-             void* workspace, size_t workspace_bytes, void* stream) {
+             const float* u, int32_t* ids_out, void* top_out, float* rest_out, int32_t* tokens_out, void* stream) {
     if (dtype != OSD_F32 && dtype != OSD_BF16) return OSD_ERR_INVALID_ARG;
     if (N <= 0 || V <= 0 || !record_ok(k, V)) return OSD_ERR_INVALID_ARG;
     if (V > osd_max_vocab(dtype)) return OSD_ERR_UNSUPPORTED;
@@ -696,9 +690,6 @@ int osd_topk(const void* logits, int64_t row_stride, int dtype, int N, int V, in
     if (!logits || row_stride < V || !ids_out || !top_out) return OSD_ERR_INVALID_ARG;
     if (temperature == 0.0f && rest_out) return OSD_ERR_INVALID_ARG;
     if (temperature > 0.0f && tokens_out && !u) return OSD_ERR_INVALID_ARG;
-    if (workspace ? workspace_bytes < osd_topk_workspace_bytes(N, k) || (reinterpret_cast<uintptr_t>(workspace) & 15u)
-                  : osd::topk_needs_workspace(V, per_chunk(dtype)))
-        return OSD_ERR_WORKSPACE;
     osd::TopkLaunch L;
     L.x = logits;
     L.stride = row_stride;
@@ -712,7 +703,6 @@ int osd_topk(const void* logits, int64_t row_stride, int dtype, int N, int V, in
     L.top = top_out;
     L.rest = rest_out;
     L.tokens = tokens_out;
-    L.workspace = workspace;
     L.stream = static_cast<hipStream_t>(stream);
     L.cus = device_cus(L.stream);
     return osd::launch_topk(L) == hipSuccess ? OSD_OK : OSD_ERR_DEVICE;

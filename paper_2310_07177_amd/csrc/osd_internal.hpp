@@ -235,33 +235,8 @@ struct TopkLaunch {
     float* rest;
     int32_t* tokens;
     int cus;
-    void* workspace;  // null, or topk_layout(N, k).total bytes
     hipStream_t stream;
 };
-// Split rows: up to kTopkSplitRows of them in a launch, an arrival counter each
-// (a cache line: see VerifyRow) at the start of the workspace, where no call's other
-// data ever lies; then what each segment posts.
-constexpr int kTopkSegments = 4;
-constexpr int64_t kTopkSplitRows = 4096;
-constexpr size_t kTopkCounterBytes = 64;
-struct TopkSegment {
-    double outside;      // mass of what the segment's list leaves out, relative to its largest logit
-    uint64_t count_max;  // length of the list, largest key
-};
-struct TopkWs {
-    size_t heads, lists, total;
-};
-inline TopkWs topk_layout(int N, int k) {
-    const size_t rows = size_t(N < kTopkSplitRows ? N : kTopkSplitRows) * kTopkSegments;
-    TopkWs w;
-    w.heads = size_t(kTopkSplitRows) * kTopkCounterBytes;
-    w.lists = w.heads + rows * sizeof(TopkSegment);
-    w.total = w.lists + rows * size_t(k) * 8;
-    return w;
-}
-// Rows longer than one workgroup holds are split.
-constexpr int kTopkRowChunks = 4096;
-inline bool topk_needs_workspace(int V, int per_chunk) { return V > kTopkRowChunks * per_chunk; }
 hipError_t launch_topk(const TopkLaunch& L);
 
 // Distillation from teacher records (distill_topk.hip).

@@ -12,11 +12,10 @@ NAN, INF = float("nan"), float("inf")
 
 
 def topk(**kw):
-    a = dict(x=FAKE, stride=64, dtype=1, N=4, V=64, k=8, T=1.0, u=FAKE, ids=FAKE, top=FAKE, rest=FAKE, toks=FAKE,
-             ws=None, wsb=0)
+    a = dict(x=FAKE, stride=64, dtype=1, N=4, V=64, k=8, T=1.0, u=FAKE, ids=FAKE, top=FAKE, rest=FAKE, toks=FAKE)
     a.update(kw)
     return osd.lib().osd_topk(a["x"], a["stride"], a["dtype"], a["N"], a["V"], a["k"], a["T"], a["u"], a["ids"],
-                              a["top"], a["rest"], a["toks"], a["ws"], a["wsb"], None)
+                              a["top"], a["rest"], a["toks"], None)
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -25,8 +24,6 @@ def topk(**kw):
     (dict(k=65), -1), (dict(k=257, V=1000, stride=1000), -1),
     (dict(T=-1.0), -1), (dict(T=NAN), -1), (dict(T=INF), -1), (dict(T=0.0), -1),  # rest at T == 0
     (dict(V=1 << 20, stride=1 << 20), -2), (dict(dtype=0, V=65537, stride=65537), -2),
-    (dict(ws=FAKE, wsb=8), -4), (dict(ws=ODD, wsb=1 << 30), -4),
-    (dict(V=32769, stride=32769), -4), (dict(dtype=0, V=16385, stride=16385), -4),  # split rows need one
 ])
 def test_topk_rejects_bad_arguments(kw, status):
     assert topk(**kw) == status
@@ -85,8 +82,6 @@ def test_workspace_sizes():
     for f in (L.osd_distill_topk_workspace_bytes, L.osd_verify_topk_workspace_bytes):
         assert f(0, 4) == 0 and f(4, 0) == 0 and f(-1, 1) == 0 and f(64, 8) > 0
     assert L.osd_verify_topk_workspace_bytes(4, 17) == 0
-    assert L.osd_topk_workspace_bytes(0, 4) == 0 and L.osd_topk_workspace_bytes(4, 0) == 0
-    assert L.osd_topk_workspace_bytes(4, 257) == 0 and L.osd_topk_workspace_bytes(4, 256) > 0
 
 
 def test_binding_refuses_cpu_tensors_shapes_and_types():

@@ -86,31 +86,17 @@ def test_kinds(osd, kind, V, k, dtype):
 
 
 @pytest.mark.parametrize("N", [1, 2, 40, 300, 1500])
-@pytest.mark.parametrize("dtype,V", [("bf16", 32003), ("f32", 9001)])
-def test_row_counts_without_a_workspace_and_with_one(osd, N, dtype, V):
-    """Few rows may be split over workgroups where a workspace is given."""
-    import ctypes
+@pytest.mark.parametrize("dtype,V", [("bf16", 32003), ("f32", 9001), ("bf16", 12001), ("bf16", 50257), ("f32", 40009)])
+def test_row_counts(osd, N, dtype, V):
+    """Few rows and many: each row's record is its own, whatever form is launched."""
     import torch
-    from paper_2310_07177_amd import binding
     k, T = 50, 1.0
     x, u = as_dtype(rows("normal", min(N, 40), V, N), dtype), uniforms(N, N)
     x = np.concatenate([x] * ((N + 39) // 40))[:N]
-    dx, du = to_device(x), to_device(u)
-    got = osd.osd_topk(dx, k, T, du)
+    got = osd.osd_topk(to_device(x), k, T, to_device(u))
     one = min(N, 40)
     check([t[:one].contiguous() for t in got], x[:one], k, T, u[:one], f"N={N}")
     assert all(torch.equal(t[r], t[r - 40]) for t in got[:3] for r in range(40, N, 97))
-    plain = [torch.empty_like(t) for t in got]
-    p = lambda t: ctypes.c_void_p(t.data_ptr())
-    st = osd.lib().osd_topk(p(dx), V, binding.OSD_BF16 if dtype == "bf16" else binding.OSD_F32, N, V, k, T, p(du),
-                            *(p(t) for t in plain), None, 0, None)
-    assert st == 0
-    torch.cuda.synchronize()
-    for a, b, name in zip(got, plain, ("ids", "top", "rest", "tokens")):
-        if name == "rest":
-            assert (a - b).abs().max().item() <= 2 * LOG_SUM
-        else:
-            assert torch.equal(a, b), name
 
 
 def test_strided_rows_offsets_and_given_outputs(osd):
@@ -155,11 +141,9 @@ def test_guard_bands(osd):
         sizes = [N * k * 4, N * k * es, N * 4, N * 4]
         bufs = [torch.full((n + 8192,), 0x5A, dtype=torch.uint8, device="cuda") for n in sizes]
         u = to_device(uniforms(N, 42))
-        ws = torch.zeros(osd.lib().osd_topk_workspace_bytes(N, k), dtype=torch.uint8, device="cuda")
         st = osd.lib().osd_topk(ctypes.c_void_p(x.data_ptr()), V, binding.OSD_BF16 if es == 2 else binding.OSD_F32, N,
                                 V, k, 1.0, ctypes.c_void_p(u.data_ptr()),
-                                *(ctypes.c_void_p(b.data_ptr() + 4096) for b in bufs),
-                                ctypes.c_void_p(ws.data_ptr()), ws.numel(), None)
+                                *(ctypes.c_void_p(b.data_ptr() + 4096) for b in bufs), None)
         assert st == 0
         torch.cuda.synchronize()
         for b, n in zip(bufs, sizes):
