@@ -195,9 +195,11 @@ __device__ __forceinline__ void over_row(const char* row, const RowCut<Fmt>& cut
     }
 }
 
-// (Of 512 threads three workgroups share a CU rather than two: 2048 rows of 128256
-// bf16 logits take 133 us, 3.9 TB/s, with 80 registers a lane and 152 us with 96.)
-template <typename Fmt, int W, int GROUPS, int G>
+// A tile holds rows of MINR to GROUPS * G rounds: only rounds from MINR on ask whether
+// the row has them or ends in them (asked in every round, 2048 rows of 128256 bf16 logits
+// took 141 us instead of 126, 4.2 TB/s).  Of 512 threads three workgroups share a CU
+// with 80 registers a lane, two with 96: these 2048 rows took 133 us and 152.
+template <typename Fmt, int W, int GROUPS, int G, int MINR>
 __global__ __launch_bounds__(W, W == 1024 ? 4 : W == 512 ? 6 : 5) void topk_row_kernel(TopkArgs a) {
     constexpr int EPC = Fmt::kPerChunk, NW = W / kWave, kRounds = GROUPS * G, kKeys = W / kWave;
     static_assert(W >= kBins && W >= OSD_MAX_TOPK && NW <= 16 && GROUPS <= 16, "");
@@ -227,20 +229,24 @@ __global__ __launch_bounds__(W, W == 1024 ? 4 : W == 512 ? 6 : 5) void topk_row_
         // (Kept in the caches, where the candidates' groups are read from again: 64
         // rows of 32003 fp32 logits take 8.6 us, and 9.8 us streamed past them.)
         const auto load = [&](int r) __attribute__((always_inline)) {
-            if (r >= rounds) return;
+            if (r >= MINR && r >= rounds) return;
             int off = (r * W + tid) * 16;
-            if (r == rounds - 1) off = min(off, cut.last_off);
-            c[r % kRing] = a.V < EPC ? load_short<Fmt>(row, a.V)
-                                     : __builtin_bit_cast(chunk_t, __builtin_amdgcn_raw_buffer_load_b128(
-                                                                       rs, off, 0, 0));
+            if (r >= MINR - 1) off = min(off, cut.last_off);
+            if constexpr (kRounds == 1) {
+                if (a.V < EPC) {
+                    c[0] = load_short<Fmt>(row, a.V);
+                    return;
+                }
+            }
+            c[r % kRing] = __builtin_bit_cast(chunk_t, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0));
         };
 #pragma unroll
         for (int r = 0; r < kRing; ++r) load(r);
         unrolled(std::make_integer_sequence<int, kRounds>{}, [&](auto step) __attribute__((always_inline)) {
             constexpr int r = decltype(step)::value;
-            if (r < rounds) {
+            if (r < MINR || r < rounds) {
                 chunk_t x = c[r % kRing];
-                if (r == rounds - 1) x = pad_lead<Fmt>(x, cut.lead(r * W + tid));
+                if (r >= MINR - 1 && r == rounds - 1) x = pad_lead<Fmt>(x, cut.lead(r * W + tid));
                 const float top = chunk_top<Fmt>(x);
                 gmax[r / G] = r % G ? max_nan(gmax[r / G], top) : top;
                 if (a.rest) {
@@ -474,12 +480,12 @@ __global__ __launch_bounds__(W, W == 1024 ? 4 : W == 512 ? 6 : 5) void topk_row_
     }
 }
 
-template <typename Fmt, int W, int GROUPS, int G>
+template <typename Fmt, int W, int GROUPS, int G, int MINR>
 hipError_t launch_tile(const TopkLaunch& L, TopkArgs a) {
     for (int64_t f = 0; f < L.N; f += kMaxGrid) {
         a.first = f;
         const unsigned g = unsigned(L.N - f < kMaxGrid ? L.N - f : kMaxGrid);
-        const hipError_t e = launch_kernel(&topk_row_kernel<Fmt, W, GROUPS, G>, dim3(g), dim3(W), 0, L.stream, a);
+        const hipError_t e = launch_kernel(&topk_row_kernel<Fmt, W, GROUPS, G, MINR>, dim3(g), dim3(W), 0, L.stream, a);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -488,21 +494,17 @@ hipError_t launch_tile(const TopkLaunch& L, TopkArgs a) {
 template <typename Fmt>
 hipError_t launch_fmt(const TopkLaunch& L, const TopkArgs& a) {
     const int chunks = (L.V + Fmt::kPerChunk - 1) / Fmt::kPerChunk;
-    if (chunks <= 256) return launch_tile<Fmt, 256, 1, 1>(L, a);
-    if (chunks <= 1024) return launch_tile<Fmt, 256, 4, 1>(L, a);
+    if (chunks <= 256) return launch_tile<Fmt, 256, 1, 1, 1>(L, a);
+    if (chunks <= 1024) return launch_tile<Fmt, 256, 4, 1, 2>(L, a);
     if (chunks > 16384) return hipErrorInvalidValue;
-    if (L.N <= L.cus) {
-        if (chunks <= 4096) return launch_tile<Fmt, 1024, 4, 1>(L, a);
-        return launch_tile<Fmt, 1024, 16, 1>(L, a);
-    }
-    if (L.N <= 3 * L.cus || chunks > 8192) {
-        if (chunks <= 4096) return launch_tile<Fmt, 512, 8, 1>(L, a);
-        if (chunks <= 8192) return launch_tile<Fmt, 512, 16, 1>(L, a);
-        return launch_tile<Fmt, 512, 16, 2>(L, a);
-    }
-    if (chunks <= 2048) return launch_tile<Fmt, 256, 8, 1>(L, a);
-    if (chunks <= 4096) return launch_tile<Fmt, 256, 16, 1>(L, a);
-    return launch_tile<Fmt, 256, 16, 2>(L, a);
+    // Threads a row (us, measured together, at 64, 256, 576 and 2048 rows).  32128 bf16 logits: 256 threads 12.0,
+    // 14.4, 18.3 and 40.8, 512 9.5, 11.3, 17.6 and 39.8, 1024 9.5, 10.8, 25.0 and 40.9;
+    // 64000: 256 20.6, 23.4, 29.0 and 75.5, 512 13.5, 16.3, 26.0 and 71.1, 1024 12.3, 15.2, 35.2
+    // and 75.7.
+    if (chunks <= 4096) return launch_tile<Fmt, 512, 8, 1, 3>(L, a);
+    if (L.N <= L.cus) return launch_tile<Fmt, 1024, 16, 1, 5>(L, a);
+    if (chunks <= 8192) return launch_tile<Fmt, 512, 16, 1, 9>(L, a);
+    return launch_tile<Fmt, 512, 16, 2, 17>(L, a);
 }
 
 }  // namespace
