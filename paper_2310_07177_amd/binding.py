@@ -152,13 +152,15 @@ def _stream_handle(device):
     return _torch()._C._cuda_getCurrentRawStream(device.index)
 
 
-# Zero-initialised workspaces, one per (device, stream, kind): the kernels leave zero
-# what has to be, so they are reused across calls on the same stream.  A captured graph
+# Zero-initialised workspaces, one per (device, stream, kind): the kernels leave
+# them zeroed, so they are reused across calls on the same stream.  A captured graph
 # holds its workspace's address, so one that a larger call supersedes is kept (sizes
 # are powers of two: all of a stream's superseded ones together are smaller than the
 # one in use).  A graph replayed on another stream than the one it was captured on
 # must not overlap calls on that one, nor other graphs captured on it.
 _workspaces = {}
+# Those that hold scratch as well, of which the kernels leave the counters zero.
+_scratch = {}
 _superseded = []
 # A workspace first needed during a capture is the graph's own: its zero fill is
 # recorded, not executed, so calls outside that capture cannot use it.
@@ -175,15 +177,16 @@ def _capture_id(stream):
     return capture.value if err == 0 and status.value == 1 else 0
 
 
-def workspace(kind, nbytes, device):
+def workspace(kind, nbytes, device, held=None):
+    held = _workspaces if held is None else held
     key = (device.index, _stream_handle(device), kind)
-    ws = _workspaces.get(key)
+    ws = held.get(key)
     if ws is None or ws.numel() < nbytes:
-        ws = _new_workspace(key, nbytes, device)
+        ws = _new_workspace(key, nbytes, device, held)
     return ws
 
 
-def _new_workspace(key, nbytes, device):
+def _new_workspace(key, nbytes, device, workspaces):
     torch = _torch()
     capture = _capture_id(key[1])
     if capture:
@@ -197,9 +200,9 @@ def _new_workspace(key, nbytes, device):
         return ws
     with _lock:
         _captured.pop(key, None)
-        if key in _workspaces:
-            _superseded.append(_workspaces[key])
-        _workspaces[key] = ws
+        if key in workspaces:
+            _superseded.append(workspaces[key])
+        workspaces[key] = ws
     return ws
 
 
@@ -637,7 +640,7 @@ def osd_distill_topk_loss_grad(teacher_ids, teacher_top, teacher_rest, student_l
         _check_out(rows, (B, K), torch.float32, "row_loss")
         _check_out(g, (B, K, V), s.dtype, "grad")
     L = lib()
-    ws = workspace("distill_topk", L.osd_distill_topk_workspace_bytes(B, K), dev)
+    ws = workspace("distill_topk", L.osd_distill_topk_workspace_bytes(B, K), dev, _scratch)
     st = _on_device(dev, L.osd_distill_topk_loss_grad, _ptr(teacher_ids), _ptr(teacher_top), _ptr(teacher_rest), Kt, k,
                     _ptr(s), s.stride(0) if B > 1 else K * V, _dtype_code(s), B, K, V, _ptr(mask), kind_code,
                     float(beta), float(tau), _ptr(loss), _ptr(rows), _ptr(g), _ptr(ws), ws.numel(),
@@ -685,7 +688,7 @@ def osd_verify_topk(target_logits, draft_ids, draft_top, draft_tokens, u_accept,
         _check_out(toks, (B, K + 1), torch.int32, "out_tokens")
         _check_out(rmask, (B, K), torch.uint8, "reject_mask")
     L = lib()
-    ws = workspace("verify_topk", L.osd_verify_topk_workspace_bytes(B, K), dev)
+    ws = workspace("verify_topk", L.osd_verify_topk_workspace_bytes(B, K), dev, _scratch)
     st = _on_device(dev, L.osd_verify_topk, _ptr(target_logits), _ptr(draft_ids), _ptr(draft_top), k,
                     _dtype_code(target_logits), B, K, V, _ptr(draft_tokens), _ptr(draft_len), _ptr(u_accept),
                     _ptr(u_resample), float(temperature), _ptr(acc), _ptr(toks), _ptr(rmask), _ptr(ws), ws.numel(),
