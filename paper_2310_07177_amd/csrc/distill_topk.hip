@@ -60,8 +60,9 @@ struct DistillTopkArgs {
 // (in every lane).  In: the record's student logits s_x and teacher logits s_t,
 // the row's largest logit, the others' largest and their mass relative to it
 // (0: none), the teacher's rest in log2 units (-inf: none).  Out: each token's
-// gradient in s_g, 2^-z f for the others' (z the student's log2 normaliser
-// relative to the row's largest logit, f their factor over tau) and D in nats.
+// gradient in s_g, the gradient at the others' largest logit (the others' go by it
+// and their exponentials relative to it: relative to the row's largest these may
+// all vanish in 32 bits while the factor P / Q overflows) and D in nats.
 struct RowTerms {
     double others;
     double D;
@@ -133,15 +134,16 @@ __device__ __forceinline__ RowTerms row_terms(const DistillTopkArgs& a, const fl
             g = q > 0.0 && (a.kind == OSD_RKL || wq > 0.0) ? q * factor(l) : 0.0;
         s_g[i] = float(bad ? nan : g);
     }
-    double f = 0.0;
+    double g = 0.0;
+    const double most = exp2_f64((double(all) - double(top)) * a.c2 - zx);  // q of the others' largest
     if (Q > 0.0) {
         if (a.kind == OSD_FKL)
-            f = (1.0 - P / Q) * a.inv_tau;
+            g = (most - P / sum) * a.inv_tau;
         else if (a.kind == OSD_RKL || wq > 0.0)
-            f = factor(o.l);
+            g = most * factor(o.l);
     }
     const double D = a.kind == OSD_JSD ? (wp > 0.0 ? wp * d0 : 0.0) + (wq > 0.0 ? wq * d1 : 0.0) : d0;
-    return RowTerms{bad ? nan : f * exp2_f64(-zx), bad ? nan : D * kLn2};
+    return RowTerms{bad ? nan : g, bad ? nan : D * kLn2};
 }
 
 // The chunk with the elements of bit mask f replaced by -inf.
@@ -171,7 +173,7 @@ __global__ __launch_bounds__((NR + 1) * kWave, 4) void distill_topk_kernel(Disti
     __shared__ uint32_t s_flag[(W * CPT + 3) / 4];  // a byte per chunk, a bit per element
     __shared__ float s_x[OSD_MAX_TOPK], s_t[OSD_MAX_TOPK], s_g[OSD_MAX_TOPK];
     __shared__ double s_p[OSD_MAX_TOPK], s_q[OSD_MAX_TOPK], s_s[NR], s_part;
-    __shared__ float s_m[NR], s_top, s_others;
+    __shared__ float s_m[NR], s_at, s_others;
     __shared__ LossTail s_tail;
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const int wid = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -253,7 +255,7 @@ __global__ __launch_bounds__((NR + 1) * kWave, 4) void distill_topk_kernel(Disti
             bad = __ballot(bad) != 0 || !is_finite(top) || sum != sum;
             const RowTerms r = row_terms(a, s_x, s_t, s_p, s_q, s_g, top, all, sum, double(rest) * 1.4426950408889634074, bad);
             if (lane == 0) {
-                s_top = top;
+                s_at = all > kNegInf ? all : 0.0f;
                 s_others = float(r.others);
                 s_part += r.D;
                 if (a.row_loss) a.row_loss[n] = float(r.D);
@@ -313,7 +315,7 @@ __global__ __launch_bounds__((NR + 1) * kWave, 4) void distill_topk_kernel(Disti
         __syncthreads();  // 2
         __syncthreads();  // 3
         if (!grow) continue;
-        const float at = s_top, scale = s_others;
+        const float at = s_at, scale = s_others;
         const rsrc_t rs = make_rsrc(grow, uint32_t(row_bytes));
         t = opaque_tid();
         held.each([&](int r) __attribute__((always_inline)) {
@@ -496,12 +498,12 @@ __global__ __launch_bounds__(kPartWaves* kWave, 4) void distill_topk_finish_kern
     }
     __syncthreads();
     if constexpr (GRAD) {
-        const float scale = s_others, c2 = float(a.c2);
+        const float at = all > kNegInf ? all : 0.0f, scale = s_others, c2 = float(a.c2);
 #pragma unroll
         for (int r = 0; r < CPT; ++r) {
             float v[EPC];
 #pragma unroll
-            for (int e = 0; e < EPC; ++e) v[e] = exp2_fast((Fmt::get(c[r], e) - top) * c2) * scale;
+            for (int e = 0; e < EPC; ++e) v[e] = exp2_fast((Fmt::get(c[r], e) - at) * c2) * scale;
             held.store(rs, r, pack_grad<Fmt>(v), tid);
             __builtin_amdgcn_sched_barrier(0);
         }

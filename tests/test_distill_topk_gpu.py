@@ -387,6 +387,27 @@ def test_graph(osd, V):
         assert all(torch.equal(a, b) for a, b in zip(out, eager))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["fkl", "rkl", "jsd"])
+@pytest.mark.parametrize("B,V", [(3, 3001), (3, 12007), (150, 12007)])
+def test_others_far_below_the_record(osd, B, V, kind, dtype):
+    """A student whose mass outside the record is far below what 32 bits hold:
+    the others still share the teacher's rest."""
+    k, tau = 33, 1.0
+    t = as_dtype(rows("normal", 3, V, 70), dtype)
+    ids, top, rest = record(t, k, tau)
+    for gap in (60.0, 88.0, 95.0, 200.0, 600.0):
+        s = rows("normal", 3, V, 71) - np.float32(gap)
+        for n in range(3):
+            s[n, ids[n]] += np.float32(gap)
+        s = as_dtype(s, dtype)
+        ti, tt, tr, ts = (np.concatenate([a] * (B // 3)) for a in (ids, top, rest, s))
+        loss, rl, g = call(osd, ti, tt, tr, ts, B, 1, kind, 0.5, tau)
+        loss = loss.clone()
+        loss[1] = loss[1] * 3 / B
+        check((loss, rl[:3], g[:3]), ids, top, rest, s, kind, 0.5, tau, None, f"gap {gap} {kind} {dtype}")
+
+
 def test_lowest_of_the_type(osd):
     """A teacher and a student that are the type's lowest value everywhere are
     uniform: D = 0."""
