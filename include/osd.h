@@ -27,11 +27,13 @@
  *     and enqueue nothing.  A failed launch returns OSD_ERR_DEVICE.
  *   - Workspaces: the caller allocates `*_workspace_bytes(...)` bytes of
  *     device memory and fills them with zeros ONCE before first use; every
- *     call leaves its workspace zeroed again when its kernels finish.  Calls
- *     that may run concurrently need distinct workspaces.  (A workspace that
- *     is not zero -- fresh from an uninitialised allocation, or shared by
- *     calls in flight on two streams -- is not detected: the outputs are then
- *     wrong, with no status to say so.)
+ *     call leaves its workspace zeroed again when its kernels finish (those of
+ *     osd_distill_topk_loss_grad and osd_verify_topk keep scratch beside
+ *     counters, and each serves its operator alone).  Calls that may run
+ *     concurrently need distinct workspaces.  (A workspace that is not zero --
+ *     fresh from an uninitialised allocation, or shared by calls in flight on
+ *     two streams -- is not detected: the outputs are then wrong, with no
+ *     status to say so.)
  *   - Thread-safe: apart from osd_verify_noalloc's per-GPU scratch array
  *     (see there), the library holds no mutable global state.
  */
@@ -422,8 +424,8 @@ int osd_topk(const void* logits, int64_t row_stride, int dtype, int N, int V, in
  *               gaps); any other overlap with them is refused.  Outputs must not
  *               overlap the other inputs
  * workspace     osd_distill_topk_workspace_bytes(B, K) zero-initialised bytes
- *               (counters among them are left zero; the rest keeps scratch that
- *               later calls need not find cleared, at any B, K, V, k)
+ *               for this operator alone (counters among them are left zero; the
+ *               rest keeps scratch that later calls need not find cleared, at any B, K, V, k)
  *
  * A row whose record is empty, names a token outside [0, V) (-1: an empty slot)
  * or one token twice, or holds a NaN or +inf, and a student row with a NaN, +inf or
@@ -454,8 +456,8 @@ int osd_distill_topk_loss_grad(const int32_t* teacher_ids, const void* teacher_t
  * temperature   T > 0 (at T == 0 the draft's probabilities play no part: use
  *               osd_verify)
  * workspace     osd_verify_topk_workspace_bytes(B, K) zero-initialised bytes
- *               (counters among them are left zero; the rest keeps scratch that
- *               later calls need not find cleared, at any B, K, V)
+ *               for this operator alone (counters among them are left zero; the
+ *               rest keeps scratch that later calls need not find cleared, at any B, K, V)
  * the others    as osd_verify
  *
  * accepted_len is -1 as in osd_verify, and where the record of a position that

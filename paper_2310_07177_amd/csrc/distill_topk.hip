@@ -570,7 +570,8 @@ hipError_t launch_fmt(const DistillTopkLaunch& L, const DistillTopkArgs& a) {
     // 10.1 and 9.4, but of 4000 9.0 and 8.4 against 9.7 and 8.5; 128 rows of 32128
     // 15.9 and 13.2 against 14.6 and 12.1, 256 of them 18.3 and 15.4 against 19.3 and 17.3;
     // 512 of 128256, where a CU holds one row, 75.5 and 54.5 against 78.4 and 42.1.
-    if (chunks > 1024 && (2 * a.N <= L.cus || (!a.grad && chunks > 7 * 10 * kWave && a.N <= kDistillTopkSplitRows)))
+    if (chunks > 1024 && a.N <= kDistillTopkSplitRows &&
+        (2 * a.N <= L.cus || (!a.grad && chunks > 7 * 10 * kWave)))
         return launch_split<Fmt>(L, a, chunks);
     const int waves = (chunks + kWave - 1) / kWave;  // of one chunk a lane
     if (waves <= 3 * 2) return launch_tile<Fmt, 3, 2, 1>(L, a);
