@@ -35,7 +35,9 @@
  *     two streams -- is not detected: the outputs are then wrong, with no
  *     status to say so.)
  *   - Thread-safe: apart from osd_verify_noalloc's per-GPU scratch array
- *     (see there), the library holds no mutable global state.
+ *     (see there), the library holds no mutable global state.  A call that is
+ *     several launches holds a lock while it enqueues them, so threads may
+ *     share a workspace as long as they share the stream too.
  */
 #ifndef OSD_H
 #define OSD_H

@@ -531,6 +531,7 @@ hipError_t launch_segments(const DistillTopkLaunch& L, DistillTopkArgs a, int ch
     if (groups > kDistillTopkParts + int64_t(a.N) * kDistillTopkLongest) return hipErrorInvalidValue;
     a.tail.G = a.N;
     const dim3 all(static_cast<uint32_t>(groups)), each(static_cast<uint32_t>(a.N));
+    const LaunchesTogether together;  // the second reads parts and split_x
     const hipError_t st = launch_kernel(&distill_topk_part_kernel<Fmt, CPT>, all, dim3(W), 0, L.stream, a);
     if (st != hipSuccess) return st;
     return a.grad ? launch_kernel(&distill_topk_finish_kernel<Fmt, CPT, true>, all, dim3(W), 0, L.stream, a)

@@ -3,6 +3,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <pthread.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -24,6 +25,17 @@ inline hipError_t launch_kernel(void (*kernel)(P...), dim3 grid, dim3 block, siz
     void* ptrs[] = {static_cast<void*>(&args)..., nullptr};
     return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, ptrs, lds, stream);
 }
+
+// Held while a call enqueues launches of which a later one reads what an earlier one
+// left in the workspace: another thread's call on the same stream and workspace cannot
+// enqueue its own between them.  (A plain mutex: locking it throws nothing.)
+inline pthread_mutex_t g_launches = PTHREAD_MUTEX_INITIALIZER;
+struct LaunchesTogether {
+    LaunchesTogether() { pthread_mutex_lock(&g_launches); }
+    ~LaunchesTogether() { pthread_mutex_unlock(&g_launches); }
+    LaunchesTogether(const LaunchesTogether&) = delete;
+    LaunchesTogether& operator=(const LaunchesTogether&) = delete;
+};
 
 // Kernel tile shape chosen from V: W threads per workgroup, CPT 16-byte chunks
 // per thread per row.
