@@ -292,6 +292,7 @@ int verify_distill_impl(const void* target_logits, const void* draft_logits, int
         const DistillWs dw = distill_layout(B, K);
         uint8_t* rmask = reject_mask;
         if (erridx && !rmask) rmask = reinterpret_cast<uint8_t*>(w + ws.mask);
+        const osd::LaunchesTogether together;  // the second reads the first's mask
         int st = osd_verify(target_logits, draft_logits, dtype, B, K, V, draft_tokens, draft_len, u_accept,
                             u_resample, temperature, accepted_len, out_tokens, rmask, w + ws.verify, vw.total,
                             stream);

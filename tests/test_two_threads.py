@@ -80,7 +80,8 @@ print("launches", *order)
 """
 
 
-@pytest.mark.parametrize("call,each", [("distill_topk", 2), ("distill_topk_grad", 2)])
+@pytest.mark.parametrize("call,each", [("distill_topk", 2), ("distill_topk_grad", 2),
+                                       ("verify_distill_rejected", 3)])
 def test_launches_of_a_call_stay_together(call, each, tmp_path):
     stub = str(tmp_path / "stub.so")
     (tmp_path / "stub.cpp").write_text(STUB)
