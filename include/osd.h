@@ -408,8 +408,9 @@ int osd_topk(const void* logits, int64_t row_stride, int dtype, int N, int V, in
  *   RKL  KL(q || p)                     q_j (log(q_b / p_b) - D) / tau
  *   JSD  beta KL(p || m) + (1 - beta) KL(q || m),  m = beta p + (1 - beta) q
  *                                       (1 - beta) q_j (log(q_b / m_b) - KL(q || m)) / tau
- * (0 log 0 = 0; a token with q_j = 0 outside the record has gradient 0).  With a record that
- * holds the whole row this is osd_distill_loss_grad.
+ * (0 log 0 = 0; a token with logit -inf outside the record has gradient 0; q_j / Q is taken of the
+ * logits, so FKL's gradient holds however far the others lie below the record).  With a record
+ * that holds the whole row this is osd_distill_loss_grad.
  *
  * teacher_ids   [.., k] int32, teacher_top [.., k] dtype, teacher_rest [..]
  *               fp32: records as osd_topk writes them (rest at T = tau).  The

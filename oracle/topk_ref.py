@@ -120,7 +120,10 @@ def distill(ids, top, rest, student, kind, beta, tau, mask=None):
             qj = np.exp(lq)
             g = np.where(qj > 0, qj * f[-1], 0.0)
             g[at] = np.where(q[:-1] > 0, q[:-1] * f[:-1], 0.0)
-            if kind == "fkl":
+            if kind == "fkl":  # q - p in the record; outside q_j - P q_j / Q, where q_j and Q may have no value
+                share = np.exp(lq - big) if big > -INF else np.zeros(V)
+                share[at] = 0.0
+                g = qj - p[-1] * share / max(share.sum(), 1.0)
                 g[at] = q[:-1] - p[:-1]
             grad[n] = g / tau
     total = float(rows[on].sum()) if on.any() else 0.0

@@ -136,12 +136,11 @@ __device__ __forceinline__ RowTerms row_terms(const DistillTopkArgs& a, const fl
     }
     double g = 0.0;
     const double most = exp2_f64((double(all) - double(top)) * a.c2 - zx);  // q of the others' largest
-    if (Q > 0.0) {
-        if (a.kind == OSD_FKL)
-            g = (most - P / sum) * a.inv_tau;
-        else if (a.kind == OSD_RKL || wq > 0.0)
-            g = most * factor(o.l);
-    }
+    // (FKL: q_j - P q_j / Q, of which the second part stays where q_j and Q vanish.)
+    if (a.kind == OSD_FKL)
+        g = sum > 0.0 ? (most - P / sum) * a.inv_tau : 0.0;
+    else if (Q > 0.0 && (a.kind == OSD_RKL || wq > 0.0))
+        g = most * factor(o.l);
     const double D = a.kind == OSD_JSD ? (wp > 0.0 ? wp * d0 : 0.0) + (wq > 0.0 ? wq * d1 : 0.0) : d0;
     return RowTerms{bad ? nan : g, bad ? nan : D * kLn2};
 }

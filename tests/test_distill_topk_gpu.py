@@ -419,3 +419,71 @@ def test_lowest_of_the_type(osd):
         loss, rl, g = osd.osd_distill_topk_loss_grad(ids.view(2, 1, k), top.view(2, 1, k), rest.view(2, 1),
                                                      to_device(x.reshape(2, 1, V)), "fkl")
         assert np.abs(host(rl)).max() < 4 * LOG_SUM
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["fkl", "rkl", "jsd"])
+@pytest.mark.parametrize("B,V", [(3, 3001), (3, 12007), (150, 12007)])
+def test_others_below_64_bits(osd, B, V, kind, dtype):
+    """The same where the others' mass leaves fp64's range too (a student masked
+    with -1e4): the loss is finite, and the gradient that loss's own: a row's
+    gradients add up to 0, those outside the record in FKL to Q - P, Q = 0.
+
+    Sums: each gradient is off by half a step of the type and 2^-15 of itself, and
+    all by 40 LOG_SUM q (see above), which adds up to these of the sum of their
+    magnitudes and 40 LOG_SUM."""
+    k, tau = 33, 1.0
+    t = as_dtype(rows("normal", 3, V, 80), dtype)
+    ids, top, rest = record(t, k, tau)
+    step = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    for gap in (700.0, 740.0, 760.0, 900.0, 1.0e4):
+        s = rows("normal", 3, V, 81) - np.float32(gap)
+        for n in range(3):
+            s[n, ids[n]] += np.float32(gap)
+        s = as_dtype(s, dtype)
+        ti, tt, tr, ts = (np.concatenate([a] * (B // 3)) for a in (ids, top, rest, s))
+        loss, rl, g = call(osd, ti, tt, tr, ts, B, 1, kind, 0.5, tau)
+        loss = loss.clone()
+        loss[1] = loss[1] * 3 / B
+        check((loss, rl[:3], g[:3]), ids, top, rest, s, kind, 0.5, tau, None, f"gap {gap} {kind} {dtype}")
+        assert np.isfinite(host(rl)).all()
+        g = topk_ref.values(host(g[:3]).reshape(3, V))
+        for n in range(3):
+            lim = (step + 2.0 ** -15) * 1.01 * np.abs(g[n]).sum() + 40 * LOG_SUM
+            assert abs(g[n].sum()) <= lim, f"gap {gap} {kind} {dtype}: {g[n].sum()}"
+            if kind == "fkl":
+                e = np.exp(topk_ref.values(t[n]) - topk_ref.values(t[n]).max())
+                P = np.delete(e, ids[n]).sum() / e.sum()
+                assert abs(np.delete(g[n], ids[n]).sum() + P) <= lim, f"gap {gap} {dtype}"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["fkl", "rkl", "jsd"])
+@pytest.mark.parametrize("V", [3001, 12007])
+@pytest.mark.parametrize("fill", ["lowest", -1.0e4, -1.0e30])
+def test_gradient_of_a_student_with_finite_fills(osd, fill, V, kind, dtype):
+    """Masked tokens at a large negative number, in the record and outside it: the
+    gradient as the reference has it.  (FKL's loss is up to the type's largest; the
+    batch's sum of it may leave fp32.)"""
+    B, k, tau = 4, 33, 1.0
+    t = as_dtype(rows("normal", B, V, 6), dtype)
+    ids, top, rest = record(t, k, tau)
+    s = rows("normal", B, V, 7)
+    g = np.random.default_rng(8)
+    fill = lowest(dtype) if fill == "lowest" else np.float32(fill)
+    s[0, g.random(V) < 0.9] = fill
+    s[1] = fill
+    s[1, ids[1]] = rows("normal", 1, k, 9)[0]          # all outside
+    s[2, ids[2, : k // 2]] = fill                      # half the record
+    s[3, g.random(V) < 0.5] = fill
+    s[3, ids[3]] = rows("normal", 1, k, 10)[0]
+    s = as_dtype(s, dtype)
+    loss, rl, gr = call(osd, ids, top, rest, s, B, 1, kind, 0.5, tau)
+    _, wr, wg = topk_ref.distill(ids, top, rest, s, kind, 0.5, tau)
+    assert np.allclose(host(rl).reshape(-1), wr, rtol=1e-5, atol=4 * LOG_SUM)
+    gr = topk_ref.values(host(gr).reshape(B, V))
+    step = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    tiny = 2.0 ** -133 if dtype == "bf16" else 2.0 ** -149
+    err, lim = np.abs(gr - wg), (step + 2.0 ** -15) * np.abs(wg) + 40 * LOG_SUM * qof(s, tau) + tiny
+    bad = ~(err <= lim)
+    assert not bad.any(), f"{bad.sum()}: {gr[bad][:3]} for {wg[bad][:3]}"

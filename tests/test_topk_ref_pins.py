@@ -180,3 +180,36 @@ def test_verify_invalid_sequences():
     top[:, 0, 0] = 60.0
     acc = topk_ref.verify(t, ids, top, y, ua, ur, 1.0, dl)[0]
     assert acc[1] == 0 and acc[6] == 0
+
+
+@pytest.mark.parametrize("gap", [0.0, 600.0, 740.0, 800.0, 1.0e4])
+@pytest.mark.parametrize("kind", ["fkl", "rkl", "jsd"])
+def test_gradient_of_others_far_below_is_autograd(kind, gap):
+    """Against torch's derivative of the definition in logarithms, in fp64, where
+    the others' mass has left its range."""
+    import torch
+    V, k, tau, beta = 40, 6, 1.3, 0.4
+    t = rows("normal", 1, V, 30)
+    rec = topk_ref.topk(t, k, tau)
+    ids = rec["ids"][0].astype(np.int64)
+    top = np.take_along_axis(t, rec["ids"].astype(np.int64), 1)
+    s = rows("normal", 1, V, 31).astype(np.float64) - gap
+    s[0, ids] += gap
+    x = torch.tensor(s[0], requires_grad=True)
+    lq = torch.log_softmax(x / tau, 0)
+    out = np.setdiff1d(np.arange(V), ids)
+    lb = torch.cat([lq[ids], torch.logsumexp(lq[out], 0).view(1)])
+    lt = np.append((rec["top"][0] - rec["top"][0, 0]) / tau, np.float32(rec["rest"][0]))
+    lp = torch.log_softmax(torch.tensor(lt), 0)
+    if kind == "fkl":
+        D = (lp.exp() * (lp - lb)).sum()
+    elif kind == "rkl":
+        D = (lb.exp() * (lb - lp)).sum()
+    else:
+        lm = torch.logaddexp(lp + np.log(beta), lb + np.log(1 - beta))
+        D = beta * (lp.exp() * (lp - lm)).sum() + (1 - beta) * (lb.exp() * (lb - lm)).sum()
+    D.backward()
+    _, rl, g = topk_ref.distill(rec["ids"], top, rec["rest"].astype(np.float32), s, kind, beta, tau)
+    assert abs(rl[0] - D.item()) < 1e-12 * max(1.0, D.item())
+    assert np.abs(g[0] - x.grad.numpy()).max() < 1e-12
+    assert abs(g.sum()) < 1e-12
