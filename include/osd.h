@@ -467,9 +467,10 @@ int osd_distill_topk_loss_grad(const int32_t* teacher_ids, const void* teacher_t
  * is tested is empty, names a token outside [0, V) (-1: an empty slot) or one
  * token twice, or holds a NaN or +inf.
  *
- * Tests agree with an exact computation except where u lies within about 1e-8
+ * Tests agree with an exact computation except where u lies within about 1e-11
  * (relative) of p(y)/q(y), draws except within about 1e-11 of probability mass of
- * an edge: a draw whose point lies near an edge is decided in fp64.
+ * an edge: where u lies near the ratio, and a draw's point near an edge, they are
+ * decided in fp64.
  */
 size_t osd_verify_topk_workspace_bytes(int B, int K);
 int osd_verify_topk(const void* target_logits, const int32_t* draft_ids, const void* draft_top, int k, int dtype,

@@ -23,7 +23,10 @@
 // (the errors are of either sign) 5e-9 on average and 2.5e-8 at most over
 // simulated rows of 8000 to 128000 logits.  A draw whose point lies within
 // kUnsure of an edge of its token's interval is decided again on fp64 exponentials
-// of the whole row (1e-12); that is one draw in some hundred.  fp64 exponentials
+// of the whole row (1e-12); that is one draw in some hundred.  A test is decided again
+// so where u q / p and 1 differ by less than kNearRatio: the normaliser is off by
+// (2 n ln 2 + 2 + 3) 2^-24 in terms 2^-n of the largest, by less than 2.5e-6 where these
+// carry its mass (n <= 24).  fp64 exponentials
 // throughout took three times as long for the cells (B = 64, K = 8, V = 32128
 // bf16: 20.6 us for them alone).
 #include "osd.h"
@@ -40,6 +43,7 @@ constexpr int kSlots = OSD_MAX_TOPK / kWave;
 constexpr int kSlotPad = 8;       // (the row's last chunk reads up to 7 elements before its own)
 constexpr int kTable = 1024;      // places for the ids of a record (at most 256)
 constexpr double kUnsure = 6.0e-8;
+constexpr double kNearRatio = 2.5e-6;
 // Workgroups per launch (a grid stays below 2^32 work-items).
 constexpr int64_t kMaxGrid = int64_t(1) << 22;
 
@@ -139,7 +143,9 @@ struct VerifyTopkLds {
     };
     double row_sum[OSD_MAX_K + 1];             // target rows: normaliser
     float row_top[OSD_MAX_K + 1];              //              largest logit, NaN or -inf if unusable
-    int verdict[OSD_MAX_K + 1];                // 0 accepted, 1 stop here, 2 invalid
+    int verdict[OSD_MAX_K + 1];                // 0 accepted, 1 stop here, 2 invalid, 3 too near to tell
+    double row_t[OSD_MAX_K + 1];               // for the last: the target's exponential times q_sum,
+    double row_uq[OSD_MAX_K + 1];              //               u times the draft's
     int id[OSD_MAX_TOPK];                      // the record at the first rejection: token (-1: none),
     double q[OSD_MAX_TOPK];                    // q, and
     double e[OSD_MAX_TOPK];                    // the target's exponential
@@ -381,6 +387,26 @@ __device__ __forceinline__ int find_token(const VerifyTopkArgs& a, const Draw& d
     }
 }
 
+// The sums of a row's cells from fp64 exponentials, by the whole workgroup (0 past the
+// last cell; barriers inside and at the end).
+template <typename Fmt, int kPer>
+__device__ __forceinline__ void exact_cells(const VerifyTopkArgs& a, const char* row, VerifyTopkLds& s) {
+    const int tid = threadIdx.x;
+    const RowCut<Fmt> cut(a.V);
+    if (tid < kMaxCells) s.sum[tid] = 0.0;
+    __syncthreads();
+#pragma unroll 1
+    for (int c = tid / kWave; c < a.cells; c += kNW) {
+        chunk_t x[kPer];
+        float top;
+        double sum;
+        load_cell<Fmt, kPer>(x, row, c, cut, a.V);
+        cell_sum<Fmt, kPer, true>(x, c, cut, a.c2, top, sum);
+        if ((tid & (kWave - 1)) == 0) s.sum[c] = sum;
+    }
+    __syncthreads();
+}
+
 // The last workgroup of a sequence: the tests, the first rejection, the draw.
 template <typename Fmt, int kPer>
 __device__ __forceinline__ void decide(const VerifyTopkArgs& a, int64_t b, int kb, VerifyTopkLds& s) {
@@ -420,7 +446,12 @@ __device__ __forceinline__ void decide(const VerifyTopkArgs& a, int64_t b, int k
                 verdict = 2;
             else if (i < kb) {  // u q / q_sum < p / sum
                 const double p = t[j] > kNegInf ? exp2_f64((double(t[j]) - double(top)) * a.c2) : 0.0;
-                verdict = double(u[j]) * qt[j] * sum < p * qs[j] ? 0 : 1;
+                const double uq = double(u[j]) * qt[j], pq = p * qs[j];
+                verdict = __builtin_fabs(uq * sum - pq) < kNearRatio * pq ? 3 : uq * sum < pq ? 0 : 1;
+                if (verdict == 3 && cell == 0) {
+                    s.row_t[i] = pq;
+                    s.row_uq[i] = uq;
+                }
             }
             // (A proposal outside the vocabulary, wherever it is, is caught below.)
             if (cell == 0 && i <= kb) {
@@ -433,8 +464,21 @@ __device__ __forceinline__ void decide(const VerifyTopkArgs& a, int64_t b, int k
     if (tid < kMaxCells) s.fixed[tid] = 0;
     for (int i = tid; i < (kSlotPad + kTokens + 8) / 2; i += kW) reinterpret_cast<uint32_t*>(s.slot)[i] = 0u;
     __syncthreads();
-    const int v = lane <= kb ? s.verdict[lane] : 1;
-    const int acc = __builtin_ctzll(__ballot(v != 0));
+    // The first position that is not accepted.  Where the sums of v_exp_f32 do not tell,
+    // on fp64 exponentials of its row.
+    int v, acc;
+#pragma unroll 1
+    while (true) {
+        v = lane <= kb ? s.verdict[lane] : 1;
+        acc = __builtin_ctzll(__ballot(v != 0));
+        if (__builtin_amdgcn_readlane(v, acc) != 3) break;
+        exact_cells<Fmt, kPer>(a, a.target + (b * (K + 1) + acc) * a.V * Fmt::kBytes, s);
+        const float m = cell < a.cells ? posted(&rows[acc].top[cell]) : kNegInf;
+        const double sum = half_sum(s.sum[cell] * exp2_f64((double(m) - double(s.row_top[acc])) * a.c2));
+        __syncthreads();
+        if (tid == 0) s.verdict[acc] = s.row_uq[acc] * sum < s.row_t[acc] ? 0 : 1;
+        __syncthreads();
+    }
     bool invalid = __ballot(token < 0 || token >= a.V) != 0 || __builtin_amdgcn_readlane(v, acc) == 2;
     int extra = -1;
     if (!invalid) {
@@ -482,22 +526,8 @@ __device__ __forceinline__ void decide(const VerifyTopkArgs& a, int64_t b, int k
         extra = find_token<Fmt, kPer, false>(a, d, s, sure);
         if (!sure) {  // again with fp64 exponentials
             __syncthreads();
-            if (tid < kMaxCells) {
-                s.fixed[tid] = 0;
-                s.sum[tid] = 0.0;
-            }
-            __syncthreads();
-            const RowCut<Fmt> cut(a.V);
-#pragma unroll 1
-            for (int c = wid; c < a.cells; c += kNW) {
-                chunk_t x[kPer];
-                float top;
-                double sum;
-                load_cell<Fmt, kPer>(x, d.row, c, cut, a.V);
-                cell_sum<Fmt, kPer, true>(x, c, cut, a.c2, top, sum);
-                if (lane == 0) s.sum[c] = sum;
-            }
-            __syncthreads();
+            if (tid < kMaxCells) s.fixed[tid] = 0;
+            exact_cells<Fmt, kPer>(a, d.row, s);
             S = s.sum[cell];
             d.sum = half_sum(S * weight);
             d.inv = 1.0 / d.sum;

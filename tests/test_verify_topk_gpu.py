@@ -247,3 +247,46 @@ def test_speculative_step_on_records(osd, dtype):
     from tests.test_distill_topk_gpu import record
     fi, ft, fr = record(t[:, :K].reshape(B * K, V), k, T)
     check_distill((loss, rl, g), fi, ft, fr, d.reshape(B * K, V), "fkl", 0.5, T, host(rmask), "step")
+
+
+def flat_rows(V, gap, dtype, seed, kind):
+    """[8, V] rows whose terms round alike: one head token far above equal others
+    (first, last or in the middle), in one stretch of the row or all over it; or
+    eight logits over and over, other ones in the second half."""
+    g = np.random.default_rng(seed)
+    x = np.full((8, V), -gap, np.float32)
+    for n in range(8):
+        if kind == "pattern":
+            half = V // 2 // 8 * 8
+            for lo, hi in ((0, half), (half, V)):
+                x[n, lo:hi] = np.resize(-gap * g.random(8), hi - lo)
+        elif kind == "stretch":  # one stretch of at most 2048 tokens
+            x[n] = -np.inf
+            lo = int(g.integers(0, max(1, V // 2048))) * 2048
+            x[n, lo:lo + 2047] = -gap
+        if kind != "pattern":
+            x[n, [0, V - 1, int(g.integers(V))][n % 3]] = 0.0
+    return as_dtype(x, dtype)
+
+
+FLAT = [(2048, 6.84375), (1024, 6.4375), (2047, 7.625), (4099, 8.3125), (32003, 10.375), (65536, 11.0625)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1.0, 0.875, 0.75, 0.6])
+@pytest.mark.parametrize("V,gap", FLAT)
+def test_acceptance_next_to_the_ratio(osd, V, gap, T, dtype):
+    """Uniforms next to p(y) / q(y), the head proposed from a record of its own."""
+    T = float(np.float32(T))
+    t = flat_rows(V, gap if dtype == "bf16" else np.float32(gap * 1.0437), dtype, V, "head")
+    n = 64
+    which = np.arange(n) % 8
+    p = np.array([topk_ref.softmax(r / T).max() for r in topk_ref.values(t)])
+    y = np.array([int(np.argmax(r)) for r in topk_ref.values(t)], np.int32)[which]
+    ua = p[which].astype(np.float32)
+    for b in range(n):
+        for _ in range(b // 8):
+            ua[b] = np.nextafter(ua[b], np.float32(0 if b % 2 else 1), dtype=np.float32)
+    x = dict(t=np.stack([t[which], t[which]], 1), ids=y.reshape(n, 1, 1), top=np.zeros((n, 1, 1), t.dtype),
+             y=y.reshape(n, 1), ua=ua.reshape(n, 1), ur=uniforms(n, 5))
+    check(call(osd, x, T), x, T, None, f"V={V} T={T} {dtype}")
