@@ -294,8 +294,9 @@ hipError_t launch_distill_topk(const DistillTopkLaunch& L);
 // another's.
 constexpr int kMaxCells = 32;
 struct VerifyTopkRow {
-    double sum[kMaxCells];     // by cell: exponentials relative to
-    float top[kMaxCells];      //          the largest logit
+    double sum[kMaxCells];     // by cell: sum of exponentials,
+    float top[kMaxCells];      //          the largest logit,
+    float mean[kMaxCells];     //          their mean over that mass (bf16 rows)
     float slot[OSD_MAX_TOPK];  // the row's logits at its record's tokens
     double q_sum;              // the record's softmax: normaliser (0: no record)
     double q_token;            // the proposal's exponential
@@ -304,7 +305,7 @@ struct VerifyTopkRow {
     uint32_t arrivals;         // (row 0) workgroups of the sequence
     uint32_t pad[25];
 };
-static_assert(sizeof(VerifyTopkRow) == 1536, "whole cache lines");
+static_assert(sizeof(VerifyTopkRow) == 1664, "whole cache lines");
 struct VerifyTopkLaunch {
     const void* target;
     const int32_t* ids;

@@ -16,19 +16,25 @@
 // tokens).  They post what they found in the workspace, and the last of a sequence
 // to arrive decides and draws.
 //
-// Precision: the cells' sums take v_exp_f32 and are summed in fp64 from eight
-// terms up.  With relative errors d_j of the terms the running mass C at a token is
-// off by (1 - C) sum p_j d_j over the tokens before it less C times the same over
-// those after: at most half the largest error of terms that carry mass, 6e-8, and
-// (the errors are of either sign) 5e-9 on average and 2.5e-8 at most over
-// simulated rows of 8000 to 128000 logits.  A draw whose point lies within
-// kUnsure of an edge of its token's interval is decided again on fp64 exponentials
-// of the whole row (1e-12); that is one draw in some hundred.  A test is decided again
-// so where u q / p and 1 differ by less than kNearRatio: the normaliser is off by
-// (2 n ln 2 + 2 + 3) 2^-24 in terms 2^-n of the largest, by less than 2.5e-6 where these
-// carry its mass (n <= 24).  fp64 exponentials
-// throughout took three times as long for the cells (B = 64, K = 8, V = 32128
-// bf16: 20.6 us for them alone).
+// Precision: a cell's sum takes v_exp_f32 and is summed in fp64 from pairs up.
+// A term is then off by at most kTerm = 1.8e-7 of itself: 8.5e-8 by the instruction (the
+// most over every argument from -126 to 127), 6e-8 by the sum of a pair, 3.4e-8 by its
+// argument.  (The rounding of (x - m) c2 alone would be 2 n ln 2 2^-24 of a term 2^-n,
+// the same in equal terms: 1e-6 at n = 12.  bf16 logits have exact products with 16
+// bits of c2, see cell_sum; the others take reduced arguments, see Near.)  With errors
+// d_j of the terms the normaliser is off by D = sum p_j d_j, and the mass R_t up to a token
+// that is left of p, less the point u R, by
+//   E = (1 - u) sum_{j <= t} p_j e_j - u sum_{j > t} p_j e_j,
+// e_j = d_j - D where the token keeps mass and d_j where the record takes all of it (its
+// exact exponential is subtracted).  With A the mass of p up to the token, collecting d_j,
+//   |E| <= kTerm (A (1 - u) + (1 - A) u + A (1 - A)).
+// A draw whose point lies within that of an edge of its token's interval is decided again
+// on fp64 exponentials of the whole row (1e-12), and so is a test where u q / p and 1
+// differ by less than kNearRatio (the normaliser is off by kTerm).  That holds up its
+// sequence by 25 + 6 us at V = 128256, where it is one draw in fifty (B = 256, K = 8, bf16:
+// 120 us a call, 95 if none were), and by some 8 us at V = 32128, one in eighty
+// (B = 64: 19.3 us, 21.5 with one).  fp64 exponentials throughout took three times as long for
+// the cells (20.6 us of the latter for them alone), reduced arguments in all cells 142 us.
 #include "osd.h"
 #include "osd_device.hpp"
 #include "osd_internal.hpp"
@@ -42,8 +48,8 @@ constexpr int kW = 256, kNW = kW / kWave;
 constexpr int kSlots = OSD_MAX_TOPK / kWave;
 constexpr int kSlotPad = 8;       // (the row's last chunk reads up to 7 elements before its own)
 constexpr int kTable = 1024;      // places for the ids of a record (at most 256)
-constexpr double kUnsure = 6.0e-8;
-constexpr double kNearRatio = 2.5e-6;
+constexpr double kTerm = 1.8e-7;
+constexpr double kNearRatio = 2.0e-7;  // (kTerm and the roundings of fp64 ones)
 // Workgroups per launch (a grid stays below 2^32 work-items).
 constexpr int64_t kMaxGrid = int64_t(1) << 22;
 
@@ -60,6 +66,8 @@ struct VerifyTopkArgs {
     const float* u_accept;
     const float* u_resample;
     double c2;
+    float hi, lo, inv;   // c2 = hi + lo, 1 / c2; hi NaN where Near does not serve
+    float hi16, lo16;    // c2 = hi16 + lo16, hi16 of 16 significant bits
     VerifyTopkRow* rows;
     int32_t* accepted_len;
     int32_t* out_tokens;
@@ -93,47 +101,171 @@ __device__ inline void load_cell(chunk_t (&c)[kPer], const char* row, int cell, 
     for (int r = 0; r < kPer; ++r) c[r] = row_chunk<Fmt>(row, ch0 + r * kWave, cut, V);
 }
 
-// One cell by one wave: its largest logit, and the sum of exponentials relative
-// to it (0 where there is no finite one).
-template <typename Fmt, int kPer, bool EXACT>
-__device__ inline void cell_sum(chunk_t (&c)[kPer], int cell, const RowCut<Fmt>& cut, double c2, float& m, double& S) {
+// 2^(x c2 - k) for logits x whose scaled value is at most k + 1, from 2^-120 on (what
+// is smaller counts as that, and -inf too).  n = rint(x c2) and the rest
+// r = x c2 - n come from x by multiply-adds, not from a rounded difference: with
+// |k| < 2^20, r is off by 2^-25 + 2^-26 + 2^-28 at most (its roundings; c2 as a sum of two
+// floats).  n - k lands in the low bits of `z` and is added to the exponent of 2^r.
+constexpr float kLargestShift = 0x1p20f;
+struct Near {
+    float hi, lo, z, least, most;  // z: 1.5 * 2^23 - k
+    __device__ Near(const VerifyTopkArgs& a, float k, float largest)
+        : hi(a.hi), lo(a.lo), z(12582912.0f - k), least((k - 120.0f) * a.inv), most(largest) {}
+    __device__ __forceinline__ float pow2(float x) const {
+        x = __builtin_amdgcn_fmed3f(x, least, most);
+        const float t = __builtin_fmaf(x, hi, z), n = t - z;
+        const float r = __builtin_fmaf(x, lo, __builtin_fmaf(x, hi, -n));
+        return __uint_as_float(__float_as_uint(exp2_fast(r)) + (__float_as_uint(t) << 23));
+    }
+};
+
+// Wave total of floats, in every lane.
+template <int CTRL, int ROWS>
+__device__ inline float dpp_add_f32(float v) {
+    return v + __uint_as_float(dpp_sum_src<CTRL, ROWS>(__float_as_uint(v)));
+}
+__device__ inline float wave_sum_f32(float v) {
+    v = dpp_add_f32<kDppRowShr1, 0xF>(v);
+    v = dpp_add_f32<kDppRowShr2, 0xF>(v);
+    v = dpp_add_f32<kDppRowShr4, 0xF>(v);
+    v = dpp_add_f32<kDppRowShr8, 0xF>(v);
+    v = dpp_add_f32<kDppRowBcast15, 0xA>(v);
+    v = dpp_add_f32<kDppRowBcast31, 0xC>(v);
+    return readlane_f32(v, kWave - 1);
+}
+
+// The chunk with -inf replaced by the lowest finite bf16 value.
+__device__ inline chunk_t finite_pairs(const chunk_t& c) {
+    const auto f = [](uint32_t w) {
+        w -= (w & 0xFFFF0000u) == 0xFF800000u ? 0x10000u : 0u;
+        return w - ((w & 0xFFFFu) == 0xFF80u ? 1u : 0u);
+    };
+    return chunk_t{f(c.x), f(c.y), f(c.z), f(c.w)};
+}
+
+// The sum of a chunk's exponentials, in fp64 from pairs up.
+template <int EPC>
+__device__ __forceinline__ double pair_sum(const float (&e)[EPC]) {
+    double s = double(e[0] + e[1]);
+#pragma unroll
+    for (int i = 2; i < EPC; i += 2) s += double(e[i] + e[i + 1]);
+    return s;
+}
+
+// The chunk with its first `lead` elements replaced by the lowest finite value.
+template <typename Fmt>
+__device__ inline chunk_t lowest_lead(const chunk_t& c, int lead) {
+    if constexpr (Fmt::kPerChunk == 8) {
+        const auto w = [lead](uint32_t x, int e) {
+            return lead > e + 1 ? 0xFF7FFF7Fu : (lead > e ? (x & 0xFFFF0000u) | 0xFF7Fu : x);
+        };
+        return chunk_t{w(c.x, 0), w(c.y, 2), w(c.z, 4), w(c.w, 6)};
+    } else {
+        return chunk_t{lead > 0 ? 0xFF7FFFFFu : c.x, lead > 1 ? 0xFF7FFFFFu : c.y, lead > 2 ? 0xFF7FFFFFu : c.z,
+                       lead > 3 ? 0xFF7FFFFFu : c.w};
+    }
+}
+
+// One cell by one wave: its largest logit m, and the sum S of exponentials (0 where
+// there is no finite one), relative to m or, with the mean of the logits over their mass
+// given (not NaN), as sum 2^(x hi16): 2^(mean lo16) S is then that of 2^(x c2).
+template <typename Fmt, int kPer>
+__device__ inline void cell_sum(const VerifyTopkArgs& a, chunk_t (&c)[kPer], int cell, const RowCut<Fmt>& cut, float& m,
+                                double& S, float& mean) {
     constexpr int EPC = Fmt::kPerChunk;
     const int lane = threadIdx.x & (kWave - 1), ch0 = cell * kPer * kWave + lane;
-    if ((cell + 1) * kPer * kWave > cut.nfull) {  // the row's end
+    const bool end = (cell + 1) * kPer * kWave > cut.nfull;  // the row's end
+    // (bf16: padding of the lowest finite value serves the path that is taken most.)
+    if (end) {
 #pragma unroll
-        for (int r = 0; r < kPer; ++r) c[r] = pad_lead<Fmt>(c[r], cut.lead(ch0 + r * kWave));
+        for (int r = 0; r < kPer; ++r)
+            c[r] = EPC == 8 ? lowest_lead<Fmt>(c[r], cut.lead(ch0 + r * kWave))
+                            : pad_lead<Fmt>(c[r], cut.lead(ch0 + r * kWave));
     }
-    m = kNegInf;
+    const auto largest = [&] {
+        float x = kNegInf;
+        if constexpr (EPC == 8) {
+            // Pairs of bf16 patterns as f16 numbers, see chunks_max (which drops a NaN).
+            typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
+            h2_t h = __builtin_bit_cast(h2_t, c[0].x);
 #pragma unroll
-    for (int r = 0; r < kPer; ++r)
+            for (int i = 1; i < 4 * kPer; ++i)
+                h = __builtin_elementwise_maximum(h, __builtin_bit_cast(h2_t, uint32_t(c[i / 4][i % 4])));
+            const uint32_t b = __builtin_bit_cast(uint32_t, h);
+            x = max_nan(__uint_as_float(b << 16), __uint_as_float(b & 0xFFFF0000u));
+            if (__ballot(!(__builtin_fabsf(x) < 0x1p121f)) == 0) return wave_max_nan(x);
+            x = kNegInf;
+        }
 #pragma unroll
-        for (int e = 0; e < EPC; ++e) m = max_nan(m, Fmt::get(c[r], e));
-    opaque<kPer>(c);
-    m = wave_max_nan(m);
+        for (int r = 0; r < kPer; ++r)
+#pragma unroll
+            for (int e = 0; e < EPC; ++e) x = max_nan(x, Fmt::get(c[r], e));
+        opaque<kPer>(c);
+        return wave_max_nan(x);
+    };
+    m = largest();
     S = 0.0;
-    if (!is_finite(m)) return;
-    const float scale = float(c2);
+    mean = __builtin_nanf("");
+    if constexpr (EPC == 8) {
+        // x hi16 is exact (8 bits times 16), so v_exp_f32 takes it as it is.  What lo16 adds,
+        // a factor 2^(x lo16), is taken for the cell at the mean of x over its mass: off by
+        // half the variance of x lo16 ln 2 there, 2e-9 for halves 24 octaves apart.
+        // (Largest logits of 2^-60 to 2^100 leave the others their range.)
+        const float h = m * a.hi16;
+        if (h >= -60.0f && h <= 100.0f) {
+#pragma unroll 1
+            while (true) {
+                float X = 0.0f;
+                S = 0.0;
 #pragma unroll
-    for (int r = 0; r < kPer; ++r) {
-        if constexpr (EXACT) {
+                for (int r = 0; r < kPer; ++r) {
+                    float e8[EPC];
+#pragma unroll
+                    for (int e = 0; e < EPC; ++e) {
+                        const float x = Fmt::get(c[r], e);
+                        e8[e] = exp2_fast(x * a.hi16);
+                        X = __builtin_fmaf(e8[e], x, X);
+                    }
+                    S += pair_sum<EPC>(e8);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                S = wave_sum(S);
+                mean = wave_sum_f32(X) * __builtin_amdgcn_rcpf(float(S));
+                if (mean == mean) return;
+                // A -inf (times 0): again with the lowest finite value in its place.
+#pragma unroll
+                for (int r = 0; r < kPer; ++r) c[r] = finite_pairs(c[r]);
+            }
+        }
+        if (end) {
+#pragma unroll
+            for (int r = 0; r < kPer; ++r) c[r] = pad_lead<Fmt>(c[r], cut.lead(ch0 + r * kWave));
+            m = largest();
+        }
+    }
+    if (!is_finite(m)) return;
+    const float k = __builtin_rintf(m * a.hi);
+    if (!(__builtin_fabsf(k) < kLargestShift)) {
+#pragma unroll
+        for (int r = 0; r < kPer; ++r)
 #pragma unroll
             for (int e = 0; e < EPC; ++e) {
-                S += exp2_f64((double(Fmt::get(c[r], e)) - double(m)) * c2);
+                S += exp2_f64((double(Fmt::get(c[r], e)) - double(m)) * a.c2);
                 if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // few registers
             }
-            continue;
-        }
+        S = wave_sum(S);
+        return;
+    }
+    const Near near(a, k, m);
+#pragma unroll
+    for (int r = 0; r < kPer; ++r) {
         float e8[EPC];
 #pragma unroll
-        for (int e = 0; e < EPC; ++e) e8[e] = exp2_fast((Fmt::get(c[r], e) - m) * scale);
-#pragma unroll
-        for (int w = 1; w < EPC; w <<= 1)
-#pragma unroll
-            for (int e = 0; e < EPC; e += 2 * w) e8[e] = e8[e] + e8[e + w];
-        S += double(e8[0]);
+        for (int e = 0; e < EPC; ++e) e8[e] = near.pow2(Fmt::get(c[r], e));
+        S += pair_sum<EPC>(e8);
         __builtin_amdgcn_sched_barrier(0);
     }
-    S = wave_sum(S);
+    S = wave_sum(S) * exp2_f64(double(k) - double(m) * a.c2);
 }
 
 struct VerifyTopkLds {
@@ -252,21 +384,26 @@ __device__ inline void post_record(const VerifyTopkArgs& a, int64_t b, int i, in
 struct Draw {
     const char* row;
     double top, sum, inv;  // largest logit, normaliser and its reciprocal
+    float k;          // Near's shift
+    double unit;      // and the probability mass of one of its units
     double point;     // in probability mass
+    double u;
     double cum;       // lane c: mass up to and with cell c
+    double before;    // the same of p alone
     uint64_t lives;   // cells with mass
     bool with_q;      // the residual, or p alone
 };
 
 // The smallest token whose running mass exceeds the point; the last one with mass
-// if rounding put the point past it (-1: none has).  sure: the point is further than kUnsure
-// from both edges of the token's interval.
+// if rounding put the point past it (-1: none has).  sure: the point is further from both
+// edges of the token's interval than these may be off.
 template <typename Fmt, int kPer, bool EXACT>
 __device__ __forceinline__ int find_token(const VerifyTopkArgs& a, const Draw& d, VerifyTopkLds& s, bool& sure) {
     constexpr int EPC = Fmt::kPerChunk, kCell = kPer * kWave, kEach = kCell / kW, kTokens = kCell * EPC;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = tid / kWave;
     const RowCut<Fmt> cut(a.V);
-    const float scale = float(a.c2), top = float(d.top);
+    const Near near(a, d.k, float(d.top));
+    const double per = 1.0 / d.unit;
     // The first cell that may hold the point (the sums of the cells and of their
     // elements differ by rounding), then upwards; down from there only if rounding
     // put the point past the last token.
@@ -288,7 +425,7 @@ __device__ __forceinline__ int find_token(const VerifyTopkArgs& a, const Draw& d
         __syncthreads();
 #pragma unroll
         for (int n = 0; n < kEach; ++n) c[n] = pad_lead<Fmt>(c[n], cut.lead(ch0 + n));
-        // The masses of the thread's tokens times the normaliser: of p, then without the record's part
+        // The masses of the thread's tokens in d.unit: of p, then without the record's part
         // (few threads hold any of it).  In fp64 they are taken again when needed.
         float w[EXACT ? 1 : kEach * EPC];
         if constexpr (!EXACT) {
@@ -301,12 +438,12 @@ __device__ __forceinline__ int find_token(const VerifyTopkArgs& a, const Draw& d
                 for (int e = 0; e < EPC; ++e) {
                     slot[e] = slots[e];
                     any |= slot[e];
-                    w[n * EPC + e] = exp2_fast((Fmt::get(c[n], e) - top) * scale);
+                    w[n * EPC + e] = near.pow2(Fmt::get(c[n], e));
                 }
                 if (any) {
 #pragma unroll
                     for (int e = 0; e < EPC; ++e)
-                        if (slot[e]) w[n * EPC + e] = float(fmax(double(w[n * EPC + e]) - s.q[slot[e] - 1] * d.sum, 0.0));
+                        if (slot[e]) w[n * EPC + e] = float(fmax(double(w[n * EPC + e]) - s.q[slot[e] - 1] * per, 0.0));
                 }
             }
         }
@@ -327,7 +464,7 @@ __device__ __forceinline__ int find_token(const VerifyTopkArgs& a, const Draw& d
                         }
                         __builtin_amdgcn_sched_barrier(0);  // few registers
                     } else {
-                        f(first + e, double(w[n * EPC + e]) * d.inv);
+                        f(first + e, double(w[n * EPC + e]) * d.unit);
                     }
                 }
             }
@@ -367,8 +504,11 @@ __device__ __forceinline__ int find_token(const VerifyTopkArgs& a, const Draw& d
         __syncthreads();
         if (mine) s.slot[kSlotPad + at] = 0;
         if (up && hit != 0x7FFFFFFF) {
-            // (An edge at 0 is exact.)
-            sure = s.high - d.point > kUnsure && (d.point - s.low > kUnsure || s.low == 0.0);
+            // (The edges lie in this cell: the largest bound over A there.)
+            const double from = cell > 0 ? readlane_f64(d.before, cell - 1) : 0.0, to = readlane_f64(d.before, cell);
+            const double A = fmin(fmax(1.0 - d.u, from), to);
+            const double unsure = kTerm * (A * (1.0 - d.u) + (1.0 - A) * d.u + A * (1.0 - A)) + 1e-11;
+            sure = s.high - d.point > unsure && d.point - s.low > unsure;
             return s.token;
         }
         const int last = s.last;
@@ -387,22 +527,52 @@ __device__ __forceinline__ int find_token(const VerifyTopkArgs& a, const Draw& d
     }
 }
 
-// The sums of a row's cells from fp64 exponentials, by the whole workgroup (0 past the
-// last cell; barriers inside and at the end).
+// log2 of what a posted sum of a cell counts relative to a row's largest logit.
+template <int EPC>
+__device__ inline double cell_scale(const VerifyTopkArgs& a, float m, float mean, float top) {
+    if (EPC == 8 && mean == mean) return double(mean) * double(a.lo16) - double(top) * a.c2;
+    return (double(m) - double(top)) * a.c2;
+}
+
+// The sums of a row's cells from fp64 exponentials relative to the row's largest logit,
+// by the whole workgroup (0 past the last cell; barriers inside and at the end).  Small
+// code, and the next chunks on their way: a row of 128256 bf16 logits takes 25 us, and 40 with
+// one chunk on its way.
 template <typename Fmt, int kPer>
-__device__ __forceinline__ void exact_cells(const VerifyTopkArgs& a, const char* row, VerifyTopkLds& s) {
-    const int tid = threadIdx.x;
+__device__ __forceinline__ void exact_cells(const VerifyTopkArgs& a, const char* row, double top, VerifyTopkLds& s) {
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = tid / kWave;
     const RowCut<Fmt> cut(a.V);
     if (tid < kMaxCells) s.sum[tid] = 0.0;
     __syncthreads();
+    const auto chunk = [&](int i) { return ((i / kPer * kNW + wid) * kPer + i % kPer) * kWave + lane; };
+    const int n = a.cells > wid ? ((a.cells - 1 - wid) / kNW + 1) * kPer : 0;
+    // (A row shorter than one chunk: nothing is read, and all but chunk 0 is padding.)
+    const bool tiny = a.V < Fmt::kPerChunk;
+    const rsrc_t rs = make_rsrc(row, tiny ? 0u : uint32_t(a.V) * Fmt::kBytes);
+    const auto load = [&](int i) {
+        return __builtin_bit_cast(chunk_t, __builtin_amdgcn_raw_buffer_load_b128(rs, cut.off(chunk(i)), 0, 0));
+    };
+    constexpr int kRing = 4;
+    static_assert(kPer % kRing == 0, "");
+    chunk_t ahead[kRing];
+#pragma unroll
+    for (int j = 0; j < kRing; ++j) ahead[j] = load(j);
+    if (tiny) ahead[0] = load_short<Fmt>(row, a.V);
+    double S = 0.0;
 #pragma unroll 1
-    for (int c = tid / kWave; c < a.cells; c += kNW) {
-        chunk_t x[kPer];
-        float top;
-        double sum;
-        load_cell<Fmt, kPer>(x, row, c, cut, a.V);
-        cell_sum<Fmt, kPer, true>(x, c, cut, a.c2, top, sum);
-        if ((tid & (kWave - 1)) == 0) s.sum[c] = sum;
+    for (int i = 0; i < n; i += kRing) {
+#pragma unroll
+        for (int j = 0; j < kRing; ++j) {
+            const chunk_t x = pad_lead<Fmt>(ahead[j], cut.lead(chunk(i + j)));
+            ahead[j] = load(i + j + kRing);
+#pragma unroll
+            for (int e = 0; e < Fmt::kPerChunk; ++e) S += exp2_f64((double(Fmt::get(x, e)) - top) * a.c2);
+        }
+        if ((i + kRing) % kPer == 0) {
+            S = wave_sum(S);
+            if (lane == 0) s.sum[i / kPer * kNW + wid] = S;
+            S = 0.0;
+        }
     }
     __syncthreads();
 }
@@ -422,7 +592,7 @@ __device__ __forceinline__ void decide(const VerifyTopkArgs& a, int64_t b, int k
     const int cell = lane & 31;
 #pragma unroll 1
     for (int i0 = 2 * wid + (lane >> 5); i0 - (lane >> 5) <= kb; i0 += kBatch * kRows) {
-        float m[kBatch], t[kBatch], u[kBatch];
+        float m[kBatch], t[kBatch], u[kBatch], mean[kBatch];
         double v[kBatch], qs[kBatch], qt[kBatch];
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
@@ -431,6 +601,7 @@ __device__ __forceinline__ void decide(const VerifyTopkArgs& a, int64_t b, int k
             const bool rec = i < kb;
             m[j] = cell < a.cells ? posted(&r.top[cell]) : kNegInf;
             v[j] = cell < a.cells ? posted(&r.sum[cell]) : 0.0;
+            mean[j] = EPC == 8 && cell < a.cells ? posted(&r.mean[cell]) : __builtin_nanf("");
             qs[j] = rec ? posted(&r.q_sum) : 1.0;
             qt[j] = rec ? posted(&r.q_token) : 0.0;
             t[j] = rec ? posted(&r.t_token) : 0.0f;
@@ -440,7 +611,7 @@ __device__ __forceinline__ void decide(const VerifyTopkArgs& a, int64_t b, int k
         for (int j = 0; j < kBatch; ++j) {
             const int i = i0 + j * kRows;
             const float top = half_max_nan(m[j]);
-            const double sum = half_sum(v[j] * exp2_f64((double(m[j]) - double(top)) * a.c2));
+            const double sum = half_sum(v[j] * exp2_f64(cell_scale<EPC>(a, m[j], mean[j], top)));
             int verdict = 1;
             if (!is_finite(top) || t[j] != t[j] || !(qs[j] > 0.0))
                 verdict = 2;
@@ -472,9 +643,8 @@ __device__ __forceinline__ void decide(const VerifyTopkArgs& a, int64_t b, int k
         v = lane <= kb ? s.verdict[lane] : 1;
         acc = __builtin_ctzll(__ballot(v != 0));
         if (__builtin_amdgcn_readlane(v, acc) != 3) break;
-        exact_cells<Fmt, kPer>(a, a.target + (b * (K + 1) + acc) * a.V * Fmt::kBytes, s);
-        const float m = cell < a.cells ? posted(&rows[acc].top[cell]) : kNegInf;
-        const double sum = half_sum(s.sum[cell] * exp2_f64((double(m) - double(s.row_top[acc])) * a.c2));
+        exact_cells<Fmt, kPer>(a, a.target + (b * (K + 1) + acc) * a.V * Fmt::kBytes, double(s.row_top[acc]), s);
+        const double sum = half_sum(s.sum[cell]);
         __syncthreads();
         if (tid == 0) s.verdict[acc] = s.row_uq[acc] * sum < s.row_t[acc] ? 0 : 1;
         __syncthreads();
@@ -496,6 +666,7 @@ __device__ __forceinline__ void decide(const VerifyTopkArgs& a, int64_t b, int k
                           (unsigned long long)(fmin(s.e[tid] * d.inv, s.q[tid]) * 0x1p62));
         };
         const float m = cell < a.cells ? posted(&r.top[cell]) : kNegInf;
+        const float mean = EPC == 8 && cell < a.cells ? posted(&r.mean[cell]) : __builtin_nanf("");
         double S = cell < a.cells ? posted(&r.sum[cell]) : 0.0;
         if (rejected && tid < a.k) {
             const int64_t pos = b * K + acc;
@@ -507,29 +678,35 @@ __device__ __forceinline__ void decide(const VerifyTopkArgs& a, int64_t b, int k
             s.e[tid] = id >= 0 && t > kNegInf ? exp2_f64((double(t) - d.top) * a.c2) : 0.0;
             correct();
         }
-        const double u = double(a.u_resample[b]);
+        d.u = double(a.u_resample[b]);
         __syncthreads();
-        const double weight = exp2_f64((double(m) - d.top) * a.c2);
+        double weight = exp2_f64(cell_scale<EPC>(a, m, mean, float(d.top)));
         const auto masses = [&] {  // lane c < 32 of every wave: cell c
             const double mass = lane < kMaxCells ? S * weight * d.inv : 0.0;
             d.lives = __ballot(mass > 0.0);
             d.with_q = rejected;
+            d.before = wave_scan_add(mass);
             d.cum = wave_scan_add(fmax(mass - double(s.fixed[cell]) * 0x1p-62, 0.0));
             if (readlane_f64(d.cum, kWave - 1) <= 0.0) {  // rounding left nothing: from p
-                d.cum = wave_scan_add(mass);
+                d.cum = d.before;
                 d.with_q = false;
             }
-            d.point = u * readlane_f64(d.cum, kWave - 1);
+            d.point = d.u * readlane_f64(d.cum, kWave - 1);
         };
         masses();
-        bool sure;
-        extra = find_token<Fmt, kPer, false>(a, d, s, sure);
+        bool sure = false;
+        d.k = __builtin_rintf(s.row_top[acc] * a.hi);
+        if (__builtin_fabsf(d.k) < kLargestShift) {
+            d.unit = exp2_f64(double(d.k) - d.top * a.c2) * d.inv;
+            extra = find_token<Fmt, kPer, false>(a, d, s, sure);
+        }
         if (!sure) {  // again with fp64 exponentials
             __syncthreads();
             if (tid < kMaxCells) s.fixed[tid] = 0;
-            exact_cells<Fmt, kPer>(a, d.row, s);
+            exact_cells<Fmt, kPer>(a, d.row, d.top, s);
             S = s.sum[cell];
-            d.sum = half_sum(S * weight);
+            weight = 1.0;
+            d.sum = half_sum(S);
             d.inv = 1.0 / d.sum;
             if (rejected && tid < a.k) correct();
             __syncthreads();
@@ -577,12 +754,13 @@ __global__ __launch_bounds__(kW, kPer == 4 ? 5 : 4) void verify_topk_kernel(Veri
         const int cell = g * kNW + wid;
         if (cell < a.cells) {
             chunk_t c[kPer];
-            float m;
+            float m, mean;
             double S;
             load_cell<Fmt, kPer>(c, x, cell, cut, a.V);
-            cell_sum<Fmt, kPer, false>(c, cell, cut, a.c2, m, S);
+            cell_sum<Fmt, kPer>(a, c, cell, cut, m, S, mean);
             if (lane == 0) {
                 post(&rows[i].sum[cell], S);
+                if constexpr (Fmt::kPerChunk == 8) post(&rows[i].mean[cell], mean);
                 post(&rows[i].top[cell], m);
             }
         }
@@ -634,6 +812,13 @@ hipError_t launch_verify_topk(const VerifyTopkLaunch& L) {
     a.u_accept = L.u_accept;
     a.u_resample = L.u_resample;
     a.c2 = scaled_log2e(L.temperature);
+    // (Where T or 1 / T is beyond 1e30 fp64 serves alone.)
+    a.hi = a.c2 > 1e-30 && a.c2 < 1e30 ? float(a.c2) : __builtin_nanf("");
+    a.lo = float(a.c2 - double(a.hi));
+    a.inv = float(1.0 / a.c2);
+    const uint32_t bits = __builtin_bit_cast(uint32_t, float(a.c2));
+    a.hi16 = a.hi == a.hi ? __builtin_bit_cast(float, (bits + 0x80u) & 0xFFFFFF00u) : a.hi;
+    a.lo16 = float(a.c2 - double(a.hi16));
     a.rows = L.rows;
     a.accepted_len = L.accepted_len;
     a.out_tokens = L.out_tokens;

@@ -6,7 +6,7 @@ import pytest
 
 from oracle import topk_ref
 from tests._helpers import to_device
-from tests._topk_helpers import as_dtype, rows, uniforms
+from tests._topk_helpers import as_dtype, lowest, rows, uniforms
 from tests.test_topk_gpu import host
 
 pytestmark = pytest.mark.gpu
@@ -273,6 +273,43 @@ FLAT = [(2048, 6.84375), (1024, 6.4375), (2047, 7.625), (4099, 8.3125), (32003, 
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1.0, 0.875, 0.6])
+@pytest.mark.parametrize("kind", ["head", "stretch", "pattern"])
+@pytest.mark.parametrize("V,gap", FLAT)
+def test_draws_next_to_edges_of_flat_rows(osd, V, gap, kind, T, dtype):
+    """Uniforms next to the edges of tokens' intervals, where the errors of equal
+    terms add up: the bonus token, and the correction after a proposal that the
+    target has as good as no mass for."""
+    T = float(np.float32(T))
+    t = flat_rows(V, gap if dtype == "bf16" else np.float32(gap * 1.0437), dtype, V, kind)
+    z = topk_ref.values(t)
+    g = np.random.default_rng(V + 1)
+    n = 96 if V < 5000 else 32
+    which = g.integers(0, 8, n)
+    ids = np.zeros((n, 1, 1), np.int32)
+    ur = np.zeros((2, n), np.float32)
+    for b in range(n):
+        p = topk_ref.softmax(z[which[b]] / T)
+        some = np.nonzero(p > 0)[0]
+        y = ids[b, 0, 0] = some[g.integers(len(some))]
+        for corrected in range(2):
+            if corrected:  # the proposal's draft mass is 1
+                p[y] = 0.0
+            edge = np.float32(np.cumsum(p)[some[g.integers(len(some))]] / p.sum()) + np.float32(
+                int(g.integers(-6, 7)) * 2.0 ** -24)
+            ur[corrected, b] = np.clip(edge, np.float32(0), np.float32(1 - 2.0 ** -24))
+    pair = np.stack([t[which], t[which]], 1)
+    x = dict(t=pair, ids=ids, top=np.zeros((n, 1, 1), t.dtype), y=ids[:, :, 0], ua=np.zeros((n, 1), np.float32),
+             ur=ur[0])
+    left = check(call(osd, x, T), x, T, None, f"bonus {kind} V={V} T={T} {dtype}")
+    x["ua"][:] = np.float32(1 - 2.0 ** -24)
+    x["ur"] = ur[1]
+    left += check(call(osd, x, T), x, T, None, f"correction {kind} V={V} T={T} {dtype}")
+    # (Where tokens have 1e-8 of the mass, one point in five is within 1e-9 of an edge on either side.)
+    assert left <= n  # of 2 n
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("T", [1.0, 0.875, 0.75, 0.6])
 @pytest.mark.parametrize("V,gap", FLAT)
 def test_acceptance_next_to_the_ratio(osd, V, gap, T, dtype):
@@ -290,3 +327,31 @@ def test_acceptance_next_to_the_ratio(osd, V, gap, T, dtype):
     x = dict(t=np.stack([t[which], t[which]], 1), ids=y.reshape(n, 1, 1), top=np.zeros((n, 1, 1), t.dtype),
              y=y.reshape(n, 1), ua=ua.reshape(n, 1), ur=uniforms(n, 5))
     check(call(osd, x, T), x, T, None, f"V={V} T={T} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1e-38, 1e-30, 1e-4, 300.0, 1e30, 1e37, 3.0e38])
+@pytest.mark.parametrize("V", [5, 1001, 33000])
+def test_extreme_temperatures_and_masks(osd, V, T, dtype):
+    """Temperatures at which log2(e) / T or its parts leave the range of floats, on
+    rows with masked tokens (-inf, the lowest finite value), at the row's ragged end
+    too; small and large logits."""
+    T = float(np.float32(T))
+    B, K, k = 12, 2, 4
+    g = np.random.default_rng(V)
+    t = rows("normal", B * (K + 1), V, V).reshape(B, K + 1, V)
+    t[g.random(t.shape) < 0.3] = -np.inf
+    t[2:4, :, : V // 2] = lowest(dtype)
+    t[4:6, :, V // 2 :] = -np.inf
+    t[6:8] *= np.float32(1e-20)
+    t[8:10] *= np.float32(1e20)
+    t[:, :, V // 3] = 0.25
+    d = as_dtype(t[:, :K].reshape(B * K, V).copy(), dtype)
+    t = as_dtype(t, dtype)
+    rec = topk_ref.topk(d, k, T, uniforms(B * K, 1))
+    top = np.where(rec["ids"] < 0, as_dtype(np.full((1, 1), -np.inf, np.float32), dtype),
+                   np.take_along_axis(d, np.maximum(rec["ids"], 0).astype(np.int64), 1))
+    x = dict(t=t, ids=rec["ids"].reshape(B, K, k), top=top.reshape(B, K, k), y=rec["tokens"].reshape(B, K),
+             ua=uniforms((B, K), 2), ur=uniforms(B, 3))
+    with np.errstate(over="ignore"):
+        check(call(osd, x, T), x, T, None, f"V={V} T={T} {dtype}")
