@@ -27,7 +27,9 @@
 //   E = (1 - u) sum_{j <= t} p_j e_j - u sum_{j > t} p_j e_j,
 // e_j = d_j - D where the token keeps mass and d_j where the record takes all of it (its
 // exact exponential is subtracted).  With A the mass of p up to the token, collecting d_j,
-//   |E| <= kTerm (A (1 - u) + (1 - A) u + A (1 - A)).
+//   |E| <= kTerm (A (1 - u) + (1 - A) u + A (1 - A) + 1.5 c),
+// where c is the mass of the cell that holds the token: its tokens are summed anew, with
+// other errors (at most 1.2e-7) than they have in the cell's sum (1.5e-7 in bf16).
 // A draw whose point lies within that of an edge of its token's interval is decided again
 // on fp64 exponentials of the whole row (1e-12), and so is a test where u q / p and 1
 // differ by less than kNearRatio (the normaliser is off by kTerm).  That holds up its
@@ -507,7 +509,8 @@ __device__ __forceinline__ int find_token(const VerifyTopkArgs& a, const Draw& d
             // (The edges lie in this cell: the largest bound over A there.)
             const double from = cell > 0 ? readlane_f64(d.before, cell - 1) : 0.0, to = readlane_f64(d.before, cell);
             const double A = fmin(fmax(1.0 - d.u, from), to);
-            const double unsure = kTerm * (A * (1.0 - d.u) + (1.0 - A) * d.u + A * (1.0 - A)) + 1e-11;
+            const double unsure =
+                kTerm * (A * (1.0 - d.u) + (1.0 - A) * d.u + A * (1.0 - A) + 1.5 * (to - from)) + 1e-11;
             sure = s.high - d.point > unsure && d.point - s.low > unsure;
             return s.token;
         }
