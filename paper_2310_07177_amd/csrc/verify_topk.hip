@@ -699,7 +699,8 @@ __device__ __forceinline__ void decide(const VerifyTopkArgs& a, int64_t b, int k
         masses();
         bool sure = false;
         d.k = __builtin_rintf(s.row_top[acc] * a.hi);
-        if (__builtin_fabsf(d.k) < kLargestShift) {
+        // (Nothing left of p by these sums: fp64 ones have to say so before p is drawn from.)
+        if (d.with_q == rejected && __builtin_fabsf(d.k) < kLargestShift) {
             d.unit = exp2_f64(double(d.k) - d.top * a.c2) * d.inv;
             extra = find_token<Fmt, kPer, false>(a, d, s, sure);
         }

@@ -355,3 +355,34 @@ def test_extreme_temperatures_and_masks(osd, V, T, dtype):
              ua=uniforms((B, K), 2), ur=uniforms(B, 3))
     with np.errstate(over="ignore"):
         check(call(osd, x, T), x, T, None, f"V={V} T={T} {dtype}")
+
+
+@pytest.mark.parametrize("T", [1.0, 0.875, 0.75, 0.6])
+def test_residual_of_one_token_with_little_mass(osd, T):
+    """A draft that is the target but for one token, which it lacks: at u next to 1
+    a proposal is rejected, and that token is the correction however little mass it
+    has (fp32 masses leave less than their rounding, or nothing).  The record: one
+    logit far above 255 equal ones, or any."""
+    V, k, n = 1000, 256, 160
+    T = float(np.float32(T))
+    g = np.random.default_rng(3)
+    t = np.full((n, 2, V), -np.inf, np.float32)
+    ids = np.stack([np.sort(g.choice(V, k, replace=False)) for _ in range(n)]).astype(np.int32)
+    top = g.normal(0, 2, (n, k)).astype(np.float32)
+    left = np.zeros(n, np.int64)
+    for b in range(n):
+        if b % 4:
+            top[b] = -T * (np.log(k - 1) + g.random())
+            top[b, g.integers(k)] = 0.0
+        left[b] = g.choice(np.setdiff1d(np.arange(V), ids[b]))
+        t[b, :, ids[b]] = top[b][:, None]
+        mass = np.exp(top[b].astype(np.float64) / T).sum()
+        t[b, :, left[b]] = T * np.log(mass * np.geomspace(7e-8, 1e-6, n)[b])
+    x = dict(t=t, ids=ids.reshape(n, 1, k), top=top.reshape(n, 1, k), y=ids[np.arange(n), top.argmax(1)].reshape(n, 1),
+             ua=np.full((n, 1), 1 - 2.0 ** -24, np.float32), ur=uniforms(n, 4))
+    acc, toks, rmask = (host(o) for o in call(osd, x, T))
+    wa, wt, wm, margin = topk_ref.verify(x["t"], x["ids"], x["top"], x["y"], x["ua"], x["ur"], T)
+    sure = margin > 1e-10  # (the fp64 exponentials are within 1e-12)
+    assert sure.sum() > n // 2 and (wa[sure] == 0).all() and (wt[sure, 0] == left[sure]).all()
+    bad = sure & ((acc != wa) | (toks[:, 0] != wt[:, 0]))
+    assert not bad.any(), f"{bad.sum()}: {acc[bad]} {toks[bad, 0]} for {wt[bad, 0]}"
