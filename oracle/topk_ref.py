@@ -52,10 +52,9 @@ def topk(x, k, T, u=None):
         if T == 0:
             tokens[n] = order[0]
             continue
-        with np.errstate(divide="ignore"):
-            e = np.exp((r - r[order[0]]) / T)
-            e[order] = 0.0
-            rest[n] = np.log(e.sum())
+        out = np.delete(r, order)
+        if (out > -INF).any():  # (relative to their largest: exp has no range for far ones)
+            rest[n] = (out.max() - r[order[0]]) / T + np.log(np.exp((out - out.max()) / T).sum())
         if u is not None:
             s, margin[n] = inverse_cdf(np.exp((r[order] - r[order[0]]) / T), u[n])
             tokens[n] = order[s]

@@ -15,8 +15,9 @@
 //
 // The mass of the tokens outside the record is the sum over the groups below the
 // threshold, what the others hold besides candidates, and the candidates that were
-// not taken: nothing is subtracted, so it keeps its relative accuracy however small
-// it is.  The draw sums fp64 exponentials of the record's logits.
+// not taken: nothing is subtracted, so it keeps its relative accuracy down to 2^-60 of the
+// largest logit's; below that it is summed over the row once more, relative to the
+// largest logit outside.  The draw sums fp64 exponentials of the record's logits.
 //
 // What bounds it in bulk is instruction issue: a row of 64 KB arrives at a CU in 2.7
 // us, in which its four SIMDs issue some 6500 vector instructions, and the sweep
@@ -67,7 +68,7 @@ struct TopkLds {
     uint32_t bin[kBins];         // counts, then where each bin's candidates begin
     uint32_t fill[kBins];
     double sum[W / kWave];
-    uint32_t maxkey, tkey, ncand, count;
+    uint32_t maxkey, tkey, ncand, count, far;
 };
 
 // Candidates come first: larger logit, then lower id.
@@ -181,9 +182,9 @@ __device__ __forceinline__ void unrolled(std::integer_sequence<int, R...>, F f) 
     (f(std::integral_constant<int, R>{}), ...);
 }
 
-// Elements of the row, in chunk order, that `f` is called with: every chunk of the
-// row by the whole workgroup, kAhead of them requested at a time (rare: small
-// code before speed).
+// Calls f(logit, token) for the elements of the row (-inf: padding too), every chunk of it by
+// the whole workgroup (rare: small code before speed; two or four chunks of a thread
+// requested at a time were no faster).
 template <typename Fmt, int W, typename F>
 __device__ __forceinline__ void over_row(const char* row, const RowCut<Fmt>& cut, int V, F f) {
 #pragma unroll 1
@@ -446,7 +447,50 @@ __global__ __launch_bounds__(W, W == 1024 ? 4 : W == 512 ? 6 : 5) void topk_row_
         double t = lane < NW ? s.sum[lane] : 0.0;
         for (int r = k + lane; r < nc; r += kWave) t += double(weight(key_float(uint32_t(s.sorted[r] >> 32))));
         t = wave_sum(t);
-        if (lane == 0) a.rest[n] = t > 0.0 ? float(log2_f64(t) * kLn2) : kNegInf;
+        if (lane == 0) {
+            // (Fewer candidates than slots: they are the row's finite logits.)
+            s.far = t < 0x1p-60 && nc >= k && k < a.V;
+            if (!s.far) a.rest[n] = t > 0.0 ? float(log2_f64(t) * kLn2) : kNegInf;
+        }
+    }
+    if (a.rest) {
+        __syncthreads();
+        // Far below the largest logit fp32 exponentials relative to it, or to a thread's
+        // first chunk, leave their range one after another (2^-126): the others' largest
+        // logit, then their mass relative to that, over the row once more each (576 rows of
+        // 32128 bf16 logits ~ N(0, 9), k = 64: 17 us at T = 1, 38 at T = 0.1, where most
+        // rows come here).
+        if (uniform(s.far)) {
+            const uint64_t last = s.sorted[k - 1];
+            const float xk = key_float(uint32_t(last >> 32));
+            const int tk = int(~uint32_t(last));
+            const auto outside = [&](float x, int token) __attribute__((always_inline)) {
+                return int(x < xk) | (int(x == xk) & int(token > tk)) ? x : kNegInf;
+            };
+            float most = kNegInf;
+            over_row<Fmt, W>(row, cut, a.V, [&](float x, int token) __attribute__((always_inline)) {
+                most = fmaxf(most, outside(x, token));
+            });
+            most = wave_max(most);
+            if (lane == 0) s.key[wid] = float_key(most);
+            __syncthreads();
+            most = wave_max(lane < NW ? key_float(s.key[lane]) : kNegInf);
+            double mass = 0.0;
+            if (most > kNegInf)
+                over_row<Fmt, W>(row, cut, a.V, [&](float x, int token) __attribute__((always_inline)) {
+                    mass += double(exp2_fast((outside(x, token) - most) * c2));
+                });
+            mass = wave_sum(mass);
+            if (lane == 0) s.sum[wid] = mass;
+            __syncthreads();
+            if (wid == 0) {
+                mass = wave_sum(lane < NW ? s.sum[lane] : 0.0);
+                if (lane == 0)
+                    a.rest[n] = most > kNegInf
+                                    ? float(((double(most) - double(top)) * a.c2 + log2_f64(mass)) * kLn2)
+                                    : kNegInf;
+            }
+        }
     }
     if (wid == NW - 1 && a.tokens) {
         const int held = min(nc, k);

@@ -487,3 +487,41 @@ def test_gradient_of_a_student_with_finite_fills(osd, fill, V, kind, dtype):
     err, lim = np.abs(gr - wg), (step + 2.0 ** -15) * np.abs(wg) + 40 * LOG_SUM * qof(s, tau) + tiny
     bad = ~(err <= lim)
     assert not bad.any(), f"{bad.sum()}: {gr[bad][:3]} for {wg[bad][:3]}"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["fkl", "rkl", "jsd"])
+@pytest.mark.parametrize("tau,gap", [(1.0, 88.0), (1.0, 110.0), (1.0, 600.0), (1.0, 1.0e4), (0.05, 0.0), (0.02, 0.0)])
+@pytest.mark.parametrize("V", [1001, 32003])
+def test_records_of_teachers_with_little_mass_outside(osd, V, tau, gap, kind, dtype):
+    """osd_topk's records of rows with far peaks and at small temperatures, distilled
+    from: KL(q || p) needs the logarithm of the teacher's rest, however small that is.
+
+    The rest is within 8.4e-6 and half a step of the exact one (test_topk_gpu.py), which
+    enters D through the student's Q <= 1 once and its gradient through q_j Q.  The
+    others' exponentials are taken relative to their largest in 32 bits: below 2^-126 of
+    it (reached at small tau) v_exp_f32 gives 0, which leaves out less than 2^-126 of the
+    largest gradient."""
+    tau = float(np.float32(tau))
+    B, k = 4, 40
+    g = np.random.default_rng(V)
+    t, s = rows("normal", B, V, 90), rows("normal", B, V, 91)
+    for n, peaks in enumerate((1, 5, k, 0)):
+        t[n, g.choice(V, peaks, replace=False)] += np.float32(gap)
+    t, s = as_dtype(t, dtype), as_dtype(s, dtype)
+    ids, top, rest, _ = osd.osd_topk(to_device(t), k, tau)
+    wi, wt, wrest = record(t, k, tau)
+    assert np.array_equal(host(ids), wi) and np.isfinite(host(rest)).all()
+    got = osd.osd_distill_topk_loss_grad(ids.view(B, 1, k), top.view(B, 1, k), rest.view(B, 1),
+                                         to_device(s.reshape(B, 1, V)), kind, 0.5, tau)
+    wl, wr, wg = topk_ref.distill(wi, wt, topk_ref.topk(t, k, tau)["rest"], s, kind, 0.5, tau)
+    off = 8.4e-6 + 2.0 ** -24 * np.abs(wrest)
+    rl = host(got[1]).reshape(-1)
+    assert (np.abs(rl - wr) <= 4 * LOG_SUM + 1e-5 * np.abs(wr) + off).all(), f"{rl} {wr}"
+    gr = topk_ref.values(host(got[2]).reshape(B, V))
+    step = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    tiny = 2.0 ** -133 if dtype == "bf16" else 2.0 ** -149
+    lim = ((step + 2.0 ** -15) * np.abs(wg) + (40 * LOG_SUM * np.maximum(1.0, np.abs(wr)) + 2 * off)[:, None]
+           * qof(s, tau) / tau + tiny + 2.0 ** -126 * np.abs(wg).max(-1, keepdims=True))
+    err = np.abs(gr - wg)
+    assert (err <= lim).all(), f"{(err > lim).sum()}: {gr[err > lim][:3]} {wg[err > lim][:3]}"

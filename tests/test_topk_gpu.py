@@ -176,3 +176,67 @@ def test_other_stream_and_graph(osd):
         torch.cuda.synchronize()
         check(out, xs[i], k, T, us[i], f"replay {i}")
         assert all(torch.equal(a, b) for a, b in zip(out, eager))
+
+
+# The others' mass where it lies far below the largest logit, or T is small: terms up
+# to 100 octaves above a thread's reference (the kernel's own limit), each off by
+# (2 * 100 ln 2 + 2) 2^-24 at most.
+FAR_SUM = (200 * np.log(2) + 2) * 2.0 ** -24
+
+
+def check_far(got, x, k, T, label):
+    want = topk_ref.topk(x, k, T)
+    ids, _, rest, _ = (host(t) for t in got)
+    assert np.array_equal(ids, want["ids"]), f"{label}: ids"
+    bad = np.isneginf(rest) != np.isneginf(want["rest"])
+    assert not bad.any(), f"{label}: rest {rest[bad]} {want['rest'][bad]}"
+    some = ~np.isneginf(rest)
+    err = np.abs(rest[some] - want["rest"][some])
+    lim = FAR_SUM + 2.0 ** -24 * np.abs(want["rest"][some])
+    assert (err <= lim).all(), f"{label}: rest {rest[some][err > lim][:3]} {want['rest'][some][err > lim][:3]}"
+
+
+FAR_SHAPES = [(100, 64, "f32"), (1000, 64, "bf16"), (1000, 1, "f32"), (4099, 200, "bf16"), (32000, 64, "bf16"),
+              (32003, 256, "f32"), (70001, 100, "bf16"), (128256, 128, "bf16")]
+
+
+@pytest.mark.parametrize("gap", [60.0, 80.0, 88.0, 95.0, 110.0, 200.0, 600.0, 1.0e4])
+@pytest.mark.parametrize("V,k,dtype", FAR_SHAPES)
+def test_mass_far_below_the_record(osd, V, k, dtype, gap):
+    """Peaks of one token, half the record and all of it above the others; one
+    row with nothing outside."""
+    x = rows("normal", 4, V, 71)
+    g = np.random.default_rng(72)
+    for n, peaks in enumerate((1, max(1, k // 2), k)):
+        x[n, g.choice(V, peaks, replace=False)] += np.float32(gap)
+    keep = g.choice(V, max(1, k // 2), replace=False)
+    only = np.full(V, -np.inf, np.float32)
+    only[keep] = x[3, keep]
+    x[3] = only
+    x = as_dtype(x, dtype)
+    check_far(osd.osd_topk(to_device(x), k, 1.0), x, k, 1.0, f"V={V} k={k} {dtype} gap={gap}")
+
+
+@pytest.mark.parametrize("T", [0.25, 0.1, 0.05, 0.03125, 0.02, 0.001])
+@pytest.mark.parametrize("V,k,dtype", FAR_SHAPES)
+def test_mass_at_small_temperatures(osd, V, k, dtype, T):
+    T = float(np.float32(T))
+    x = as_dtype(rows("normal", 5, V, 73), dtype)
+    check_far(osd.osd_topk(to_device(x), k, T), x, k, T, f"V={V} k={k} {dtype} T={T}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,N", [(1003, 3), (32000, 3), (32000, 600)])
+def test_ties_far_below_the_record(osd, V, N, dtype):
+    """The record's last slots and the mass outside of one value, far below the
+    first slots: ids decide which of them are outside."""
+    k = 40
+    x = np.full((3, V), -300.0, np.float32)
+    x[0, 7] = 1.0
+    x[1, [3, V - 1]] = 2.0
+    x[2, V // 2] = 0.5
+    x[2, : V // 3] = -301.0
+    x = as_dtype(x, dtype)
+    got = osd.osd_topk(to_device(np.concatenate([x] * (N // 3))), k, 1.0)
+    check_far([None if t is None else t[:3].contiguous() for t in got], x, k, 1.0, f"V={V} {dtype}")
+    assert all((host(t)[:3] == host(t)[-3:]).all() for t in got[:3])

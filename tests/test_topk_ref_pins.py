@@ -213,3 +213,17 @@ def test_gradient_of_others_far_below_is_autograd(kind, gap):
     assert abs(rl[0] - D.item()) < 1e-12 * max(1.0, D.item())
     assert np.abs(g[0] - x.grad.numpy()).max() < 1e-12
     assert abs(g.sum()) < 1e-12
+
+
+@pytest.mark.parametrize("T", [1.0, 0.02, 0.001])
+def test_rest_far_below_the_record(T):
+    """Against torch's logsumexp; where exp of the difference is 0 in fp64 too."""
+    import torch
+    x = rows("normal", 5, 300, 40)
+    x[1, 7] += 900.0
+    x[2, :10] += 5.0e3
+    rec = topk_ref.topk(x, 10, T)
+    for n in range(5):
+        out = np.delete(x[n].astype(np.float64), rec["ids"][n])
+        want = torch.logsumexp(torch.tensor((out - rec["top"][n, 0]) / T), 0).item()
+        assert abs(rec["rest"][n] - want) < 1e-12 * max(1.0, abs(want))
