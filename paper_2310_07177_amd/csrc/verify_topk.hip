@@ -273,7 +273,7 @@ __device__ inline void cell_sum(const VerifyTopkArgs& a, chunk_t (&c)[kPer], int
 struct VerifyTopkLds {
     union {
         int32_t table[kNW][kTable];            // ids seen, by wave
-        uint16_t slot[512 * 8];                // 1 + the slot of each token of one cell, or 0
+        uint16_t slot[kSlotPad + 512 * 8 + 8];  // 1 + the slot of each token of one cell, or 0
     };
     double row_sum[OSD_MAX_K + 1];             // target rows: normaliser
     float row_top[OSD_MAX_K + 1];              //              largest logit, NaN or -inf if unusable
@@ -636,6 +636,7 @@ __device__ __forceinline__ void decide(const VerifyTopkArgs& a, int64_t b, int k
         }
     }
     if (tid < kMaxCells) s.fixed[tid] = 0;
+    static_assert((kSlotPad + kTokens + 8) * sizeof(s.slot[0]) <= sizeof(s.slot), "a cell's tokens and the padding");
     for (int i = tid; i < (kSlotPad + kTokens + 8) / 2; i += kW) reinterpret_cast<uint32_t*>(s.slot)[i] = 0u;
     __syncthreads();
     // The first position that is not accepted.  Where the sums of v_exp_f32 do not tell,
