@@ -263,6 +263,7 @@ __global__ __launch_bounds__((NR + 1) * kWave, 4) void distill_topk_kernel(Disti
 #pragma unroll
             for (int j = 0; j < kSlots; ++j)
                 if (id[j] >= 0) atomicAnd(&s_flag[word(id[j])], ~bit(id[j]));
+            wave_lds_order();  // (before the next row's are set)
             if (!grow) continue;
             __syncthreads();  // 4: the others' gradient is written
 #pragma unroll

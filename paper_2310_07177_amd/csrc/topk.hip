@@ -296,12 +296,15 @@ __global__ __launch_bounds__(W, W == 1024 ? 4 : W == 512 ? 6 : 5) void topk_row_
             const uint32_t base = most >> 16;
             uint32_t* bins = &s.bin[lane * 4];
             bins[0] = bins[1] = bins[2] = bins[3] = 0u;
+            wave_lds_order();
 #pragma unroll
             for (int j = 0; j < kKeys; ++j) {
                 const uint32_t at = base - (s.key[j * kWave + lane] >> 16);
                 if (at < uint32_t(kBins)) atomicAdd(&s.bin[at], 1u);
             }
+            wave_lds_order();
             const uint32_t b0 = bins[0], b1 = bins[1], b2 = bins[2], b3 = bins[3];
+            wave_lds_order();
             const uint32_t upto = wave_scan_count(b0 + b1 + b2 + b3) + before;
             const uint64_t full = __ballot(upto >= uint32_t(k));
             if (full) {
@@ -357,6 +360,7 @@ __global__ __launch_bounds__(W, W == 1024 ? 4 : W == 512 ? 6 : 5) void topk_row_
             int at = int(upto - mine) - first;
             for (uint32_t f = flags; f; f &= f - 1, ++at)
                 if (uint32_t(at) < uint32_t(kQueue)) queue[at] = (__builtin_ctz(f) * G) * W + tid;  // its first chunk
+            wave_lds_order();
             const int elements = min(total - first, kQueue) * G * EPC;
             constexpr int kStep = 4;  // elements a lane requests at once
 #pragma unroll 1
@@ -385,6 +389,7 @@ __global__ __launch_bounds__(W, W == 1024 ? 4 : W == 512 ? 6 : 5) void topk_row_
                     if (a.rest && !in) S += double(weight(x[j]));
                 }
             }
+            wave_lds_order();
         }
         __syncthreads();
         nc = int(uniform(s.ncand));

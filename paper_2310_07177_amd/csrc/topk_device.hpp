@@ -46,6 +46,14 @@ __device__ inline double log2_f64(double x) {
     return double(__builtin_amdgcn_frexp_exp(x)) + y + (m * exp2_f64(-1.0 - y) * 2.0 - 1.0) * 1.4426950408889634074;
 }
 
+// Between LDS accesses of one lane and those of other lanes of its wave to the same
+// words: the compiler keeps their order (the wave's own LDS accesses run in order; no
+// instruction).
+__device__ inline void wave_lds_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // The larger of two floats, NaN if either is one.
 __device__ inline float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 

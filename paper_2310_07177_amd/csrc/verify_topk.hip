@@ -358,6 +358,7 @@ __device__ inline void post_record(const VerifyTopkArgs& a, int64_t b, int i, in
     // An id twice: its place in the table is taken by an equal one.
 #pragma unroll
     for (int t = 0; t < kTable / kWave; ++t) table[t * kWave + lane] = -1;
+    wave_lds_order();
 #pragma unroll
     for (int j = 0; j < kSlots; ++j) {
         if (id[j] < 0) continue;
