@@ -808,7 +808,6 @@ int osd_verify_topk(const void* target_logits, const int32_t* draft_ids, const v
     L.reject_mask = reject_mask;
     L.rows = static_cast<osd::VerifyTopkRow*>(workspace);
     L.stream = static_cast<hipStream_t>(stream);
-    L.cus = device_cus(L.stream);
     return osd::launch_verify_topk(L) == hipSuccess ? OSD_OK : OSD_ERR_DEVICE;
 }
 

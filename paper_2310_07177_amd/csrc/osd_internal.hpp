@@ -322,7 +322,6 @@ struct VerifyTopkLaunch {
     int32_t* out_tokens;
     uint8_t* reject_mask;
     VerifyTopkRow* rows;  // [B*(K+1)]
-    int cus;
     hipStream_t stream;
 };
 hipError_t launch_verify_topk(const VerifyTopkLaunch& L);

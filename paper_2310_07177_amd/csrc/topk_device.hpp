@@ -73,26 +73,6 @@ __device__ inline uint32_t order_key(float x) { return x == x ? float_key(x + 0.
 constexpr uint32_t kKeyNegInf = 0x007FFFFFu;
 constexpr uint32_t kKeyPosInf = 0xFF800000u;
 
-// The elements of chunks, in one sweep over a held row.  For bf16 the shift and
-// the mask that unpack a pair are opaque, anew in each sweep: the unpacked values
-// of one sweep are then not kept for the next, which would double the registers
-// of a row.  (An opaque copy of the chunks themselves did that in places.)
-template <typename Fmt>
-struct Sweep {
-    uint32_t shift = 16u, mask = 0xFFFF0000u;
-    __device__ __forceinline__ Sweep() {
-        if constexpr (Fmt::kPerChunk == 8) asm volatile("" : "+s"(shift), "+s"(mask));
-    }
-    __device__ __forceinline__ float get(const chunk_t& c, int e) const {
-        if constexpr (Fmt::kPerChunk == 8) {
-            const uint32_t w = (e >> 1) == 0 ? c.x : (e >> 1) == 1 ? c.y : (e >> 1) == 2 ? c.z : c.w;
-            return __uint_as_float((e & 1) ? w & mask : w << shift);
-        } else {
-            return Fmt::get(c, e);
-        }
-    }
-};
-
 // Stores chunk ch of the row at the descriptor's base (whole: it is known to have no
 // padding).
 template <typename Fmt>
@@ -163,10 +143,6 @@ struct HeldRow {
 #pragma unroll
         for (int r = 0; r < CPT; ++r)
             if (r >= MINR - 1 && r == rounds - 1) c[r] = pad_lead<Fmt>(c[r], cut.lead(r * W + tid));
-    }
-    // The token of element e of this thread's chunk of round r.
-    __device__ int token(int r, int e, int tid) const {
-        return cut.token((r * W + tid) * Fmt::kPerChunk + e);
     }
     __device__ __forceinline__ void store(rsrc_t rs, int r, const chunk_t& c, int tid) const {
         store_chunk(cut, rs, r * W + tid, r < rounds - 1, c);
