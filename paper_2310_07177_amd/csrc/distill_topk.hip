@@ -551,10 +551,20 @@ hipError_t launch_split(const DistillTopkLaunch& L, const DistillTopkArgs& a, in
 template <typename Fmt, int NR, int CPT, int MINR>
 hipError_t launch_tile(const DistillTopkLaunch& L, DistillTopkArgs a) {
     constexpr int W = (NR + 1) * kWave;
-    // As many workgroups as are resident at once take the rows in turn.  Where a mask
-    // leaves some of them more to do than others, eight times as many even that out: 16384
-    // rows of 32000 bf16 logits, 4 in 10 unmasked, 355 us to 328 (all: 497 to 521), 2048
-    // of 128256 223 to 183; not of 4000, 110 to 131.
+    // Twice as many workgroups as are resident at once (1024 threads a CU: the record wave's
+    // fp64 terms take 108 to 128 registers, whatever the row waves hold) take the rows in
+    // turn.  Where a mask leaves some of them more to do than others, eight times as many
+    // even that out for long rows.  16384 bf16 rows (of 64000: 8192) with 1, 4, 8 in 10
+    // unmasked and all, us, without that and with it:
+    //   1000   54  78 108 101   122 124 130 127
+    //   4000   63 107 148 138   122 131 151 149
+    //   8000   95 139 191 186   127 139 189 191
+    //   16000 155 231 323 335   143 231 326 358
+    //   18500 203 244 359 369   177 244 353 401
+    //   24000 217 282 390 409   201 266 384 446
+    //   32000 280 355 472 492   266 317 445 513
+    //   64000 265 412 555 544   233 375 538 568
+    // Of 2048 rows it is the same.  (The tile changes at 17920.)
     const int each = a.mask && NR * CPT >= 70 ? 8 : 1;
     int g = L.cus * (2048 / W) * each;
     if (g > kMaxDistillTopkGroups) g = kMaxDistillTopkGroups;

@@ -18,8 +18,8 @@ namespace osd {
 // 2^n by ldexp.  fp64 vector instructions run at the rate of unpacked fp32 ones
 // on this part, so this costs about twice what v_exp_f32 with its fp64 sum does,
 // and a draw decided on such masses agrees with exact arithmetic to about 1e-12 of
-// the row's mass: fp32 exponentials leave 1e-8, which over a flat row of 32000
-// tokens moves one draw in a thousand.
+// the row's mass: fp32 exponentials leave up to 1e-7, which over a flat row of 32000
+// tokens moves one draw in a hundred.
 __device__ inline double exp2_f64(double x) {
     constexpr double kMagic = 6755399441055744.0;  // 1.5 * 2^52
     x = __builtin_fmax(x, -1100.0);
