@@ -27,16 +27,18 @@
 //   E = (1 - u) sum_{j <= t} p_j e_j - u sum_{j > t} p_j e_j,
 // e_j = d_j - D where the token keeps mass and d_j where the record takes all of it (its
 // exact exponential is subtracted).  With A the mass of p up to the token, collecting d_j,
-//   |E| <= kTerm (A (1 - u) + (1 - A) u + A (1 - A) + 1.5 c),
+//   |E| <= kTerm (A (1 - u) + (1 - A) u + A (1 - A) + 2 c),
 // where c is the mass of the cell that holds the token: its tokens are summed anew, with
-// other errors (at most 1.2e-7) than they have in the cell's sum (1.5e-7 in bf16).
+// errors of their own (1.2e-7, and 6e-8 by rounding what the record leaves).
 // A draw whose point lies within that of an edge of its token's interval is decided again
 // on fp64 exponentials of the whole row (1e-12), and so is a test where u q / p and 1
 // differ by less than kNearRatio (the normaliser is off by kTerm).  That holds up its
-// sequence by 25 + 6 us at V = 128256, where it is one draw in fifty (B = 256, K = 8, bf16:
-// 120 us a call, 95 if none were), and by some 8 us at V = 32128, one in eighty
-// (B = 64: 19.3 us, 21.5 with one).  fp64 exponentials throughout took three times as long for
-// the cells (20.6 us of the latter for them alone), reduced arguments in all cells 142 us.
+// sequence by 25 + 6 us at V = 128256, one draw in seventy (B = 256, K = 8, bf16: 120 us a
+// call, 97 if none were), and by 7 + 4 us at V = 32128, one in two hundred (B = 64: 19.3 us a
+// call, some 28 with one).  fp64 exponentials throughout took three times as long for the
+// cells (20.6 us of the latter for them alone), reduced arguments in all cells 142 us; the
+// record's tokens taken away by the sums' own exponentials, and a bound that gains by
+// it, left four in five of these draws and cost 0.5 us of the 19.3.
 #include "osd.h"
 #include "osd_device.hpp"
 #include "osd_internal.hpp"
@@ -154,18 +156,12 @@ __device__ __forceinline__ double pair_sum(const float (&e)[EPC]) {
     return s;
 }
 
-// The chunk with its first `lead` elements replaced by the lowest finite value.
-template <typename Fmt>
+// The chunk with its first `lead` elements replaced by the lowest finite bf16 value.
 __device__ inline chunk_t lowest_lead(const chunk_t& c, int lead) {
-    if constexpr (Fmt::kPerChunk == 8) {
-        const auto w = [lead](uint32_t x, int e) {
-            return lead > e + 1 ? 0xFF7FFF7Fu : (lead > e ? (x & 0xFFFF0000u) | 0xFF7Fu : x);
-        };
-        return chunk_t{w(c.x, 0), w(c.y, 2), w(c.z, 4), w(c.w, 6)};
-    } else {
-        return chunk_t{lead > 0 ? 0xFF7FFFFFu : c.x, lead > 1 ? 0xFF7FFFFFu : c.y, lead > 2 ? 0xFF7FFFFFu : c.z,
-                       lead > 3 ? 0xFF7FFFFFu : c.w};
-    }
+    const auto w = [lead](uint32_t x, int e) {
+        return lead > e + 1 ? 0xFF7FFF7Fu : (lead > e ? (x & 0xFFFF0000u) | 0xFF7Fu : x);
+    };
+    return chunk_t{w(c.x, 0), w(c.y, 2), w(c.z, 4), w(c.w, 6)};
 }
 
 // One cell by one wave: its largest logit m, and the sum S of exponentials (0 where
@@ -180,9 +176,13 @@ __device__ inline void cell_sum(const VerifyTopkArgs& a, chunk_t (&c)[kPer], int
     // (bf16: padding of the lowest finite value serves the path that is taken most.)
     if (end) {
 #pragma unroll
-        for (int r = 0; r < kPer; ++r)
-            c[r] = EPC == 8 ? lowest_lead<Fmt>(c[r], cut.lead(ch0 + r * kWave))
-                            : pad_lead<Fmt>(c[r], cut.lead(ch0 + r * kWave));
+        for (int r = 0; r < kPer; ++r) {
+            const int lead = cut.lead(ch0 + r * kWave);
+            if constexpr (EPC == 8)
+                c[r] = lowest_lead(c[r], lead);
+            else
+                c[r] = pad_lead<Fmt>(c[r], lead);
+        }
     }
     const auto largest = [&] {
         float x = kNegInf;
@@ -216,7 +216,7 @@ __device__ inline void cell_sum(const VerifyTopkArgs& a, chunk_t (&c)[kPer], int
         const float h = m * a.hi16;
         if (h >= -60.0f && h <= 100.0f) {
 #pragma unroll 1
-            while (true) {
+            for (int pass = 0; pass < 2; ++pass) {
                 float X = 0.0f;
                 S = 0.0;
 #pragma unroll
@@ -233,11 +233,14 @@ __device__ inline void cell_sum(const VerifyTopkArgs& a, chunk_t (&c)[kPer], int
                 }
                 S = wave_sum(S);
                 mean = wave_sum_f32(X) * __builtin_amdgcn_rcpf(float(S));
-                if (mean == mean) return;
-                // A -inf (times 0): again with the lowest finite value in its place.
+                if (is_finite(mean)) return;
+                // A -inf (times 0): again with the lowest finite value in its place.  (Or X
+                // overflows, with logits of 1e10 at such temperatures: the other ways.)
 #pragma unroll
                 for (int r = 0; r < kPer; ++r) c[r] = finite_pairs(c[r]);
             }
+            S = 0.0;
+            mean = __builtin_nanf("");
         }
         if (end) {
 #pragma unroll
@@ -410,11 +413,12 @@ __device__ __forceinline__ int find_token(const VerifyTopkArgs& a, const Draw& d
     // The first cell that may hold the point (the sums of the cells and of their
     // elements differ by rounding), then upwards; down from there only if rounding
     // put the point past the last token.
+    sure = false;
+    if (d.lives == 0) return -1;  // (no cell to read)
     const uint64_t from = __ballot((d.lives >> lane & 1) && d.cum > d.point - 1e-14);
     int cell = from ? __builtin_ctzll(from) : 63 - __builtin_clzll(d.lives);
     const int start = cell;
     bool up = true;
-    sure = false;
     while (true) {
         const int ch0 = cell * kCell + tid * kEach;
         chunk_t c[kEach];
@@ -511,7 +515,7 @@ __device__ __forceinline__ int find_token(const VerifyTopkArgs& a, const Draw& d
             const double from = cell > 0 ? readlane_f64(d.before, cell - 1) : 0.0, to = readlane_f64(d.before, cell);
             const double A = fmin(fmax(1.0 - d.u, from), to);
             const double unsure =
-                kTerm * (A * (1.0 - d.u) + (1.0 - A) * d.u + A * (1.0 - A) + 1.5 * (to - from)) + 1e-11;
+                kTerm * (A * (1.0 - d.u) + (1.0 - A) * d.u + A * (1.0 - A) + 2.0 * (to - from)) + 1e-11;
             sure = s.high - d.point > unsure && d.point - s.low > unsure;
             return s.token;
         }

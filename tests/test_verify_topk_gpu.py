@@ -386,3 +386,25 @@ def test_residual_of_one_token_with_little_mass(osd, T):
     assert sure.sum() > n // 2 and (wa[sure] == 0).all() and (wt[sure, 0] == left[sure]).all()
     bad = sure & ((acc != wa) | (toks[:, 0] != wt[:, 0]))
     assert not bad.any(), f"{bad.sum()}: {acc[bad]} {toks[bad, 0]} for {wt[bad, 0]}"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1e6, 1e9, 1e20])
+def test_large_logits_at_large_temperatures(osd, T, dtype):
+    """Logits whose products with their exponentials leave fp32 although the scaled
+    logits are ordinary ones (60 to 99 bits), with and without masked tokens."""
+    T = float(np.float32(T))
+    B, K, V, k = 8, 2, 5001, 8
+    g = np.random.default_rng(9)
+    t = (g.uniform(-99, 99, (B, K + 1, V)) * T * np.log(2)).astype(np.float32)
+    t[:4][g.random((4, K + 1, V)) < 0.3] = -np.inf
+    t[2:6, :, 3] = np.float32(98.5 * T * np.log(2))
+    d = as_dtype(t[:, :K].reshape(B * K, V).copy(), dtype)
+    t = as_dtype(t, dtype)
+    rec = topk_ref.topk(d, k, T, uniforms(B * K, 1))
+    top = np.take_along_axis(d, rec["ids"].astype(np.int64), 1)
+    x = dict(t=t, ids=rec["ids"].reshape(B, K, k), top=top.reshape(B, K, k), y=rec["tokens"].reshape(B, K),
+             ua=uniforms((B, K), 2), ur=uniforms(B, 3))
+    check(call(osd, x, T), x, T, None, f"T={T} {dtype}")
+    x["ua"][:] = 0.0
+    check(call(osd, x, T), x, T, None, f"bonus T={T} {dtype}")
