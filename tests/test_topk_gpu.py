@@ -240,3 +240,15 @@ def test_ties_far_below_the_record(osd, V, N, dtype):
     got = osd.osd_topk(to_device(np.concatenate([x] * (N // 3))), k, 1.0)
     check_far([None if t is None else t[:3].contiguous() for t in got], x, k, 1.0, f"V={V} {dtype}")
     assert all((host(t)[:3] == host(t)[-3:]).all() for t in got[:3])
+
+
+@pytest.mark.parametrize("N,V,k,dtype", [(4, 2, 1, "bf16"), (4, 5, 2, "bf16"), (4, 3, 2, "f32"), (4, 9, 4, "bf16"),
+                                         (4, 257, 256, "f32"), (300, 128256, 64, "bf16"), (300, 65536, 256, "f32")])
+def test_mass_far_below_in_short_rows_and_many_long_ones(osd, N, V, k, dtype):
+    x = rows("normal", 4, V, 81)
+    for n, gap in enumerate((90.0, 700.0, 3.0e4)):
+        x[n, np.argsort(-x[n])[:k]] += np.float32(gap)
+    x = as_dtype(x, dtype)
+    got = osd.osd_topk(to_device(np.concatenate([x] * (N // 4))), k, 1.0)
+    check_far([None if t is None else t[:4].contiguous() for t in got], x, k, 1.0, f"V={V} k={k} {dtype}")
+    assert all((host(t)[:4] == host(t)[-4:]).all() for t in got[:3])

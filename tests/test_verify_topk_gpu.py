@@ -408,3 +408,51 @@ def test_large_logits_at_large_temperatures(osd, T, dtype):
     check(call(osd, x, T), x, T, None, f"T={T} {dtype}")
     x["ua"][:] = 0.0
     check(call(osd, x, T), x, T, None, f"bonus T={T} {dtype}")
+
+
+@pytest.mark.parametrize("kind", ["head", "pattern"])
+@pytest.mark.parametrize("V,gap", [(100003, 11.5), (131072, 11.75)])
+def test_draws_next_to_edges_of_the_longest_bf16_rows(osd, V, gap, kind):
+    test_draws_next_to_edges_of_flat_rows(osd, V, gap, kind, 1.0, "bf16")
+    if kind == "head":
+        test_acceptance_next_to_the_ratio(osd, V, gap, 1.0, "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K", [2, 5, 16])
+def test_every_position_next_to_its_ratio(osd, K, dtype):
+    """Uniforms next to p(y) / q(y) at all positions: one after another is decided
+    in fp64, the first that fails ends it; ragged lengths."""
+    V, gap, T, B = 2048, 6.84375, 1.0, 40
+    t = flat_rows(V, gap, dtype, V, "head")
+    z = topk_ref.values(t)
+    which = (np.arange(B * K).reshape(B, K) + np.arange(B)[:, None]) % 8
+    p = np.array([topk_ref.softmax(r / T).max() for r in z])
+    y = np.array([int(np.argmax(r)) for r in z], np.int32)[which]
+    ua = p[which].astype(np.float32)
+    for b in range(B):
+        for i in range(K):  # accepted up to position b % (K + 1)
+            for _ in range(1 + (b + i) % 3):
+                ua[b, i] = np.nextafter(ua[b, i], np.float32(0 if i < b % (K + 1) else 1), dtype=np.float32)
+    rows_t = np.concatenate([t[which], t[which[:, :1]]], 1)
+    x = dict(t=rows_t, ids=y.reshape(B, K, 1), top=np.zeros((B, K, 1), t.dtype), y=y, ua=ua, ur=uniforms(B, 5))
+    check(call(osd, x, T), x, T, None, f"K={K} {dtype}")
+    dl = (np.arange(B) % K + 1).astype(np.int32)
+    check(call(osd, x, T, dl), x, T, dl, f"ragged K={K} {dtype}")
+    acc = host(call(osd, x, T)[0])
+    assert set(acc.tolist()) == set(range(K + 1))
+
+
+def test_masked_rows_and_other_sizes_on_one_workspace(osd):
+    """Calls of several K, V and types in turn through the binding's workspace: what
+    one leaves there does not reach the next."""
+    import torch
+    calls = []
+    for n, (B, K, V, k, dtype, kind) in enumerate([(6, 16, 3001, 40, "bf16", "masked"), (3, 1, 70001, 7, "bf16", "normal"),
+                                                   (40, 5, 2048, 256, "f32", "equal"), (2, 3, 5, 2, "bf16", "normal"),
+                                                   (9, 2, 40003, 33, "f32", "masked_lowest")]):
+        x = inputs(B, K, V, k, dtype, 1.0, 400 + n, kind=kind)
+        calls.append((x, call(osd, x, 1.0)))
+        check(calls[-1][1], x, 1.0, None, f"{kind} V={V}")
+    for x, first in calls[::-1] + calls:
+        assert all(torch.equal(a, b) for a, b in zip(call(osd, x, 1.0), first))
