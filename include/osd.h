@@ -480,6 +480,135 @@ int osd_verify_topk(const void* target_logits, const int32_t* draft_ids, const v
                     void* stream);
 
 /*
+ * The paged cache of keys and values, and the attention that reads it: what a
+ * step of speculative decoding runs the target over its drafted tokens with.
+ * The candidate tree of osd_verify_tree (or the chain of osd_verify) goes
+ * through osd_cache_append and osd_tree_attention in every layer; once its
+ * tokens are verified, osd_cache_keep moves the accepted path of every layer to
+ * where the context ends.
+ *
+ * The cache of one layer is two arrays of pages of page_size tokens,
+ * [pages, kv_heads, page_size, head_dim] in `dtype`, with page_stride elements
+ * between pages (so that K and V may share one allocation).  A sequence's
+ * tokens lie on the pages that its row of page_table names: token j on page
+ * page_table[b, j / page_size], slot j % page_size.  Arguments shared by the
+ * three operators:
+ *
+ * k_cache, v_cache   the caches
+ * page_stride        elements between pages, >= kv_heads * page_size * head_dim
+ * pages, page_size   pages of the cache, tokens of a page (any number)
+ * kv_heads, head_dim head_dim a multiple of 8, at most OSD_MAX_HEAD_DIM
+ * page_table         [B, table_len] int32; entries behind a sequence's last
+ *                    token are not looked at
+ * seq_len            [B] int32: tokens of the context, c_b; -1: no sequence
+ *                    (a padded batch)
+ * N                  new tokens of a sequence: node n of sequence b is token
+ *                    c_b + n of the cache
+ * parent             [B, N] int32 as in osd_verify_tree (node 0 is the root,
+ *                    0 <= parent[n] < n), or NULL: a chain, every node's parent
+ *                    the one before it.  N <= OSD_MAX_TREE_NODES with a tree
+ * new_len            [B] int32 or NULL: nodes that sequence b has, n_b <= N
+ *                    (NULL: N); the nodes behind are padding
+ *
+ * Base addresses and strides of all arrays but the int32 ones are multiples of
+ * 16 bytes; a table covers at most 2^31 - 1 tokens (otherwise
+ * OSD_ERR_INVALID_ARG).  Unsupported head sizes and batches above
+ * OSD_MAX_CACHE_BATCH give OSD_ERR_UNSUPPORTED.  Pages that several sequences
+ * name are read correctly; a page that a call writes must belong to one
+ * sequence alone.  Outputs must not overlap inputs, except as said.
+ */
+#define OSD_MAX_HEAD_DIM 256
+#define OSD_MAX_CACHE_BATCH 4096
+
+typedef enum { OSD_ROTATE_HALVES = 0, OSD_ROTATE_PAIRS = 1 } osd_rotation;
+
+/*
+ * osd_cache_append -- new tokens' keys and values into the pages behind the
+ * context, rotated by their positions on the way, and their queries rotated
+ * along with them.
+ *
+ * A token's position is c_b + its depth (a tree: the number of its ancestors; a
+ * chain: n), so that an accepted path needs no new rotation when it moves.  The
+ * first rotary_dim values of a head are taken as pairs (x, y), element i with
+ * element i + rotary_dim / 2 (OSD_ROTATE_HALVES) or elements 2i and 2i + 1
+ * (OSD_ROTATE_PAIRS), and become (x cos - y sin, y cos + x sin); the others, and
+ * all of V, are copied.
+ *
+ * q             [B, N, q_heads, head_dim], q_stride elements between tokens
+ *               (token (b, n) at (b * N + n) * q_stride); NULL: keys and values
+ *               alone
+ * q_out         out, as q with q_out_stride between tokens; q itself with the
+ *               same stride, or no part of it; NULL iff q is
+ * k, v          [B, N, kv_heads, head_dim], k_stride and v_stride between tokens
+ * rotation      [rotation_rows, rotary_dim] fp32: for each position the cosines
+ *               of its rotary_dim / 2 angles, then the sines; NULL: no rotation
+ * rotary_dim    even, 2 .. head_dim (ignored without rotation)
+ *
+ * Nothing is written for padding but zeros in q_out.  A token that has no place
+ * (its page outside the cache or the table) or no position (beyond rotation_rows,
+ * an invalid tree), and all of a sequence whose n_b is outside 0 .. N, is not
+ * written to the cache; its q_out is NaN.
+ */
+int osd_cache_append(void* k_cache, void* v_cache, int64_t page_stride, int pages, int page_size, int kv_heads,
+                     int head_dim, int dtype, const int32_t* page_table, int table_len, const int32_t* seq_len,
+                     const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, int q_heads,
+                     const void* k, int64_t k_stride, const void* v, int64_t v_stride, int B, int N,
+                     const int32_t* parent, const int32_t* new_len, const float* rotation, int rotation_rows,
+                     int rotary_dim, int rotation_style, void* stream);
+
+/*
+ * osd_tree_attention -- attention of the drafted tokens: node n sees the context,
+ * its ancestors and itself (all of them already in the cache),
+ *   out = sum_j softmax_j(scale q . k_j) v_j,   j < c_b or j = c_b + an ancestor of n or n.
+ * N = 1 is the decoding of single tokens, parent = NULL that of chains.
+ *
+ * q             [B, N, q_heads, head_dim], q_stride elements between tokens;
+ *               query head h reads kv head h / (q_heads / kv_heads)
+ * scale         finite
+ * out           out [B, N, q_heads, head_dim]
+ * workspace     osd_tree_attention_workspace_bytes(...) zero-initialised bytes
+ *               for this operator alone (counters among them are left zero; the
+ *               rest keeps scratch that later calls need not find cleared, at any
+ *               sizes)
+ *
+ * N <= OSD_MAX_TREE_NODES.  Padding, and sequences of length -1, get zeros.  A
+ * sequence that is invalid (n_b outside 0 .. N, tokens beyond its table, a page
+ * outside the cache, an invalid tree) gets NaN.  What the cache holds in tokens
+ * that a node does not see (NaN, too) does not reach its output.  Scores, softmax
+ * and sums are fp32; probabilities are rounded to bf16 for the product with bf16
+ * values.  Work is divided over the GPU by the lengths in device memory, so a
+ * captured call serves any lengths; how it is divided, and with it the last bits,
+ * depends on all of the batch.  Equal calls give equal bits.
+ */
+size_t osd_tree_attention_workspace_bytes(int B, int N, int q_heads, int kv_heads, int head_dim);
+int osd_tree_attention(const void* q, int64_t q_stride, int q_heads, const void* k_cache, const void* v_cache,
+                       int64_t page_stride, int pages, int page_size, int kv_heads, int head_dim, int dtype,
+                       const int32_t* page_table, int table_len, const int32_t* seq_len, int B, int N,
+                       const int32_t* parent, const int32_t* new_len, float scale, void* out, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/*
+ * osd_cache_keep -- the accepted path's keys and values move to where the context
+ * ends: token c_b + path_nodes[b, i] to token c_b + 1 + i, i < accepted_len[b], in
+ * the caches of all layers (the root, token c_b, is in place).  A chain needs no
+ * move.
+ *
+ * layers, layer_stride  the caches are [layers, pages, ...], layer_stride elements
+ *                       between layers
+ * path_nodes            [B, N] int32 and
+ * accepted_len          [B] int32: as osd_verify_tree returns them
+ * new_seq_len           out [B] int32: c_b + 1 + accepted_len[b]; not seq_len itself
+ *
+ * Nothing moves, and new_seq_len is c_b, where accepted_len is outside 0 .. N - 1
+ * (-1: an invalid tree), the path is no ascending list of nodes in 1 .. N - 1, or
+ * the root or a node on the path has no place.
+ */
+int osd_cache_keep(void* k_cache, void* v_cache, int64_t page_stride, int pages, int page_size, int kv_heads,
+                   int head_dim, int dtype, int layers, int64_t layer_stride, const int32_t* page_table,
+                   int table_len, const int32_t* seq_len, int B, int N, const int32_t* path_nodes,
+                   const int32_t* accepted_len, int32_t* new_seq_len, void* stream);
+
+/*
  * Vocabulary-sharded verification.  When the target and draft LM heads are
  * split by vocabulary over G ranks (tensor parallelism), rank g holds columns
  * [v_begin_g, v_begin_g + V_g) of every logit row, and no rank sees a whole

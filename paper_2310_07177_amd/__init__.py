@@ -1,5 +1,6 @@
 """MI355X (gfx950) library for the vocabulary-wide logits path of online
-speculative decoding (Liu et al., arXiv:2310.07177).
+speculative decoding (Liu et al., arXiv:2310.07177), and for the paged cache and
+the tree attention that the drafted tokens go through before it.
 
     osd_verify             speculative-sampling verification (Appendix A.1, Eq. 5)
     osd_verify_noalloc     the same without a workspace (library-held scratch)
@@ -17,6 +18,12 @@ speculative decoding (Liu et al., arXiv:2310.07177).
     osd_distill_topk_loss_grad  distillation loss and gradient against teacher
                            records
     osd_verify_topk        verification of proposals drawn from draft records
+    osd_cache_append       drafted tokens' keys and values into a paged cache,
+                           rotated by their positions, the queries along with them
+    osd_tree_attention     attention of a tree (or chain) of drafted tokens over
+                           the cache
+    osd_cache_keep         the accepted path's rows moved to where the context
+                           ends, in all layers
     osd_shard_verify_*     verification with the vocabulary split over ranks
                            (stats, mass, draw: one call per phase per rank)
 
@@ -24,7 +31,8 @@ The computation lives in libosd.so (C ABI: include/osd.h); this package is
 argument marshalling over it.  Build with ``python -m paper_2310_07177_amd.build``.
 """
 from .binding import (OSD_BF16, OSD_F32, OSD_FKL, OSD_JSD, OSD_MAX_K, OSD_MAX_TOPK, OSD_RKL,  # noqa: F401
-                      OsdError, lib, osd_distill_loss_grad, osd_distill_topk_loss_grad, osd_max_vocab, osd_sample,
-                      osd_shard_verify_draw, osd_shard_verify_mass, osd_shard_verify_stats, osd_topk, osd_verify,
+                      OsdError, lib, osd_cache_append, osd_cache_keep, osd_distill_loss_grad,
+                      osd_distill_topk_loss_grad, osd_max_vocab, osd_sample, osd_shard_verify_draw,
+                      osd_shard_verify_mass, osd_shard_verify_stats, osd_topk, osd_tree_attention, osd_verify,
                       osd_verify_distill, osd_verify_distill_rejected, osd_verify_noalloc, osd_verify_topk,
                       osd_verify_tree)

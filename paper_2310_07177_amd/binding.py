@@ -22,6 +22,9 @@ OSD_MAX_K = 16
 OSD_MAX_SHARDS = 64
 OSD_MAX_TREE_NODES = 64
 OSD_MAX_TOPK = 256
+OSD_MAX_HEAD_DIM = 256
+OSD_MAX_CACHE_BATCH = 4096
+OSD_ROTATE_HALVES, OSD_ROTATE_PAIRS = 0, 1
 # Byte sizes of the sharded verification's records (osd_shard_row_stats,
 # osd_shard_mass in include/osd.h); the binding keeps them as uint8 tensors.
 SHARD_ROW_STATS_BYTES = 40
@@ -33,7 +36,8 @@ EXPORTS = ("osd_max_vocab", "osd_status_string", "osd_verify_workspace_bytes", "
            "osd_verify_distill", "osd_verify_distill_rejected", "osd_verify_tree_workspace_bytes", "osd_verify_tree",
            "osd_sample_workspace_bytes", "osd_sample", "osd_shard_verify_stats", "osd_shard_verify_mass",
            "osd_shard_verify_draw", "osd_topk", "osd_distill_topk_workspace_bytes",
-           "osd_distill_topk_loss_grad", "osd_verify_topk_workspace_bytes", "osd_verify_topk")
+           "osd_distill_topk_loss_grad", "osd_verify_topk_workspace_bytes", "osd_verify_topk",
+           "osd_cache_append", "osd_tree_attention_workspace_bytes", "osd_tree_attention", "osd_cache_keep")
 
 _lib = None
 _lock = threading.Lock()
@@ -109,6 +113,17 @@ def lib():
             L.osd_verify_topk.restype = i32
             L.osd_verify_topk.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, f32, vp, vp, vp, vp,
                                           sz, vp]
+            L.osd_cache_append.restype = i32
+            L.osd_cache_append.argtypes = [vp, vp, i64, i32, i32, i32, i32, i32, vp, i32, vp, vp, i64, vp, i64, i32,
+                                           vp, i64, vp, i64, i32, i32, vp, vp, vp, i32, i32, i32, vp]
+            L.osd_tree_attention_workspace_bytes.restype = sz
+            L.osd_tree_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+            L.osd_tree_attention.restype = i32
+            L.osd_tree_attention.argtypes = [vp, i64, i32, vp, vp, i64, i32, i32, i32, i32, i32, vp, i32, vp, i32,
+                                             i32, vp, vp, f32, vp, vp, sz, vp]
+            L.osd_cache_keep.restype = i32
+            L.osd_cache_keep.argtypes = [vp, vp, i64, i32, i32, i32, i32, i32, i32, i64, vp, i32, vp, i32, i32, vp,
+                                         vp, vp, vp]
             _lib = L
     return _lib
 
@@ -696,3 +711,149 @@ def osd_verify_topk(target_logits, draft_ids, draft_top, draft_tokens, u_accept,
     if st != OSD_OK:
         raise OsdError("osd_verify_topk", st)
     return acc, toks, rmask
+
+
+def _cache_args(k_cache, v_cache, page_table, seq_len, layers=False):
+    """The C ABI's description of a paged cache, checked."""
+    torch = _torch()
+    if k_cache.dim() != 4 + layers or v_cache.shape != k_cache.shape:
+        raise ValueError("the caches must be two " + ("[layers, " if layers else "[")
+                         + "pages, kv_heads, page_size, head_dim] tensors of one shape")
+    if v_cache.dtype != k_cache.dtype:
+        raise TypeError("the caches must share a dtype")
+    P, H, S, D = k_cache.shape[layers:]
+    stride = k_cache.stride()[layers:]
+    if v_cache.stride() != k_cache.stride() or stride[3] != 1 or stride[2] != D or stride[1] != S * D:
+        raise ValueError("a page must be contiguous, and the caches' strides the same")
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [B, pages of a sequence]")
+    B, table_len = page_table.shape
+    _check_out(page_table, (B, table_len), torch.int32, "page_table")
+    _check_out(seq_len, (B,), torch.int32, "seq_len")
+    return B, table_len, stride[0], P, H, S, D, _dtype_code(k_cache)
+
+
+def _token_stride(t, B, N, H, D, dtype, name):
+    """Elements between the tokens of a [B, N, H, D] tensor."""
+    if t.shape != (B, N, H, D) or t.dtype != dtype:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {(B, N, H, D)}")
+    s = t.stride()
+    step = s[1] if N > 1 else s[0] if B > 1 else H * D
+    if s[3] != 1 or (H > 1 and s[2] != D) or (B > 1 and s[0] != N * step):
+        raise ValueError(f"{name}: a token's heads must lie one after another, tokens at one distance")
+    return step
+
+
+def osd_cache_append(k, v, k_cache, v_cache, page_table, seq_len, q=None, rotation=None, pairs=False, parent=None,
+                     new_len=None, q_out=None):
+    """New tokens' keys and values into the paged cache through the C ABI,
+    rotated by their positions on the way, their queries along with them.
+
+    k, v [B, N, kv_heads, head_dim] and q [B, N, q_heads, head_dim] or None:
+    bf16 or fp32, a token's heads one after another (slices of one projection
+    serve as they are).  k_cache, v_cache [pages, kv_heads, page_size,
+    head_dim] like them (any distance between pages), page_table [B, T] and
+    seq_len [B] int32 (context lengths; -1: no sequence).  rotation: [rows,
+    rotary_dim] float32, the cosines, then the sines of a position's angles, or
+    None; pairs: of elements side by side instead of the two halves.  parent
+    [B, N] int32 as osd_verify_tree takes it, or None: a chain.  new_len [B]
+    int32: how many of the N tokens a sequence has.  Returns the rotated
+    queries (new, or `q_out`, which may be q) or None."""
+    torch = _torch()
+    B, table_len, page_stride, P, H, S, D, code = _cache_args(k_cache, v_cache, page_table, seq_len)
+    dev = k_cache.device
+    _check_same_device(dev, k, v, k_cache, v_cache, page_table, seq_len, q, rotation, parent, new_len, q_out)
+    if k.dim() != 4 or (q is not None and q.dim() != 4):
+        raise ValueError("k, v and q must be [B, N, heads, head_dim]")
+    N, dt = k.shape[1], k_cache.dtype
+    k_step, v_step = _token_stride(k, B, N, H, D, dt, "k"), _token_stride(v, B, N, H, D, dt, "v")
+    Hq = q_step = out_step = 0
+    if q is not None:
+        Hq = q.shape[2]
+        q_step = _token_stride(q, B, N, Hq, D, dt, "q")
+        if q_out is None:
+            q_out = torch.empty(B, N, Hq, D, dtype=dt, device=dev)
+            out_step = Hq * D
+        else:
+            out_step = _token_stride(q_out, B, N, Hq, D, dt, "q_out")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    rows = R = 0
+    if rotation is not None:
+        if rotation.dim() != 2:
+            raise ValueError("rotation must be [positions, rotary_dim]")
+        rows, R = rotation.shape
+        _check_out(rotation, (rows, R), torch.float32, "rotation")
+    _check_out(parent, (B, N), torch.int32, "parent")
+    _check_out(new_len, (B,), torch.int32, "new_len")
+    st = _on_device(dev, lib().osd_cache_append, _ptr(k_cache), _ptr(v_cache), page_stride, P, S, H, D, code,
+                    _ptr(page_table), table_len, _ptr(seq_len), _ptr(q), q_step, _ptr(q_out), out_step, Hq, _ptr(k),
+                    k_step, _ptr(v), v_step, B, N, _ptr(parent), _ptr(new_len), _ptr(rotation), rows, R,
+                    OSD_ROTATE_PAIRS if pairs else OSD_ROTATE_HALVES, _stream_handle(dev))
+    if st != OSD_OK:
+        raise OsdError("osd_cache_append", st)
+    return q_out
+
+
+def osd_tree_attention(q, k_cache, v_cache, page_table, seq_len, parent=None, new_len=None, scale=None, out=None):
+    """Attention of drafted tokens through the C ABI: every node of a tree (or
+    chain: parent None) over the context, its ancestors and itself, all in the
+    paged cache.
+
+    q [B, N, q_heads, head_dim] (any distance between tokens), the other
+    arguments as osd_cache_append; scale: 1 / sqrt(head_dim) by default.
+    Returns [B, N, q_heads, head_dim] as a new (or the given `out`) tensor."""
+    torch = _torch()
+    B, table_len, page_stride, P, H, S, D, code = _cache_args(k_cache, v_cache, page_table, seq_len)
+    dev = q.device
+    _check_same_device(dev, q, k_cache, v_cache, page_table, seq_len, parent, new_len, out)
+    if q.dim() != 4:
+        raise ValueError("q must be [B, N, q_heads, head_dim]")
+    N, Hq = q.shape[1], q.shape[2]
+    step = _token_stride(q, B, N, Hq, D, k_cache.dtype, "q")
+    _check_out(parent, (B, N), torch.int32, "parent")
+    _check_out(new_len, (B,), torch.int32, "new_len")
+    if out is None:
+        out = torch.empty(B, N, Hq, D, dtype=q.dtype, device=dev)
+    else:
+        _check_out(out, (B, N, Hq, D), q.dtype, "out")
+    L = lib()
+    ws = workspace("tree_attention", L.osd_tree_attention_workspace_bytes(B, N, Hq, H, D), dev, _scratch)
+    st = _on_device(dev, L.osd_tree_attention, _ptr(q), step, Hq, _ptr(k_cache), _ptr(v_cache), page_stride, P, S, H,
+                    D, code, _ptr(page_table), table_len, _ptr(seq_len), B, N, _ptr(parent), _ptr(new_len),
+                    D ** -0.5 if scale is None else float(scale), _ptr(out), _ptr(ws), ws.numel(),
+                    _stream_handle(dev))
+    if st != OSD_OK:
+        raise OsdError("osd_tree_attention", st)
+    return out
+
+
+def osd_cache_keep(k_cache, v_cache, page_table, seq_len, path_nodes, accepted_len, out=None):
+    """The accepted path of each sequence's tree moves to where its context
+    ends, through the C ABI, in the caches of all layers at once.
+
+    k_cache, v_cache [layers, pages, kv_heads, page_size, head_dim] (one
+    layer: without the first axis), path_nodes [B, N] and accepted_len [B]
+    int32 as osd_verify_tree returns them.  Returns the new context lengths [B]
+    int32 (a new tensor, or the given `out`, not seq_len itself)."""
+    torch = _torch()
+    if k_cache.dim() == 4:
+        k_cache, v_cache = k_cache.unsqueeze(0), v_cache.unsqueeze(0)
+    B, table_len, page_stride, P, H, S, D, code = _cache_args(k_cache, v_cache, page_table, seq_len, layers=True)
+    dev = k_cache.device
+    _check_same_device(dev, k_cache, v_cache, page_table, seq_len, path_nodes, accepted_len, out)
+    if path_nodes.dim() != 2:
+        raise ValueError("path_nodes must be [B, N]")
+    N = path_nodes.shape[1]
+    _check_out(path_nodes, (B, N), torch.int32, "path_nodes")
+    _check_out(accepted_len, (B,), torch.int32, "accepted_len")
+    if out is None:
+        out = torch.empty(B, dtype=torch.int32, device=dev)
+    else:
+        _check_out(out, (B,), torch.int32, "out")
+    st = _on_device(dev, lib().osd_cache_keep, _ptr(k_cache), _ptr(v_cache), page_stride, P, S, H, D, code,
+                    k_cache.shape[0], k_cache.stride(0), _ptr(page_table), table_len, _ptr(seq_len), B, N,
+                    _ptr(path_nodes), _ptr(accepted_len), _ptr(out), _stream_handle(dev))
+    if st != OSD_OK:
+        raise OsdError("osd_cache_keep", st)
+    return out

@@ -812,3 +812,199 @@ int osd_verify_topk(const void* target_logits, const int32_t* draft_ids, const v
 }
 
 }  // extern "C"
+
+// ---------------------------------------------------------------------------
+// The paged cache: appended to, attended over, its accepted paths moved.
+// ---------------------------------------------------------------------------
+namespace {
+
+// Elements between pages, layers and tokens, at most (so that no address computation overflows).
+constexpr int64_t kMaxStride = int64_t(1) << 40, kMaxTokenStride = int64_t(1) << 28;
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// The cache arguments that the three operators share.
+int check_cache(const void* k_cache, const void* v_cache, int64_t page_stride, int pages, int page_size, int kv_heads,
+                int head_dim, int dtype, const int32_t* page_table, int table_len, const int32_t* seq_len, int B,
+                int N) {
+    if (dtype != OSD_F32 && dtype != OSD_BF16) return OSD_ERR_INVALID_ARG;
+    if (pages <= 0 || page_size <= 0 || kv_heads <= 0 || head_dim <= 0 || table_len <= 0 || B <= 0 || N <= 0)
+        return OSD_ERR_INVALID_ARG;
+    if (!k_cache || !v_cache || !page_table || !seq_len) return OSD_ERR_INVALID_ARG;
+    if (head_dim % 8 || head_dim > OSD_MAX_HEAD_DIM || B > OSD_MAX_CACHE_BATCH) return OSD_ERR_UNSUPPORTED;
+    const int64_t es = dtype == OSD_BF16 ? 2 : 4;
+    if (int64_t(table_len) * page_size > 0x7FFFFFFFll || int64_t(page_size) * head_dim * es > 0x7FFFFFFFll)
+        return OSD_ERR_INVALID_ARG;
+    if (kv_heads > 65535 || page_stride < int64_t(kv_heads) * page_size * head_dim ||
+        page_stride > kMaxStride || page_stride * es % 16)
+        return OSD_ERR_INVALID_ARG;
+    if (!aligned16(k_cache) || !aligned16(v_cache)) return OSD_ERR_INVALID_ARG;
+    return OSD_OK;
+}
+
+osd::CachePages cache_pages(int64_t page_stride, int pages, int page_size, int head_dim, int dtype,
+                            const int32_t* page_table, int table_len) {
+    const int64_t es = dtype == OSD_BF16 ? 2 : 4;
+    osd::CachePages c;
+    c.table = page_table;
+    c.table_len = table_len;
+    c.pages = pages;
+    c.page_size = page_size;
+    c.capacity = table_len * page_size;
+    // With l = ceil(log2 S), m = ceil(2^(31 + l) / S) < 2^32: j m / 2^(31 + l) is above j / S by less
+    // than j / 2^(31 + l) < 2^-l <= 1 / S for j < 2^31, so it does not reach the next whole number.
+    int l = 0;
+    while ((int64_t(1) << l) < page_size) ++l;
+    c.shift = uint32_t(31 + l);
+    c.magic = uint32_t(((uint64_t(1) << c.shift) + uint64_t(page_size) - 1) / uint64_t(page_size));
+    c.page_bytes = page_stride * es;
+    c.row_bytes = int(head_dim * es);
+    c.head_bytes = int64_t(page_size) * c.row_bytes;
+    return c;
+}
+
+// Tokens of `heads` heads at `stride` elements.
+bool stride_ok(int64_t stride, int heads, int head_dim, int64_t es) {
+    return stride >= int64_t(heads) * head_dim && stride <= kMaxTokenStride && stride * es % 16 == 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+int osd_cache_append(void* k_cache, void* v_cache, int64_t page_stride, int pages, int page_size, int kv_heads,
+                     int head_dim, int dtype, const int32_t* page_table, int table_len, const int32_t* seq_len,
+                     const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, int q_heads,
+                     const void* k, int64_t k_stride, const void* v, int64_t v_stride, int B, int N,
+                     const int32_t* parent, const int32_t* new_len, const float* rotation, int rotation_rows,
+                     int rotary_dim, int rotation_style, void* stream) {
+    const int st = check_cache(k_cache, v_cache, page_stride, pages, page_size, kv_heads, head_dim, dtype, page_table,
+                               table_len, seq_len, B, N);
+    if (st != OSD_OK) return st;
+    if (int64_t(B) * N > 0x7FFFFFFFll || (parent && N > OSD_MAX_TREE_NODES)) return OSD_ERR_INVALID_ARG;
+    const int64_t es = dtype == OSD_BF16 ? 2 : 4, tokens = int64_t(B) * N;
+    if (!k || !v || !aligned16(k) || !aligned16(v) || (!q) != (!q_out)) return OSD_ERR_INVALID_ARG;
+    if (!stride_ok(k_stride, kv_heads, head_dim, es) || !stride_ok(v_stride, kv_heads, head_dim, es))
+        return OSD_ERR_INVALID_ARG;
+    if (q) {
+        if (q_heads <= 0 || q_heads > 65535 || !aligned16(q) || !aligned16(q_out)) return OSD_ERR_INVALID_ARG;
+        if (!stride_ok(q_stride, q_heads, head_dim, es) || !stride_ok(q_out_stride, q_heads, head_dim, es))
+            return OSD_ERR_INVALID_ARG;
+        const uint64_t row = uint64_t(q_heads) * head_dim * es;
+        if (!(q_out == q && q_out_stride == q_stride) &&
+            meets(q, uint64_t((tokens - 1) * q_stride * es) + row, q_out, uint64_t((tokens - 1) * q_out_stride * es) + row))
+            return OSD_ERR_INVALID_ARG;
+    }
+    if (rotation) {
+        if (rotation_rows <= 0 || rotary_dim <= 0 || rotary_dim % 2 || rotary_dim > head_dim) return OSD_ERR_INVALID_ARG;
+        if (rotation_style != OSD_ROTATE_HALVES && rotation_style != OSD_ROTATE_PAIRS) return OSD_ERR_INVALID_ARG;
+        if (!aligned16(rotation)) return OSD_ERR_INVALID_ARG;
+    }
+    osd::AppendLaunch L;
+    L.k_cache = static_cast<char*>(k_cache);
+    L.v_cache = static_cast<char*>(v_cache);
+    L.pages = cache_pages(page_stride, pages, page_size, head_dim, dtype, page_table, table_len);
+    L.seq_len = seq_len;
+    L.q = static_cast<const char*>(q);
+    L.q_out = static_cast<char*>(q_out);
+    L.k = static_cast<const char*>(k);
+    L.v = static_cast<const char*>(v);
+    L.q_stride = q_stride * es;
+    L.q_out_stride = q_out_stride * es;
+    L.k_stride = k_stride * es;
+    L.v_stride = v_stride * es;
+    L.dtype = dtype;
+    L.B = B;
+    L.N = N;
+    L.q_heads = q ? q_heads : 0;
+    L.kv_heads = kv_heads;
+    L.head_dim = head_dim;
+    L.parent = parent;
+    L.new_len = new_len;
+    L.rotation = rotation;
+    L.rotation_rows = rotation ? rotation_rows : 0;
+    L.rotary_dim = rotation ? rotary_dim : 0;
+    L.style = rotation_style;
+    L.stream = static_cast<hipStream_t>(stream);
+    return osd::launch_append(L) == hipSuccess ? OSD_OK : OSD_ERR_DEVICE;
+}
+
+size_t osd_tree_attention_workspace_bytes(int B, int N, int q_heads, int kv_heads, int head_dim) {
+    if (B <= 0 || B > OSD_MAX_CACHE_BATCH || N <= 0 || N > OSD_MAX_TREE_NODES) return 0;
+    if (kv_heads <= 0 || q_heads <= 0 || q_heads > 65535 || q_heads % kv_heads) return 0;
+    if (head_dim <= 0 || head_dim % 8 || head_dim > OSD_MAX_HEAD_DIM) return 0;
+    return round_up(osd::tree_attention_workspace(B, N, q_heads, kv_heads, head_dim), kAlign);
+}
+
+int osd_tree_attention(const void* q, int64_t q_stride, int q_heads, const void* k_cache, const void* v_cache,
+                       int64_t page_stride, int pages, int page_size, int kv_heads, int head_dim, int dtype,
+                       const int32_t* page_table, int table_len, const int32_t* seq_len, int B, int N,
+                       const int32_t* parent, const int32_t* new_len, float scale, void* out, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+    const int st = check_cache(k_cache, v_cache, page_stride, pages, page_size, kv_heads, head_dim, dtype, page_table,
+                               table_len, seq_len, B, N);
+    if (st != OSD_OK) return st;
+    if (N > OSD_MAX_TREE_NODES || q_heads <= 0 || q_heads > 65535 || q_heads % kv_heads) return OSD_ERR_INVALID_ARG;
+    const int64_t es = dtype == OSD_BF16 ? 2 : 4;
+    if (!q || !out || !aligned16(q) || !aligned16(out)) return OSD_ERR_INVALID_ARG;
+    if (!stride_ok(q_stride, q_heads, head_dim, es)) return OSD_ERR_INVALID_ARG;
+    if (!(scale - scale == 0.0f)) return OSD_ERR_INVALID_ARG;  // NaN, infinite
+    const uint64_t row = uint64_t(q_heads) * head_dim * es, tokens = uint64_t(B) * N;
+    if (meets(q, (tokens - 1) * uint64_t(q_stride * es) + row, out, tokens * row)) return OSD_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < osd_tree_attention_workspace_bytes(B, N, q_heads, kv_heads, head_dim) ||
+        !aligned16(workspace))
+        return OSD_ERR_WORKSPACE;
+    osd::TreeAttentionLaunch L;
+    L.q = static_cast<const char*>(q);
+    L.q_stride = q_stride * es;
+    L.k_cache = static_cast<const char*>(k_cache);
+    L.v_cache = static_cast<const char*>(v_cache);
+    L.pages = cache_pages(page_stride, pages, page_size, head_dim, dtype, page_table, table_len);
+    L.seq_len = seq_len;
+    L.dtype = dtype;
+    L.B = B;
+    L.N = N;
+    L.q_heads = q_heads;
+    L.kv_heads = kv_heads;
+    L.head_dim = head_dim;
+    L.parent = parent;
+    L.new_len = new_len;
+    L.scale = scale;
+    L.out = static_cast<char*>(out);
+    L.workspace = static_cast<char*>(workspace);
+    L.stream = static_cast<hipStream_t>(stream);
+    L.cus = device_cus(L.stream);
+    return osd::launch_tree_attention(L) == hipSuccess ? OSD_OK : OSD_ERR_DEVICE;
+}
+
+int osd_cache_keep(void* k_cache, void* v_cache, int64_t page_stride, int pages, int page_size, int kv_heads,
+                   int head_dim, int dtype, int layers, int64_t layer_stride, const int32_t* page_table,
+                   int table_len, const int32_t* seq_len, int B, int N, const int32_t* path_nodes,
+                   const int32_t* accepted_len, int32_t* new_seq_len, void* stream) {
+    const int st = check_cache(k_cache, v_cache, page_stride, pages, page_size, kv_heads, head_dim, dtype, page_table,
+                               table_len, seq_len, B, N);
+    if (st != OSD_OK) return st;
+    const int64_t es = dtype == OSD_BF16 ? 2 : 4;
+    if (N > OSD_MAX_TREE_NODES || layers <= 0 || layers > 65535 || layer_stride < 0 || layer_stride > kMaxStride ||
+        layer_stride * es % 16)
+        return OSD_ERR_INVALID_ARG;
+    if (!path_nodes || !accepted_len || !new_seq_len) return OSD_ERR_INVALID_ARG;
+    if (meets(seq_len, uint64_t(B) * 4, new_seq_len, uint64_t(B) * 4)) return OSD_ERR_INVALID_ARG;
+    osd::KeepLaunch L;
+    L.k_cache = static_cast<char*>(k_cache);
+    L.v_cache = static_cast<char*>(v_cache);
+    L.pages = cache_pages(page_stride, pages, page_size, head_dim, dtype, page_table, table_len);
+    L.layer_bytes = layer_stride * es;
+    L.layers = layers;
+    L.seq_len = seq_len;
+    L.B = B;
+    L.N = N;
+    L.kv_heads = kv_heads;
+    L.path_nodes = path_nodes;
+    L.accepted_len = accepted_len;
+    L.new_seq_len = new_seq_len;
+    L.stream = static_cast<hipStream_t>(stream);
+    return osd::launch_keep(L) == hipSuccess ? OSD_OK : OSD_ERR_DEVICE;
+}
+
+}  // extern "C"

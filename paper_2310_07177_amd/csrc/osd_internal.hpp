@@ -326,4 +326,70 @@ struct VerifyTopkLaunch {
 };
 hipError_t launch_verify_topk(const VerifyTopkLaunch& L);
 
+// The paged cache (cache.hip, tree_attention.hip): where the tokens of a
+// sequence lie.
+struct CachePages {
+    const int32_t* table;    // [B, table_len]
+    int table_len;
+    int pages, page_size;
+    int capacity;            // tokens of a table
+    uint32_t magic, shift;   // j / page_size = j * magic >> shift, j < 2^31
+    int64_t page_bytes;      // between pages
+    int64_t head_bytes;      // between the heads of a page
+    int row_bytes;           // of one token of one head
+};
+
+struct AppendLaunch {
+    char* k_cache;
+    char* v_cache;
+    CachePages pages;
+    const int32_t* seq_len;
+    const char* q;
+    char* q_out;
+    const char* k;
+    const char* v;
+    int64_t q_stride, q_out_stride, k_stride, v_stride;  // bytes
+    int dtype, B, N, q_heads, kv_heads, head_dim;
+    const int32_t* parent;
+    const int32_t* new_len;
+    const float* rotation;
+    int rotation_rows, rotary_dim, style;
+    hipStream_t stream;
+};
+hipError_t launch_append(const AppendLaunch& L);
+
+struct KeepLaunch {
+    char* k_cache;
+    char* v_cache;
+    CachePages pages;
+    int64_t layer_bytes;
+    int layers;
+    const int32_t* seq_len;
+    int B, N, kv_heads;
+    const int32_t* path_nodes;
+    const int32_t* accepted_len;
+    int32_t* new_seq_len;
+    hipStream_t stream;
+};
+hipError_t launch_keep(const KeepLaunch& L);
+
+struct TreeAttentionLaunch {
+    const char* q;
+    int64_t q_stride;  // bytes
+    const char* k_cache;
+    const char* v_cache;
+    CachePages pages;
+    const int32_t* seq_len;
+    int dtype, B, N, q_heads, kv_heads, head_dim;
+    const int32_t* parent;
+    const int32_t* new_len;
+    float scale;
+    char* out;
+    char* workspace;
+    int cus;
+    hipStream_t stream;
+};
+size_t tree_attention_workspace(int B, int N, int q_heads, int kv_heads, int head_dim);
+hipError_t launch_tree_attention(const TreeAttentionLaunch& L);
+
 }  // namespace osd
