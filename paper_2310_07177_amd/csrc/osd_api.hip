@@ -833,7 +833,7 @@ int check_cache(const void* k_cache, const void* v_cache, int64_t page_stride, i
     if (!k_cache || !v_cache || !page_table || !seq_len) return OSD_ERR_INVALID_ARG;
     if (head_dim % 8 || head_dim > OSD_MAX_HEAD_DIM || B > OSD_MAX_CACHE_BATCH) return OSD_ERR_UNSUPPORTED;
     const int64_t es = dtype == OSD_BF16 ? 2 : 4;
-    if (int64_t(table_len) * page_size > 0x7FFFFFFFll || int64_t(page_size) * head_dim * es > 0x7FFFFFFFll)
+    if (int64_t(table_len) * page_size > (int64_t(1) << 30) || int64_t(page_size) * head_dim * es > 0x7FFFFFFFll)
         return OSD_ERR_INVALID_ARG;
     if (kv_heads > 65535 || page_stride < int64_t(kv_heads) * page_size * head_dim ||
         page_stride > kMaxStride || page_stride * es % 16)
