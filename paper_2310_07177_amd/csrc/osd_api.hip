@@ -833,7 +833,8 @@ int check_cache(const void* k_cache, const void* v_cache, int64_t page_stride, i
     if (!k_cache || !v_cache || !page_table || !seq_len) return OSD_ERR_INVALID_ARG;
     if (head_dim % 8 || head_dim > OSD_MAX_HEAD_DIM || B > OSD_MAX_CACHE_BATCH) return OSD_ERR_UNSUPPORTED;
     const int64_t es = dtype == OSD_BF16 ? 2 : 4;
-    if (int64_t(table_len) * page_size > (int64_t(1) << 30) || int64_t(page_size) * head_dim * es > 0x7FFFFFFFll)
+    if (int64_t(table_len) * page_size > (int64_t(1) << 30) ||
+        int64_t(table_len) * page_size * B > (int64_t(1) << 36) || int64_t(page_size) * head_dim * es > 0x7FFFFFFFll)
         return OSD_ERR_INVALID_ARG;
     if (kv_heads > 65535 || page_stride < int64_t(kv_heads) * page_size * head_dim ||
         page_stride > kMaxStride || page_stride * es % 16)
@@ -933,7 +934,7 @@ size_t osd_tree_attention_workspace_bytes(int B, int N, int q_heads, int kv_head
     if (B <= 0 || B > OSD_MAX_CACHE_BATCH || N <= 0 || N > OSD_MAX_TREE_NODES) return 0;
     if (kv_heads <= 0 || q_heads <= 0 || q_heads > 65535 || q_heads % kv_heads) return 0;
     if (head_dim <= 0 || head_dim % 8 || head_dim > OSD_MAX_HEAD_DIM) return 0;
-    return round_up(osd::tree_attention_workspace(B, N, q_heads, kv_heads, head_dim), kAlign);
+    return round_up(osd::tree_attention_workspace(N, q_heads, kv_heads, head_dim), kAlign);
 }
 
 int osd_tree_attention(const void* q, int64_t q_stride, int q_heads, const void* k_cache, const void* v_cache,

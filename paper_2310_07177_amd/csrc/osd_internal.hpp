@@ -389,7 +389,7 @@ struct TreeAttentionLaunch {
     int cus;
     hipStream_t stream;
 };
-size_t tree_attention_workspace(int B, int N, int q_heads, int kv_heads, int head_dim);
+size_t tree_attention_workspace(int N, int q_heads, int kv_heads, int head_dim);
 hipError_t launch_tree_attention(const TreeAttentionLaunch& L);
 
 }  // namespace osd

@@ -1,0 +1,493 @@
+// tree_attention.hpp -- what the two kernels of osd_tree_attention share: the
+// matrix products, the softmax of a step, how work is divided, how parts are
+// joined and rows written.
+//
+// The rows that read one kv head (all nodes, all its query heads) are the columns
+// of two matrix products with each tile of keys:
+//   S^T = K Q^T            A: 16 keys,          B: 16 rows of queries
+//   O^T += V^T P^T         A: 16 of the values, B: the same rows
+// so that the probabilities come out of the first product where the second takes
+// them: a lane holds 4 keys of every 16 for one row, and as the order of keys
+// within a product is free, these are its 8 (bf16) or 1 (fp32) of the second's.
+// K is read as the first product's A operand, 16 bytes a lane.  Softmax in one pass:
+// running maximum and sum in fp32, rescaled when a step raises a maximum.
+#pragma once
+
+#include "cache_device.hpp"
+
+namespace osd {
+namespace attention {
+
+constexpr int kMaxGroups = 512;   // workgroups of a launch
+constexpr int kMaxPieces = 64;    // workgroups that share a unit
+
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+
+// Maximum and sum over the four lanes that hold one row (lane, +16, +32, +48).
+__device__ inline float rows_max(float x) {
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ inline float rows_sum(float x) {
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+// 2^(a - b), 0 where a is -inf (nothing seen yet).
+__device__ inline float rescale(float a, float b) { return a == kNegInf ? 0.0f : exp2_fast(a - b); }
+
+// The matrix products of one format.  KT tiles of 16 keys make a step.
+//   K: chunk c of a key holds elements c * kChunk + group * (16 / ES) ..
+//   V: a lane holds VW elements of a row for each block of 16 * VW of them.
+// A value that is not finite must not reach rows that do not see its key (0 * inf
+// is NaN): in steps that have keys of the tree the product takes 0 in its place, and
+// the rows that see it get it when they are written.
+struct Bf16Ops {
+    using Fmt = BF16;
+    static constexpr int kKT = 2, kChunk = 32;
+    template <int VW>
+    struct Value {
+        typedef uint32_t reg_t __attribute__((ext_vector_type(VW / 2)));
+        reg_t x;
+        __device__ bool finite() const {
+            bool f = true;
+#pragma unroll
+            for (int e = 0; e < VW / 2; ++e)
+                f = f && (x[e] & 0x7F80u) != 0x7F80u && (x[e] & 0x7F800000u) != 0x7F800000u;
+            return f;
+        }
+    };
+    __device__ static f32x4_t qk(const chunk_t& k, const chunk_t& q, f32x4_t s) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k), __builtin_bit_cast(bf16x8_t, q), s,
+                                                       0, 0, 0);
+    }
+    __device__ static chunk_t negate(chunk_t q) { return q ^ 0x80008000u; }
+    struct Probs {
+        chunk_t x;
+    };
+    __device__ static Probs probs(const float (&p)[8]) {
+        Probs r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.x[i] = pack_bf16x2(p[2 * i], p[2 * i + 1]);
+        return r;
+    }
+    // Element t of the 8 keys of a lane.
+    template <int VW>
+    __device__ static chunk_t column(const Value<VW> (&v)[8], int t) {
+        chunk_t a;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            a[i] = __builtin_amdgcn_perm(v[2 * i + 1].x[t / 2], v[2 * i].x[t / 2], (t & 1) ? 0x07060302u : 0x05040100u);
+        return a;
+    }
+    template <int VW>
+    __device__ static f32x4_t pv(const Value<VW> (&v)[8], int t, const Probs& p, f32x4_t o) {
+        return qk(column(v, t), p.x, o);
+    }
+    __device__ static uint32_t half_finite(uint32_t h) { return (h & 0x7F80u) == 0x7F80u ? 0u : h; }
+    __device__ static uint32_t pair_finite(uint32_t h) { return half_finite(h & 0xFFFFu) | half_finite(h >> 16) << 16; }
+    template <int VW>
+    __device__ static void clean(Value<VW>& v) {
+#pragma unroll
+        for (int e = 0; e < VW / 2; ++e) v.x[e] = pair_finite(v.x[e]);
+    }
+};
+
+struct F32Ops {
+    using Fmt = F32;
+    static constexpr int kKT = 1, kChunk = 16;
+    template <int VW>
+    struct Value {
+        static_assert(VW == 4, "16 bytes");
+        f32x4_t x;
+        __device__ bool finite() const {
+            bool f = true;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f = f && (__float_as_uint(x[e]) & 0x7F800000u) != 0x7F800000u;
+            return f;
+        }
+    };
+    __device__ static f32x4_t qk(const chunk_t& k, const chunk_t& q, f32x4_t s) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[i]), __uint_as_float(q[i]), s, 0, 0, 0);
+        return s;
+    }
+    __device__ static chunk_t negate(chunk_t q) { return q ^ 0x80000000u; }
+    struct Probs {
+        f32x4_t x;
+    };
+    __device__ static Probs probs(const float (&p)[4]) { return Probs{f32x4_t{p[0], p[1], p[2], p[3]}}; }
+    template <int VW>
+    __device__ static f32x4_t pv(const Value<VW> (&v)[4], int t, const Probs& p, f32x4_t o) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i].x[t], p.x[i], o, 0, 0, 0);
+        return o;
+    }
+    template <int VW>
+    __device__ static void clean(Value<VW>& v) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v.x[e] = v.x[e] - v.x[e] == 0.0f ? v.x[e] : 0.0f;
+    }
+};
+
+struct no_t {
+    static constexpr bool value = false;
+};
+struct yes_t {
+    static constexpr bool value = true;
+};
+
+struct Args {
+    TreeAttentionLaunch L;
+    float c2;            // |scale| * log2(e)
+    int group;           // query heads of a kv head
+    int blocks;          // row blocks of a kv head
+    uint32_t* counters;  // [kMaxGroups] zero on entry and exit: arrivals of the unit that begins in a workgroup
+    float* stats;        // [2 * kMaxGroups, rows, 2] maximum (times c2) and sum
+    float* parts;        // [2 * kMaxGroups, rows, DT] sums of p v
+    uint32_t stats_bytes, parts_bytes;
+};
+
+// A sequence: 0 normal, 1 nothing to attend to (zeros), 2 invalid (NaN).
+struct Seq {
+    int len, n, state;
+};
+__device__ inline Seq sequence(const TreeAttentionLaunch& L, int b) {
+    Seq s{L.seq_len[b], L.new_len ? L.new_len[b] : L.N, 0};
+    if (s.len < 0 || s.n == 0) s.state = 1;
+    else if (!cache_fits(L.pages, s.len, s.n, L.N)) s.state = 2;
+    return s;
+}
+
+// Work is counted in tiles of keys.  A unit is one row block of one kv head of one
+// sequence, all its keys; units lie one after another, and workgroup w of W takes
+// the tiles from w * total / W on: equal shares whatever the lengths, at most two
+// pieces of which are parts of units (the others it has alone).
+struct Share {
+    int64_t total, W;
+    __device__ int64_t begin(int64_t w) const { return w * total / W; }
+    __device__ int64_t owner(int64_t tile) const { return ((tile + 1) * W - 1) / total; }
+};
+
+// Tiles of all sequences before each (s_tiles [B + 1]), and the shares.
+template <int THREADS, int TILE>
+__device__ inline Share divide(const Args& a, int* s_tiles) {
+    constexpr int WAVES = THREADS / kWave;
+    __shared__ int s_scan[WAVES];
+    const TreeAttentionLaunch& L = a.L;
+    const int tid = int(threadIdx.x), lane = tid & (kWave - 1), wave = tid / kWave;
+    const int each = (L.B + THREADS - 1) / THREADS, first = tid * each;
+    int mine = 0;
+    for (int b = first; b < first + each && b < L.B; ++b) {
+        const Seq s = sequence(L, b);
+        const int tiles = s.state ? 1 : (s.len + s.n - 1) / TILE + 1;
+        s_tiles[b] = tiles;
+        mine += tiles;
+    }
+    int sum = mine;
+#pragma unroll
+    for (int o = 1; o < kWave; o *= 2) {
+        const int up = __shfl_up(sum, o);
+        if (lane >= o) sum += up;
+    }
+    if (lane == kWave - 1) s_scan[wave] = sum;
+    __syncthreads();
+    int before = sum - mine;
+    for (int w = 0; w < wave; ++w) before += s_scan[w];
+    for (int b = first; b < first + each && b < L.B; ++b) {
+        const int tiles = s_tiles[b];
+        s_tiles[b] = before;
+        before += tiles;
+        if (b == L.B - 1) s_tiles[L.B] = before;
+    }
+    __syncthreads();
+    const int64_t units = int64_t(L.kv_heads) * a.blocks;
+    Share s{s_tiles[L.B] * units, int64_t(gridDim.x)};
+    if (s.W > L.B * units * kMaxPieces) s.W = L.B * units * kMaxPieces;
+    if (s.W > s.total) s.W = s.total;
+    return s;
+}
+
+// A workgroup's part of one unit.
+struct Piece {
+    Seq seq;
+    int b, h, tiles, t0, t1;
+    int row0, rows, live;  // of the row block: its first row, its rows, those before padding
+    int T;                 // keys
+    __device__ bool whole() const { return t0 == 0 && t1 == tiles; }
+};
+template <int ROWS>
+__device__ inline Piece find_piece(const Args& a, const int* s_tiles, int64_t pos, int64_t end) {
+    const TreeAttentionLaunch& L = a.L;
+    const int64_t units = int64_t(L.kv_heads) * a.blocks;
+    int b = 0;
+    for (int hi = L.B; hi - b > 1;) {
+        const int mid = (b + hi) / 2;
+        if (s_tiles[mid] * units <= pos) b = mid;
+        else hi = mid;
+    }
+    Piece p;
+    p.b = __builtin_amdgcn_readfirstlane(b);
+    p.seq = sequence(L, p.b);
+    p.tiles = __builtin_amdgcn_readfirstlane(s_tiles[p.b + 1] - s_tiles[p.b]);
+    const int64_t in_b = pos - s_tiles[p.b] * units;
+    const int unit = __builtin_amdgcn_readfirstlane(int(in_b / p.tiles));
+    p.t0 = __builtin_amdgcn_readfirstlane(int(in_b - int64_t(unit) * p.tiles));
+    p.t1 = __builtin_amdgcn_readfirstlane(int(end - pos < p.tiles - p.t0 ? p.t0 + (end - pos) : p.tiles));
+    p.h = unit / a.blocks;
+    p.row0 = (unit - p.h * a.blocks) * ROWS;
+    p.rows = L.N * a.group - p.row0 < ROWS ? L.N * a.group - p.row0 : ROWS;
+    p.live = p.seq.state ? 0 : p.seq.n * a.group - p.row0;
+    p.T = p.seq.state ? 0 : p.seq.len + p.seq.n;
+    return p;
+}
+
+// Queries of 16 rows as the first product's B operand, `r` of the block this lane's.
+template <typename Ops, int CHUNKS, bool FULL>
+__device__ inline void load_queries(const Args& a, const Piece& p, int r, int D, chunk_t (&q)[CHUNKS]) {
+    const TreeAttentionLaunch& L = a.L;
+    constexpr int ES = Ops::Fmt::kBytes;
+    const int grp = (int(threadIdx.x) & (kWave - 1)) >> 4;
+    const int node = (p.row0 + r) / a.group, g = p.row0 + r - node * a.group;
+    const char* at = L.q + (int64_t(p.b) * L.N + node) * L.q_stride + int64_t(p.h * a.group + g) * D * ES + grp * 16;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+        q[c] = chunk_t{0, 0, 0, 0};
+        if (r < p.live && (FULL || c * Ops::kChunk + grp * (16 / ES) < D))
+            q[c] = *reinterpret_cast<const chunk_t*>(at + c * Ops::kChunk * ES);
+        if (L.scale < 0.0f) q[c] = Ops::negate(q[c]);
+    }
+}
+
+// Elements of V that a lane reads at once where each lane reads whole pieces of rows.
+template <typename Ops, int DT>
+constexpr int kPiece = DT * Ops::Fmt::kBytes >= 256 ? 16 / Ops::Fmt::kBytes : DT / 16;
+
+// 16 MT rows and what a wave has summed for them: element (col * VW + t) of block n of
+// a row's values in acc[..][n][t].
+template <typename Ops, int DT, int MT, int VW_>
+struct Rows {
+    static constexpr int ES = Ops::Fmt::kBytes, KT = Ops::kKT, KEYS = 4 * KT, CHUNKS = DT / Ops::kChunk;
+    static constexpr int VW = VW_, BW = 16 * VW, BLOCKS = DT / BW;
+    f32x4_t acc[MT][BLOCKS][VW];
+    float top[MT], sum[MT];
+    uint64_t sees[MT];  // the tree's nodes that a row sees
+    bool odd;           // a value of the tree's steps that is not finite
+
+    __device__ void clear() {
+        odd = false;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            top[mt] = kNegInf;
+            sum[mt] = 0.0f;
+            sees[mt] = 0;
+#pragma unroll
+            for (int n = 0; n < BLOCKS; ++n)
+#pragma unroll
+                for (int t = 0; t < VW; ++t) acc[mt][n][t] = f32x4_t{0, 0, 0, 0};
+        }
+    }
+    // From the scores of the keys from j0 on to their probabilities.  TAIL: there are
+    // keys that not every row sees, or none.
+    template <bool TAIL>
+    __device__ void soften(f32x4_t (&s)[MT][KT], float c2, int j0, const Seq& seq, typename Ops::Probs (&p)[MT]) {
+        const int grp = (int(threadIdx.x) & (kWave - 1)) >> 4;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            bool on[KEYS];
+            float best = kNegInf;
+            if constexpr (TAIL) {
+#pragma unroll
+                for (int i = 0; i < KEYS; ++i) {
+                    const int j = j0 + (i / 4) * 16 + grp * 4 + (i & 3) - seq.len;
+                    on[i] = j < 0 || (j < seq.n && (sees[mt] >> (j & 63) & 1));
+                    if (!on[i]) s[mt][i / 4][i & 3] = kNegInf;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i) best = fmaxf(best, s[mt][i / 4][i & 3]);
+            best = fmaxf(rows_max(best) * c2, top[mt]);
+            if (__any(best > top[mt])) {
+                const float f = rescale(top[mt], best);
+                sum[mt] *= f;
+#pragma unroll
+                for (int n = 0; n < BLOCKS; ++n)
+#pragma unroll
+                    for (int t = 0; t < VW; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[mt][n][t][e] *= f;
+                top[mt] = best;
+            }
+            // (The same rounded product c2 * maximum is in every exponent, so its rounding cancels.)
+            const float base = top[mt] == kNegInf ? 0.0f : top[mt];
+            float x[KEYS];
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i) {
+                x[i] = exp2_fast(fmaf(s[mt][i / 4][i & 3], c2, -base));
+                if constexpr (TAIL) x[i] = on[i] ? x[i] : 0.0f;
+                sum[mt] += x[i];
+            }
+            p[mt] = Ops::probs(x);
+        }
+    }
+    // Keys behind the last may hold anything; nodes that a row does not see, too.
+    template <typename Value>
+    __device__ void guard(Value (&v)[BLOCKS][KEYS], int j0, int T) {
+        const int grp = (int(threadIdx.x) & (kWave - 1)) >> 4;
+        bool fine = true;
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) {
+            const bool in = j0 + (i / 4) * 16 + grp * 4 + (i & 3) < T;
+#pragma unroll
+            for (int n = 0; n < BLOCKS; ++n) {
+                if (!in) v[n][i].x = decltype(Value::x){};
+                fine = fine && v[n][i].finite();
+            }
+        }
+        if (__any(!fine)) {
+            odd = true;
+#pragma unroll
+            for (int n = 0; n < BLOCKS; ++n)
+#pragma unroll
+                for (int i = 0; i < KEYS; ++i) Ops::clean(v[n][i]);
+        }
+    }
+    template <typename Value>
+    __device__ void add(const Value (&v)[BLOCKS][KEYS], const typename Ops::Probs (&p)[MT]) {
+#pragma unroll
+        for (int n = 0; n < BLOCKS; ++n)
+#pragma unroll
+            for (int t = 0; t < VW; ++t)
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) acc[mt][n][t] = Ops::pv(v[n], t, p[mt], acc[mt][n][t]);
+    }
+    // The sums of row tile mt, times f, to a row of LDS.
+    template <int PITCH>
+    __device__ void store(int mt, float f, float* row) const {
+        const int grp = (int(threadIdx.x) & (kWave - 1)) >> 4;
+#pragma unroll
+        for (int n = 0; n < BLOCKS; ++n) {
+            if constexpr (VW == 1) {
+                *reinterpret_cast<f32x4_t*>(row + n * 16 + grp * 4) = acc[mt][n][0] * f;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int t = 0; t < VW; t += 4)
+                        *reinterpret_cast<f32x4_t*>(row + n * BW + (grp * 4 + e) * VW + t) =
+                            f32x4_t{acc[mt][n][t][e] * f, acc[mt][n][t + 1][e] * f, acc[mt][n][t + 2][e] * f, acc[mt][n][t + 3][e] * f};
+            }
+        }
+    }
+};
+
+// Adds the values d .. d+3 that are not finite of the keys from `from` on that a row sees.
+template <typename Fmt>
+__device__ inline void add_odd(const TreeAttentionLaunch& L, int b, int h, int d, int len, int T, int from, uint64_t sees,
+                                     f32x4_t& o) {
+    for (int j = from; j < T; ++j) {
+        if (j >= len && !(sees >> (j - len) & 1)) continue;
+        const int64_t at = cache_place(L.pages, b, j);
+        if (at < 0) continue;
+        for (int e = 0; e < 4; ++e) {
+            const float x = Fmt::load_one(L.v_cache + at + h * L.pages.head_bytes, d + e);
+            if (x - x != 0.0f) o[e] += x;
+        }
+    }
+}
+
+// Four values of a row to the output.
+template <typename Fmt>
+__device__ inline void write_row(const Args& a, const Piece& p, int row, int d, int D, f32x4_t o, float total) {
+    const TreeAttentionLaunch& L = a.L;
+    const int at = p.row0 + row, node = at / a.group, g = at - node * a.group;
+    char* to = L.out + (((int64_t(p.b) * L.N + node) * L.q_heads + p.h * a.group + g) * D + d) * Fmt::kBytes;
+    const float inv = 1.0f / total;
+    const bool on = row < p.live || (p.seq.state == 2 && (p.seq.n < 0 || p.seq.n > node));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = on ? o[e] * inv : 0.0f;
+    if constexpr (Fmt::kBytes == 2) *reinterpret_cast<u32x2_t*>(to) = u32x2_t{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+    else *reinterpret_cast<f32x4_t*>(to) = o;
+}
+
+// Parts cross workgroups through loads and stores at device scope (sc1), which
+// pass by the private caches of the dies.
+constexpr int kDeviceScope = 16;
+__device__ inline auto buffer_of(float* p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(p, 0, int(bytes), 0x00027000);
+}
+template <int ROWS, int DT>
+__device__ inline void post_part(const Args& a, int64_t slot, int row, int d, f32x4_t o, float top, float sum) {
+    const int64_t at = slot * ROWS + row;
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(chunk_t, o), buffer_of(a.parts, a.parts_bytes),
+                                           int(uint32_t(at * DT + d) * 4u), 0, kDeviceScope);
+    if (d == 0)
+        __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{__float_as_uint(top), __float_as_uint(sum)},
+                                              buffer_of(a.stats, a.stats_bytes), int(uint32_t(at) * 8u), 0, kDeviceScope);
+}
+
+// A workgroup has posted its part of a unit (all its threads call this); the last of
+// the unit's joins them, in their order.
+template <typename Fmt, int THREADS, int ROWS, int DT>
+__device__ inline void join(const Args& a, const Piece& p, const Share& share, int64_t pos, int D) {
+    __shared__ uint32_t s_arrived;
+    constexpr int BATCH = 8;  // parts in flight
+    const int tid = int(threadIdx.x);
+    const int64_t u0 = pos - p.t0, w0 = share.owner(u0), w1 = share.owner(u0 + p.tiles - 1);
+    wait_memory();
+    __syncthreads();
+    if (tid == 0) s_arrived = arrive(&a.counters[w0]);
+    __syncthreads();
+    if (s_arrived != uint32_t(w1 - w0)) return;
+    const int count = int(w1 - w0) + 1;
+    const int first_slot = 2 * int(w0) + (share.begin(w0) == u0 ? 0 : 1);
+    const auto stats = buffer_of(a.stats, a.stats_bytes), parts = buffer_of(a.parts, a.parts_bytes);
+    for (int i = tid; i < p.rows * (DT / 4); i += THREADS) {
+        const int row = i / (DT / 4), d = i % (DT / 4) * 4;
+        if (d >= D) continue;
+        float most = kNegInf, total = 0.0f;
+        f32x4_t o = {0, 0, 0, 0};
+        for (int x0 = 0; x0 < count; x0 += BATCH) {
+            u32x2_t st[BATCH];
+            chunk_t part[BATCH];
+#pragma unroll
+            for (int x = 0; x < BATCH; ++x) {
+                const int k = x0 + x < count ? x0 + x : count - 1;
+                const uint32_t at = uint32_t(k ? 2 * (int(w0) + k) : first_slot) * ROWS + row;
+                st[x] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(stats, int(at * 8u), 0, kDeviceScope));
+                part[x] = __builtin_bit_cast(chunk_t, __builtin_amdgcn_raw_buffer_load_b128(parts, int((at * DT + d) * 4u), 0, kDeviceScope));
+            }
+            float now = most;
+#pragma unroll
+            for (int x = 0; x < BATCH; ++x) now = fmaxf(now, __uint_as_float(st[x].x));
+            const float f = rescale(most, now);
+            o *= f;
+            total *= f;
+#pragma unroll
+            for (int x = 0; x < BATCH; ++x) {
+                if (x0 + x >= count) continue;
+                const float g = rescale(__uint_as_float(st[x].x), now), s = __uint_as_float(st[x].y);
+                o += __builtin_bit_cast(f32x4_t, part[x]) * g;
+                total += s == s ? s * g : s;
+            }
+            most = now;
+        }
+        write_row<Fmt>(a, p, row, d, D, o, total);
+    }
+    if (tid == 0) __hip_atomic_store(&a.counters[w0], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Rows of one workgroup, of the kernel that serves `rows` rows of a kv head.
+inline int padded_dim(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
+
+hipError_t launch_wide(const Args& a, int rows);  // tree_attention_wide.hip: bf16
+
+}  // namespace attention
+}  // namespace osd

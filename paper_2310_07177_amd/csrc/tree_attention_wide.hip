@@ -1,0 +1,295 @@
+// tree_attention_wide.hip -- osd_tree_attention of many bf16 rows: eight waves of 32
+// rows each read keys and values from LDS, where they arrive directly from memory.
+#include "tree_attention.hpp"
+
+namespace osd {
+namespace attention {
+namespace {
+
+constexpr int kWaves = 8;
+constexpr int kThreads = kWaves * kWave;
+constexpr int kPageWindow = 512;  // pages looked up at once
+
+// 16 bytes a lane from memory to LDS at `to` (uniform) + 16 * lane, without a register on
+// the way.  Counted in vmcnt; the compiler does not know of it, so that reads of LDS
+// wait for it only where wait_stage() says so.
+__device__ inline void load_lds(const char* from, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+}
+// The transposing read: 16 lanes give the places of 4 keys' pieces of 16 elements (8 bytes
+// a lane, four lanes a key) and get an element of the 4 keys each.
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+__device__ inline u32x2_t transposed(const char* at) {
+    return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                           (__attribute__((address_space(3))) s16x4_t*)(const_cast<char*>(at))));
+}
+template <int LEFT>
+__device__ inline void wait_stage() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
+
+// WR waves share the rows, WK = 8 / WR the keys of a stage.  The ring of stages in LDS
+// is filled NST - 1 ahead.  A row's 16-byte chunks lie permuted (chunk ^ key), so
+// that 16 lanes that read one chunk of 16 keys meet 16 different banks; the DMA
+// writes lanes one after another, so the permutation is in what they read.
+template <int DT, int WR>
+struct Shape {
+    static constexpr int WK = kWaves / WR, STAGE = WK == 4 ? 128 : 64, SUB = STAGE / (32 * WK);
+    static constexpr int MT = DT == 256 ? 1 : 2;  // row tiles of a wave: its sums fill half of its registers
+    static constexpr int ROWS = 16 * MT * WR, PITCH = DT + 4;
+    static constexpr int TILE_BYTES = STAGE * DT * 2;  // of K, and of V
+    static constexpr int NST = TILE_BYTES > 16384 ? 2 : 3;
+    static constexpr int RING = NST * 2 * TILE_BYTES, MERGE = kWaves * 16 * PITCH * 4;
+    static constexpr int LDS = RING > MERGE ? RING : MERGE;
+    static constexpr int LOADS = TILE_BYTES / 1024 / kWaves;  // of K, and of V, of a wave for a stage
+};
+
+template <int DT, int WR, bool FULL>
+__global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
+    using Ops = Bf16Ops;
+    using Fmt = BF16;
+    using S = Shape<DT, WR>;
+    constexpr int MT = S::MT, ES = 2;
+    using R = Rows<Ops, DT, MT, 1>;
+    constexpr int CHUNKS = R::CHUNKS, KT = R::KT;
+    constexpr int WK = S::WK, STAGE = S::STAGE, ROWS = S::ROWS, PITCH = S::PITCH, CPR = DT / 8;
+    const TreeAttentionLaunch& L = a.L;
+    const int tid = int(threadIdx.x), lane = tid & (kWave - 1), col = lane & 15, grp = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave), wr = wave % WR, wk = wave / WR;
+    const int D = FULL ? DT : L.head_dim;
+
+    extern __shared__ int s_tiles[];  // [B + 1]
+    __shared__ __attribute__((aligned(1024))) char s_ring[S::LDS];
+    __shared__ float s_stat[kWaves][16 * MT][2];
+    __shared__ uint64_t s_sees[ROWS];
+    __shared__ int s_flags[kWaves];
+    __shared__ int s_page[kPageWindow];
+    float(*s_acc)[16][PITCH] = reinterpret_cast<float(*)[16][PITCH]>(s_ring);
+    const uint32_t ring = uint32_t(uintptr_t((__attribute__((address_space(3))) char*)s_ring));
+
+    const Share share = divide<kThreads, STAGE>(a, s_tiles);
+    const int64_t w = int64_t(blockIdx.x);
+    if (w >= share.W) return;
+    const int64_t first = share.begin(w), end = share.begin(w + 1);
+    // XOR of a row's chunks, of period 16: rows of 128 bytes lie two to 64 banks.
+    const auto swizzle = [](int key) { return DT == 64 ? (key >> 1) & 7 : key & 15; };
+
+    for (int64_t pos = first; pos < end;) {
+        const Piece p = find_piece<ROWS>(a, s_tiles, pos, end);
+        const int len = p.seq.len, T = p.T;
+        chunk_t q[MT][CHUNKS];
+        R rows;
+        rows.clear();
+        bool bad = p.seq.state == 2;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) load_queries<Ops, CHUNKS, FULL>(a, p, (wr * MT + mt) * 16 + col, D, q[mt]);
+        if (p.t1 * STAGE > len && T > 0) {
+            bool tree;
+            const uint64_t all = wave_ancestors(L.parent ? L.parent + int64_t(p.b) * L.N : nullptr, p.seq.n, &tree);
+            bad = bad || !tree;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const int node = (p.row0 + (wr * MT + mt) * 16 + col) / a.group;
+                rows.sees[mt] = uint64_t(__shfl(static_cast<unsigned long long>(all), node & (kWave - 1)));
+            }
+        }
+
+        // The pages from page0 on; a stage's keys behind the last stand for the last.
+        const int stages = T > 0 ? p.t1 - p.t0 : 0;
+        int page0 = 0, page_end = 0;
+        const auto page_of = [&](int j) { return int((uint64_t(uint32_t(j)) * L.pages.magic) >> L.pages.shift); };
+        auto look = [&](int st) {  // uniform: the stage's pages are in the window
+            int j1 = (p.t0 + st + 1) * STAGE - 1;
+            j1 = j1 < T ? j1 : T - 1;
+            if (page_of(j1) < page_end) return;
+            page0 = page_of((p.t0 + st) * STAGE);
+            page_end = page0 + kPageWindow;
+            __syncthreads();
+            const int last = page_of(T - 1);
+            if (page0 + tid <= last) {
+                int page = L.pages.table[int64_t(p.b) * L.pages.table_len + page0 + tid];
+                if (uint32_t(page) >= uint32_t(L.pages.pages)) {
+                    bad = true;
+                    page = 0;
+                }
+                s_page[tid] = page;
+            }
+            __syncthreads();
+        };
+        static_assert(kThreads == kPageWindow, "a page for each thread");
+        auto issue = [&](int st) {
+            look(st);
+            const uint32_t to = ring + uint32_t(st % S::NST) * (2 * S::TILE_BYTES);
+#pragma unroll
+            for (int x = 0; x < S::LOADS; ++x) {
+                const int at = (wave * S::LOADS + x) * kWave + lane, key = at / CPR;
+                int chunk = (at % CPR) ^ swizzle(key);
+                if (!FULL && chunk * 8 >= D) chunk = 0;
+                int j = (p.t0 + st) * STAGE + key;
+                j = j < T ? j : T - 1;
+                const int in = page_of(j);
+                const int64_t from = int64_t(s_page[in - page0]) * L.pages.page_bytes + int64_t(p.h) * L.pages.head_bytes +
+                                     int64_t(j - in * L.pages.page_size) * (D * ES) + chunk * 16;
+                const uint32_t unit = to + uint32_t(wave * S::LOADS + x) * 1024u;
+                load_lds(L.k_cache + from, unit);
+                load_lds(L.v_cache + from, unit + S::TILE_BYTES);
+            }
+        };
+        __syncthreads();  // the ring is free
+        for (int st = 0; st < S::NST - 1 && st < stages; ++st) issue(st);
+
+        auto take = [&](int st, int sub, auto tail) {
+            constexpr bool TAIL = decltype(tail)::value;
+            const int k0 = (sub * WK + wk) * 32, j0 = (p.t0 + st) * STAGE + k0;
+            const char* k_row = s_ring + (st % S::NST) * (2 * S::TILE_BYTES) + (k0 + col) * (DT * ES);
+            // (A chunk's place is a XOR of the lane's part and a constant; computed each time, as all of
+            // them together would hold 30 registers.)
+            int k_lane = (grp ^ swizzle(col)) * 16;
+            const int from = grp * 4 + (col >> 2);  // the key whose piece of V this lane reads for the others
+            const char* v_row = s_ring + (st % S::NST) * (2 * S::TILE_BYTES) + S::TILE_BYTES + (k0 + from) * (DT * ES) + (col & 1) * 8;
+            int v_lane = (((col & 3) >> 1) ^ swizzle(from)) * 16;
+            asm volatile("" : "+v"(k_lane), "+v"(v_lane));
+            f32x4_t s[MT][KT];
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) s[mt][kt] = f32x4_t{0, 0, 0, 0};
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) {
+                    if (!FULL && c * Ops::kChunk >= D) continue;
+                    chunk_t k = *reinterpret_cast<const chunk_t*>(k_row + kt * 16 * (DT * ES) + (k_lane ^ c * 64));
+                    if (!FULL && c * Ops::kChunk + grp * 8 >= D) k = chunk_t{0, 0, 0, 0};
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) s[mt][kt] = Ops::qk(k, q[mt][c], s[mt][kt]);
+                }
+            }
+            typename Ops::Probs pr[MT];
+            rows.template soften<TAIL>(s, a.c2, j0, p.seq, pr);
+            // Pairs of halves of the lane's 8 keys that are keys.
+            chunk_t in;
+            if constexpr (TAIL) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = j0 + (i / 2) * 16 + grp * 4 + (i & 1) * 2;
+                    in[i] = (j < T ? 0xFFFFu : 0u) | (j + 1 < T ? 0xFFFF0000u : 0u);
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < DT / 16; ++t) {
+                chunk_t v;
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) {
+                    const u32x2_t half = transposed(v_row + kt * 16 * (DT * ES) + (v_lane ^ t * 32));
+                    v[2 * kt] = half.x;
+                    v[2 * kt + 1] = half.y;
+                }
+                if constexpr (TAIL) {
+                    chunk_t clean;
+                    v &= in;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) clean[i] = Ops::pair_finite(v[i]);
+                    rows.odd = rows.odd || __any(clean[0] != v[0] || clean[1] != v[1] || clean[2] != v[2] || clean[3] != v[3]);
+                    v = clean;
+                }
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) rows.acc[mt][t][0] = Ops::qk(v, pr[mt].x, rows.acc[mt][t][0]);
+            }
+        };
+        for (int st = 0; st < stages; ++st) {
+            if (S::NST > 2 && st + S::NST - 2 < stages) wait_stage<(S::NST - 2) * 2 * S::LOADS>();
+            else wait_stage<0>();
+            if (st + S::NST - 1 < stages) issue(st + S::NST - 1);
+#pragma unroll
+            for (int sub = 0; sub < S::SUB; ++sub) {
+                const int j0 = (p.t0 + st) * STAGE + (sub * WK + wk) * 32;
+                if (j0 >= T) continue;
+                if (j0 + 32 <= len) take(st, sub, no_t{});
+                else take(st, sub, yes_t{});
+            }
+        }
+        __syncthreads();
+
+        // The sums of the waves that share rows, relative to the largest of their maxima.
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const float sum = rows_sum(rows.sum[mt]);
+            if (grp == 0) {
+                s_stat[wave][mt * 16 + col][0] = rows.top[mt];
+                s_stat[wave][mt * 16 + col][1] = sum;
+                if (wk == 0) s_sees[(wr * MT + mt) * 16 + col] = rows.sees[mt];
+            }
+        }
+        bad = __any(bad);
+        if (lane == 0) s_flags[wave] = (bad ? 1 : 0) | (rows.odd ? 2 : 0);
+        __syncthreads();
+        int flags = 0;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) flags |= s_flags[i];
+        const bool whole = p.whole();
+        const int64_t slot = 2 * w + (pos == first ? 0 : 1);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            float all = kNegInf;
+#pragma unroll
+            for (int i = 0; i < WK; ++i) all = fmaxf(all, s_stat[i * WR + wr][mt * 16 + col][0]);
+            rows.template store<PITCH>(mt, rescale(rows.top[mt], all), s_acc[wave][col]);
+            __syncthreads();
+            for (int i = tid; i < WR * 16 * (DT / 4); i += kThreads) {
+                const int rr = i / (DT / 4), d = i % (DT / 4) * 4, x = rr / 16, r = rr % 16, row = (x * MT + mt) * 16 + r;
+                if (row >= p.rows || d >= D) continue;
+                f32x4_t o = *reinterpret_cast<const f32x4_t*>(&s_acc[x][r][d]);
+                float most = s_stat[x][mt * 16 + r][0], total = 0.0f;
+#pragma unroll
+                for (int y = 1; y < WK; ++y) {
+                    o += *reinterpret_cast<const f32x4_t*>(&s_acc[y * WR + x][r][d]);
+                    most = fmaxf(most, s_stat[y * WR + x][mt * 16 + r][0]);
+                }
+                if ((flags & 2) && row < p.live) add_odd<Fmt>(L, p.b, p.h, d, len, T, len / 32 * 32, s_sees[row], o);
+#pragma unroll
+                for (int y = 0; y < WK; ++y) {
+                    const float s = s_stat[y * WR + x][mt * 16 + r][1];
+                    total += s == s ? s * rescale(s_stat[y * WR + x][mt * 16 + r][0], most) : s;
+                }
+                if (flags & 1) total = __builtin_nanf("");
+                if (whole) write_row<Fmt>(a, p, row, d, D, o, total);
+                else post_part<ROWS, DT>(a, slot, row, d, o, most, total);
+            }
+            __syncthreads();
+        }
+        if (!whole) join<Fmt, kThreads, ROWS, DT>(a, p, share, pos, D);
+        pos += p.t1 - p.t0;
+    }
+}
+
+template <int DT, int WR>
+hipError_t launch_shape(Args& a) {
+    const TreeAttentionLaunch& L = a.L;
+    constexpr int ROWS = Shape<DT, WR>::ROWS;
+    a.blocks = (L.N * a.group + ROWS - 1) / ROWS;
+    const int grid = L.cus < kMaxGroups / 2 ? L.cus : kMaxGroups / 2;
+    const size_t lds = size_t(L.B + 1) * sizeof(int);
+    if (L.head_dim == DT)
+        return launch_kernel(&tree_attention_wide<DT, WR, true>, dim3(grid), dim3(kThreads), lds, L.stream, a);
+    return launch_kernel(&tree_attention_wide<DT, WR, false>, dim3(grid), dim3(kThreads), lds, L.stream, a);
+}
+
+template <int DT>
+hipError_t launch_dim(Args& a, int rows) {
+    if constexpr (DT < 256)
+        if (rows <= Shape<DT, 2>::ROWS) return launch_shape<DT, 2>(a);
+    return rows <= Shape<DT, 4>::ROWS ? launch_shape<DT, 4>(a) : launch_shape<DT, 8>(a);
+}
+
+}  // namespace
+
+hipError_t launch_wide(const Args& args, int rows) {
+    Args a = args;
+    switch (padded_dim(a.L.head_dim)) {
+        case 64: return launch_dim<64>(a, rows);
+        case 128: return launch_dim<128>(a, rows);
+        default: return launch_dim<256>(a, rows);
+    }
+}
+
+}  // namespace attention
+}  // namespace osd
