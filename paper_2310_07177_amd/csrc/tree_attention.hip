@@ -26,7 +26,8 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
     constexpr int ES = R::ES, KT = R::KT, STEP = 16 * KT, TILE = STEP * kWaves;
     constexpr int CHUNKS = R::CHUNKS, VW = R::VW, BW = R::BW, BLOCKS = R::BLOCKS, KEYS = R::KEYS;
     constexpr int ROWS = 16 * MT, PITCH = DT + 4;
-    const int tid = int(threadIdx.x), lane = tid & (kWave - 1), wave = tid / kWave, col = lane & 15, grp = lane >> 4;
+    const int tid = int(threadIdx.x), lane = tid & (kWave - 1), col = lane & 15, grp = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int D = GEN ? L.head_dim : DT;
     const int row_bytes = GEN ? L.pages.row_bytes : DT * ES;
 
@@ -46,8 +47,9 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
         const int len = p.seq.len, T = p.T;
         chunk_t q[MT][CHUNKS];
         R rows;
-        rows.clear();
         bool bad = p.seq.state == 2;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) rows.sees[mt] = 0;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) load_queries<Ops, CHUNKS, !GEN>(a, p, mt * 16 + col, D, q[mt]);
         if (p.t1 * TILE > len && T > 0) {
@@ -128,15 +130,7 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
         if (steps > 0 && (p.t1 - 1) * TILE + wave * STEP >= T) --steps;
         steps = __builtin_amdgcn_readfirstlane(steps);
         constexpr int PERIOD = GEN ? 1 : kWave / KT;
-        if (steps > 0) {
-            fill(0);
-            load_k(0);
-            load_v(0);
-        }
-        auto take = [&](int step, auto tail) {
-            constexpr bool TAIL = decltype(tail)::value;
-            const int j0 = (p.t0 + step) * TILE + wave * STEP;
-            f32x4_t s[MT][KT];
+        auto scores = [&](f32x4_t (&s)[MT][KT]) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -145,29 +139,58 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
 #pragma unroll
                     for (int c = 0; c < CHUNKS; ++c) s[mt][kt] = Ops::qk(k[kt][c], q[mt][c], s[mt][kt]);
                 }
+        };
+        auto take = [&](int step, auto tail) {
+            constexpr bool TAIL = decltype(tail)::value;
+            const int j0 = (p.t0 + step) * TILE + wave * STEP;
+            f32x4_t s[MT][KT];
+            scores(s);
             // The next step's keys while this one's probabilities are formed.
             const bool more = step + 1 < steps;
             if (more) {
                 if ((step + 1) % PERIOD == 0) fill(step + 1);
                 load_k(step + 1);
             }
+            if constexpr (TAIL) rows.mask(s, j0, p.seq);
             typename Ops::Probs pr[MT];
-            rows.template soften<TAIL>(s, a.c2, j0, p.seq, pr);
+            rows.template soften<TAIL>(s, a.c2, pr);
             if constexpr (TAIL) rows.guard(v, j0, T);
             rows.add(v, pr);
             if (more) load_v(step + 1);
         };
-        int step = 0;
-        for (; step < steps && (p.t0 + step) * TILE + wave * STEP + STEP <= len; ++step) take(step, no_t{});
-        for (; step < steps; ++step) take(step, yes_t{});
+        rows.clear();
+        for (bool again = false; steps > 0; again = true) {
+            fill(0);
+            load_k(0);
+            load_v(0);
+            float most[MT];
+            if (!again) {
+                f32x4_t s[MT][KT];
+                scores(s);
+                if (p.t0 * TILE + wave * STEP + STEP > len) rows.mask(s, p.t0 * TILE + wave * STEP, p.seq);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) most[mt] = kNegInf;
+                R::largest(s, most);
+            } else {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) most[mt] = rows.seen[mt];
+                rows.clear();
+            }
+            rows.refer(most, a.c2);
+            int step = 0;
+            for (; step < steps && (p.t0 + step) * TILE + wave * STEP + STEP <= len; ++step) take(step, no_t{});
+            for (; step < steps; ++step) take(step, yes_t{});
+            if (again || rows.served(a.c2)) break;
+        }
 
-        // The four waves' sums, relative to the largest of their maxima.
+        // The four waves' sums, relative to the largest of their references.
         bad = __any(bad);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             const float sum = bad ? __builtin_nanf("") : rows_sum(rows.sum[mt]);
+            if (sum == 0.0f || steps <= 0) rows.ref[mt] = kNegInf;
             if (grp == 0) {
-                s_stat[wave][mt * 16 + col][0] = rows.top[mt];
+                s_stat[wave][mt * 16 + col][0] = rows.ref[mt];
                 s_stat[wave][mt * 16 + col][1] = sum;
                 if (wave == 0) s_sees[mt * 16 + col] = rows.sees[mt];
             }
@@ -182,7 +205,7 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
             float all = kNegInf;
 #pragma unroll
             for (int i = 0; i < kWaves; ++i) all = fmaxf(all, s_stat[i][mt * 16 + col][0]);
-            rows.template store<PITCH>(mt, rescale(rows.top[mt], all), s_acc[wave][col]);
+            rows.template store<PITCH>(mt, rescale(rows.ref[mt], all), s_acc[wave][col]);
             __syncthreads();
             for (int i = tid; i < 16 * (DT / 4); i += kThreads) {
                 const int rr = i / (DT / 4), d = i % (DT / 4) * 4, row = mt * 16 + rr;
@@ -224,11 +247,9 @@ hipError_t launch_tiles(Args& a) {
 // Rows of a workgroup.  fp32 keeps to 32 (16 of DT = 256): its matrix products are what
 // bounds it from there on.
 int block_rows(int rows, int DT, int dtype) {
-    if (rows <= 16 || (DT == 256 && dtype != OSD_BF16)) return 16;
-    if (rows <= 32 && DT < 256) return 32;
-    if (dtype != OSD_BF16) return 32;
-    if (DT == 256) return rows <= 64 ? 64 : 128;
-    return rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+    if (rows <= 16) return 16;
+    if (dtype != OSD_BF16) return DT == 256 ? 16 : 32;
+    return rows <= 64 ? 64 : rows <= 128 || DT == 256 ? 128 : 256;
 }
 
 struct Workspace {
@@ -245,7 +266,7 @@ Workspace layout(int rows, int DT, int dtype) {
 
 template <typename Ops, int DT>
 hipError_t launch_dim(Args& a, int rows) {
-    if constexpr (DT < 256)
+    if constexpr (DT < 256 && Ops::Fmt::kBytes == 4)
         if (rows > 16) return launch_tiles<Ops, DT, 2>(a);
     return launch_tiles<Ops, DT, 1>(a);
 }

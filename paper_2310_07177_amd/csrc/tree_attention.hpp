@@ -10,7 +10,9 @@
 // them: a lane holds 4 keys of every 16 for one row, and as the order of keys
 // within a product is free, these are its 8 (bf16) or 1 (fp32) of the second's.
 // K is read as the first product's A operand, 16 bytes a lane.  Softmax in one pass:
-// running maximum and sum in fp32, rescaled when a step raises a maximum.
+// the exponents are relative to a reference that holds for all of a wave's keys (its
+// first step's largest score), not to a running maximum, so that no step waits for the
+// other lanes' scores or rescales sums.
 #pragma once
 
 #include "cache_device.hpp"
@@ -277,61 +279,77 @@ struct Rows {
     static constexpr int ES = Ops::Fmt::kBytes, KT = Ops::kKT, KEYS = 4 * KT, CHUNKS = DT / Ops::kChunk;
     static constexpr int VW = VW_, BW = 16 * VW, BLOCKS = DT / BW;
     f32x4_t acc[MT][BLOCKS][VW];
-    float top[MT], sum[MT];
-    uint64_t sees[MT];  // the tree's nodes that a row sees
-    bool odd;           // a value of the tree's steps that is not finite
+    float ref[MT], sum[MT];  // every exponent's reference, and the lane's sum
+    float seen[MT];          // the lane's largest score so far
+    uint64_t sees[MT];       // the tree's nodes that a row sees
+    bool odd;                // a value of the tree's steps that is not finite
 
     __device__ void clear() {
         odd = false;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            top[mt] = kNegInf;
+            seen[mt] = kNegInf;
             sum[mt] = 0.0f;
-            sees[mt] = 0;
 #pragma unroll
             for (int n = 0; n < BLOCKS; ++n)
 #pragma unroll
                 for (int t = 0; t < VW; ++t) acc[mt][n][t] = f32x4_t{0, 0, 0, 0};
         }
     }
-    // From the scores of the keys from j0 on to their probabilities.  TAIL: there are
-    // keys that not every row sees, or none.
-    template <bool TAIL>
-    __device__ void soften(f32x4_t (&s)[MT][KT], float c2, int j0, const Seq& seq, typename Ops::Probs (&p)[MT]) {
-        const int grp = (int(threadIdx.x) & (kWave - 1)) >> 4;
+    // What exponents are taken relative to: the largest of some scores (the first
+    // step's), 0 where they have none.
+    __device__ void refer(const float (&most)[MT], float c2) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            bool on[KEYS];
-            float best = kNegInf;
-            if constexpr (TAIL) {
+            const float m = rows_max(most[mt]);
+            ref[mt] = m == kNegInf ? 0.0f : m * c2;
+        }
+    }
+    // Whether the reference served: p up to 2^32 and sums of them are as exact as p up to
+    // 1 (no scale is lost in fp32 or bf16), so steps need not agree on a maximum; only
+    // where a score turned out further away are all keys taken again, now relative to
+    // the largest.
+    __device__ bool served(float c2) const {
+        bool ok = true;
 #pragma unroll
-                for (int i = 0; i < KEYS; ++i) {
-                    const int j = j0 + (i / 4) * 16 + grp * 4 + (i & 3) - seq.len;
-                    on[i] = j < 0 || (j < seq.n && (sees[mt] >> (j & 63) & 1));
-                    if (!on[i]) s[mt][i / 4][i & 3] = kNegInf;
-                }
+        for (int mt = 0; mt < MT; ++mt) {
+            const float m = rows_max(seen[mt]);
+            ok = ok && (m == kNegInf || fabsf(m * c2 - ref[mt]) <= 32.0f);
+        }
+        return __all(ok);
+    }
+    // Where keys that not every row sees begin, j0 their first step's.
+    __device__ void mask(f32x4_t (&s)[MT][KT], int j0, const Seq& seq) const {
+        const int grp = (int(threadIdx.x) & (kWave - 1)) >> 4;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i) {
+                const int j = j0 + (i / 4) * 16 + grp * 4 + (i & 3) - seq.len;
+                // (Without branches: hipcc lost the score where lanes parted here.)
+                const uint32_t on = uint32_t(j < 0) | (uint32_t(j < seq.n) & uint32_t(sees[mt] >> (j & 63)));
+                s[mt][i / 4][i & 3] = (on & 1u) != 0u ? s[mt][i / 4][i & 3] : kNegInf;
             }
+    }
+    __device__ static void largest(const f32x4_t (&s)[MT][KT], float (&most)[MT]) {
 #pragma unroll
-            for (int i = 0; i < KEYS; ++i) best = fmaxf(best, s[mt][i / 4][i & 3]);
-            best = fmaxf(rows_max(best) * c2, top[mt]);
-            if (__any(best > top[mt])) {
-                const float f = rescale(top[mt], best);
-                sum[mt] *= f;
+        for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                for (int n = 0; n < BLOCKS; ++n)
+            for (int i = 0; i < KEYS; ++i) most[mt] = fmaxf(most[mt], s[mt][i / 4][i & 3]);
+    }
+    // Scores to probabilities (times 2^-ref).  TAIL: masked ones are -inf, and their probability is 0
+    // (also with c2 = 0).
+    template <bool TAIL>
+    __device__ void soften(const f32x4_t (&s)[MT][KT], float c2, typename Ops::Probs (&p)[MT]) {
+        largest(s, seen);
 #pragma unroll
-                    for (int t = 0; t < VW; ++t)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[mt][n][t][e] *= f;
-                top[mt] = best;
-            }
-            // (The same rounded product c2 * maximum is in every exponent, so its rounding cancels.)
-            const float base = top[mt] == kNegInf ? 0.0f : top[mt];
+        for (int mt = 0; mt < MT; ++mt) {
             float x[KEYS];
 #pragma unroll
             for (int i = 0; i < KEYS; ++i) {
-                x[i] = exp2_fast(fmaf(s[mt][i / 4][i & 3], c2, -base));
-                if constexpr (TAIL) x[i] = on[i] ? x[i] : 0.0f;
+                const float score = s[mt][i / 4][i & 3];
+                x[i] = exp2_fast(fmaf(score, c2, -ref[mt]));
+                if constexpr (TAIL) x[i] = score == kNegInf ? 0.0f : x[i];
                 sum[mt] += x[i];
             }
             p[mt] = Ops::probs(x);
@@ -433,12 +451,66 @@ __device__ inline void post_part(const Args& a, int64_t slot, int row, int d, f3
                                               buffer_of(a.stats, a.stats_bytes), int(uint32_t(at) * 8u), 0, kDeviceScope);
 }
 
+// ITEMS times four values of rows, from PIECES parts in flight each.
+template <typename Fmt, int THREADS, int ROWS, int DT, int ITEMS, int PIECES>
+__device__ inline void join_parts(const Args& a, const Piece& p, int first_slot, int w0, int count, int D) {
+    const auto stats = buffer_of(a.stats, a.stats_bytes), parts = buffer_of(a.parts, a.parts_bytes);
+    const int items = p.rows * (DT / 4);
+    for (int i0 = int(threadIdx.x); i0 < items; i0 += THREADS * ITEMS) {
+        float most[ITEMS], total[ITEMS];
+        f32x4_t o[ITEMS];
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) most[k] = kNegInf, total[k] = 0.0f, o[k] = f32x4_t{0, 0, 0, 0};
+        for (int x0 = 0; x0 < count; x0 += PIECES) {
+            u32x2_t st[ITEMS][PIECES];
+            chunk_t part[ITEMS][PIECES];
+#pragma unroll
+            for (int x = 0; x < PIECES; ++x)
+#pragma unroll
+                for (int k = 0; k < ITEMS; ++k) {
+                    // (What is not there reads as zeros, and is not used.)
+                    const int i = i0 + k * THREADS, row = i / (DT / 4), d = i % (DT / 4) * 4;
+                    const bool in = i < items && x0 + x < count && d < D;
+                    const uint32_t at = uint32_t(x0 + x ? 2 * (w0 + x0 + x) : first_slot) * ROWS + row;
+                    st[k][x] = u32x2_t{0, 0};
+                    part[k][x] = chunk_t{0, 0, 0, 0};
+                    if (in) {
+                        st[k][x] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(stats, int(at * 8u), 0, kDeviceScope));
+                        part[k][x] = __builtin_bit_cast(chunk_t, __builtin_amdgcn_raw_buffer_load_b128(parts, int((at * DT + d) * 4u), 0, kDeviceScope));
+                    }
+                }
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) {
+                float now = most[k];
+#pragma unroll
+                for (int x = 0; x < PIECES; ++x)
+                    if (x0 + x < count) now = fmaxf(now, __uint_as_float(st[k][x].x));
+                const float f = rescale(most[k], now);
+                o[k] *= f;
+                total[k] *= f;
+#pragma unroll
+                for (int x = 0; x < PIECES; ++x) {
+                    if (x0 + x >= count) continue;
+                    const float g = rescale(__uint_as_float(st[k][x].x), now), s = __uint_as_float(st[k][x].y);
+                    o[k] += __builtin_bit_cast(f32x4_t, part[k][x]) * g;
+                    total[k] += s == s ? s * g : s;
+                }
+                most[k] = now;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            const int i = i0 + k * THREADS, row = i / (DT / 4), d = i % (DT / 4) * 4;
+            if (i < items && d < D) write_row<Fmt>(a, p, row, d, D, o[k], total[k]);
+        }
+    }
+}
+
 // A workgroup has posted its part of a unit (all its threads call this); the last of
 // the unit's joins them, in their order.
 template <typename Fmt, int THREADS, int ROWS, int DT>
 __device__ inline void join(const Args& a, const Piece& p, const Share& share, int64_t pos, int D) {
     __shared__ uint32_t s_arrived;
-    constexpr int BATCH = 8;  // parts in flight
     const int tid = int(threadIdx.x);
     const int64_t u0 = pos - p.t0, w0 = share.owner(u0), w1 = share.owner(u0 + p.tiles - 1);
     wait_memory();
@@ -448,39 +520,10 @@ __device__ inline void join(const Args& a, const Piece& p, const Share& share, i
     if (s_arrived != uint32_t(w1 - w0)) return;
     const int count = int(w1 - w0) + 1;
     const int first_slot = 2 * int(w0) + (share.begin(w0) == u0 ? 0 : 1);
-    const auto stats = buffer_of(a.stats, a.stats_bytes), parts = buffer_of(a.parts, a.parts_bytes);
-    for (int i = tid; i < p.rows * (DT / 4); i += THREADS) {
-        const int row = i / (DT / 4), d = i % (DT / 4) * 4;
-        if (d >= D) continue;
-        float most = kNegInf, total = 0.0f;
-        f32x4_t o = {0, 0, 0, 0};
-        for (int x0 = 0; x0 < count; x0 += BATCH) {
-            u32x2_t st[BATCH];
-            chunk_t part[BATCH];
-#pragma unroll
-            for (int x = 0; x < BATCH; ++x) {
-                const int k = x0 + x < count ? x0 + x : count - 1;
-                const uint32_t at = uint32_t(k ? 2 * (int(w0) + k) : first_slot) * ROWS + row;
-                st[x] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(stats, int(at * 8u), 0, kDeviceScope));
-                part[x] = __builtin_bit_cast(chunk_t, __builtin_amdgcn_raw_buffer_load_b128(parts, int((at * DT + d) * 4u), 0, kDeviceScope));
-            }
-            float now = most;
-#pragma unroll
-            for (int x = 0; x < BATCH; ++x) now = fmaxf(now, __uint_as_float(st[x].x));
-            const float f = rescale(most, now);
-            o *= f;
-            total *= f;
-#pragma unroll
-            for (int x = 0; x < BATCH; ++x) {
-                if (x0 + x >= count) continue;
-                const float g = rescale(__uint_as_float(st[x].x), now), s = __uint_as_float(st[x].y);
-                o += __builtin_bit_cast(f32x4_t, part[x]) * g;
-                total += s == s ? s * g : s;
-            }
-            most = now;
-        }
-        write_row<Fmt>(a, p, row, d, D, o, total);
-    }
+    // A read takes about 2 us, so as many as registers allow are in flight.
+    if (count <= 2) join_parts<Fmt, THREADS, ROWS, DT, 8, 2>(a, p, first_slot, int(w0), count, D);
+    else if (count <= 4) join_parts<Fmt, THREADS, ROWS, DT, 4, 4>(a, p, first_slot, int(w0), count, D);
+    else join_parts<Fmt, THREADS, ROWS, DT, 2, 8>(a, p, first_slot, int(w0), count, D);
     if (tid == 0) __hip_atomic_store(&a.counters[w0], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 

@@ -28,28 +28,28 @@ __device__ inline void wait_stage() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
 }
 
-// WR waves share the rows, WK = 8 / WR the keys of a stage.  The ring of stages in LDS
-// is filled NST - 1 ahead.  A row's 16-byte chunks lie permuted (chunk ^ key), so
-// that 16 lanes that read one chunk of 16 keys meet 16 different banks; the DMA
-// writes lanes one after another, so the permutation is in what they read.
-template <int DT, int WR>
+// WR waves share the rows, 16 MT each, WK = 8 / WR the keys of a stage.  The ring of
+// stages in LDS is filled NST - 1 ahead.  A row's 16-byte chunks lie permuted
+// (chunk ^ key), so that 16 lanes that read one chunk of 16 keys meet 16 different
+// banks; the DMA writes lanes one after another, so the permutation is in what they
+// read.
+template <int DT, int WR, int MT>
 struct Shape {
-    static constexpr int WK = kWaves / WR, STAGE = WK == 4 ? 128 : 64, SUB = STAGE / (32 * WK);
-    static constexpr int MT = DT == 256 ? 1 : 2;  // row tiles of a wave: its sums fill half of its registers
+    static constexpr int WK = kWaves / WR, STAGE = DT == 256 ? 32 * WK : 64, SUB = STAGE / (32 * WK);
     static constexpr int ROWS = 16 * MT * WR, PITCH = DT + 4;
     static constexpr int TILE_BYTES = STAGE * DT * 2;  // of K, and of V
-    static constexpr int NST = TILE_BYTES > 16384 ? 2 : 3;
+    static constexpr int NST = TILE_BYTES > 16384 ? 2 : 4;
     static constexpr int RING = NST * 2 * TILE_BYTES, MERGE = kWaves * 16 * PITCH * 4;
     static constexpr int LDS = RING > MERGE ? RING : MERGE;
     static constexpr int LOADS = TILE_BYTES / 1024 / kWaves;  // of K, and of V, of a wave for a stage
 };
 
-template <int DT, int WR, bool FULL>
+template <int DT, int WR, int MT, bool FULL>
 __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
     using Ops = Bf16Ops;
     using Fmt = BF16;
-    using S = Shape<DT, WR>;
-    constexpr int MT = S::MT, ES = 2;
+    using S = Shape<DT, WR, MT>;
+    constexpr int ES = 2;
     using R = Rows<Ops, DT, MT, 1>;
     constexpr int CHUNKS = R::CHUNKS, KT = R::KT;
     constexpr int WK = S::WK, STAGE = S::STAGE, ROWS = S::ROWS, PITCH = S::PITCH, CPR = DT / 8;
@@ -79,8 +79,9 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
         const int len = p.seq.len, T = p.T;
         chunk_t q[MT][CHUNKS];
         R rows;
-        rows.clear();
         bool bad = p.seq.state == 2;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) rows.sees[mt] = 0;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) load_queries<Ops, CHUNKS, FULL>(a, p, (wr * MT + mt) * 16 + col, D, q[mt]);
         if (p.t1 * STAGE > len && T > 0) {
@@ -135,9 +136,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                 load_lds(L.v_cache + from, unit + S::TILE_BYTES);
             }
         };
-        __syncthreads();  // the ring is free
-        for (int st = 0; st < S::NST - 1 && st < stages; ++st) issue(st);
-
+        const bool alive = wr * MT * 16 < p.live;  // (of padding alone: a wave helps to fill the ring)
+        bool fresh = true;                         // no reference yet
         auto take = [&](int st, int sub, auto tail) {
             constexpr bool TAIL = decltype(tail)::value;
             const int k0 = (sub * WK + wk) * 32, j0 = (p.t0 + st) * STAGE + k0;
@@ -163,8 +163,17 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                     for (int mt = 0; mt < MT; ++mt) s[mt][kt] = Ops::qk(k, q[mt][c], s[mt][kt]);
                 }
             }
+            if constexpr (TAIL) rows.mask(s, j0, p.seq);
+            if (fresh) {
+                fresh = false;
+                float most[MT];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) most[mt] = kNegInf;
+                R::largest(s, most);
+                rows.refer(most, a.c2);
+            }
             typename Ops::Probs pr[MT];
-            rows.template soften<TAIL>(s, a.c2, j0, p.seq, pr);
+            rows.template soften<TAIL>(s, a.c2, pr);
             // Pairs of halves of the lane's 8 keys that are keys.
             chunk_t in;
             if constexpr (TAIL) {
@@ -195,31 +204,55 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                 for (int mt = 0; mt < MT; ++mt) rows.acc[mt][t][0] = Ops::qk(v, pr[mt].x, rows.acc[mt][t][0]);
             }
         };
-        for (int st = 0; st < stages; ++st) {
-            if (S::NST > 2 && st + S::NST - 2 < stages) wait_stage<(S::NST - 2) * 2 * S::LOADS>();
-            else wait_stage<0>();
-            if (st + S::NST - 1 < stages) issue(st + S::NST - 1);
+        rows.clear();
+        for (bool again = false;; again = true) {
+            __syncthreads();  // the ring is free
+            if (again) {
+                float most[MT];
 #pragma unroll
-            for (int sub = 0; sub < S::SUB; ++sub) {
-                const int j0 = (p.t0 + st) * STAGE + (sub * WK + wk) * 32;
-                if (j0 >= T) continue;
-                if (j0 + 32 <= len) take(st, sub, no_t{});
-                else take(st, sub, yes_t{});
+                for (int mt = 0; mt < MT; ++mt) most[mt] = rows.seen[mt];
+                rows.clear();
+                rows.refer(most, a.c2);
             }
+            page_end = 0;
+            for (int st = 0; st < S::NST - 1 && st < stages; ++st) issue(st);
+            for (int st = 0; st < stages; ++st) {
+                // This stage is there; the ones behind it may be on their way.
+                if (S::NST > 2 && st + 2 < stages) wait_stage<(S::NST > 2 ? 4 * S::LOADS : 0)>();
+                else if (S::NST > 2 && st + 1 < stages) wait_stage<(S::NST > 2 ? 2 * S::LOADS : 0)>();
+                else wait_stage<0>();
+                if (st + S::NST - 1 < stages) issue(st + S::NST - 1);
+#pragma unroll
+                for (int sub = 0; sub < S::SUB; ++sub) {
+                    const int j0 = (p.t0 + st) * STAGE + (sub * WK + wk) * 32;
+                    if (j0 >= T || !alive) continue;
+                    if (j0 + 32 <= len) take(st, sub, no_t{});
+                    else take(st, sub, yes_t{});
+                }
+            }
+            // All waves share the stages, so that one that needs them again has all go through them.
+            const bool ok = again || fresh || rows.served(a.c2);
+            if (lane == 0) s_flags[wave] = ok;
+            __syncthreads();
+            int all = 1;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) all &= s_flags[i];
+            if (all) break;
         }
-        __syncthreads();
 
-        // The sums of the waves that share rows, relative to the largest of their maxima.
+        // The sums of the waves that share rows, relative to the largest of their references.
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             const float sum = rows_sum(rows.sum[mt]);
+            if (sum == 0.0f || fresh) rows.ref[mt] = kNegInf;
             if (grp == 0) {
-                s_stat[wave][mt * 16 + col][0] = rows.top[mt];
+                s_stat[wave][mt * 16 + col][0] = rows.ref[mt];
                 s_stat[wave][mt * 16 + col][1] = sum;
                 if (wk == 0) s_sees[(wr * MT + mt) * 16 + col] = rows.sees[mt];
             }
         }
         bad = __any(bad);
+        __syncthreads();
         if (lane == 0) s_flags[wave] = (bad ? 1 : 0) | (rows.odd ? 2 : 0);
         __syncthreads();
         int flags = 0;
@@ -232,7 +265,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
             float all = kNegInf;
 #pragma unroll
             for (int i = 0; i < WK; ++i) all = fmaxf(all, s_stat[i * WR + wr][mt * 16 + col][0]);
-            rows.template store<PITCH>(mt, rescale(rows.top[mt], all), s_acc[wave][col]);
+            rows.template store<PITCH>(mt, rescale(rows.ref[mt], all), s_acc[wave][col]);
             __syncthreads();
             for (int i = tid; i < WR * 16 * (DT / 4); i += kThreads) {
                 const int rr = i / (DT / 4), d = i % (DT / 4) * 4, x = rr / 16, r = rr % 16, row = (x * MT + mt) * 16 + r;
@@ -261,23 +294,23 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
     }
 }
 
-template <int DT, int WR>
+template <int DT, int WR, int MT>
 hipError_t launch_shape(Args& a) {
     const TreeAttentionLaunch& L = a.L;
-    constexpr int ROWS = Shape<DT, WR>::ROWS;
+    constexpr int ROWS = Shape<DT, WR, MT>::ROWS;
     a.blocks = (L.N * a.group + ROWS - 1) / ROWS;
     const int grid = L.cus < kMaxGroups / 2 ? L.cus : kMaxGroups / 2;
     const size_t lds = size_t(L.B + 1) * sizeof(int);
     if (L.head_dim == DT)
-        return launch_kernel(&tree_attention_wide<DT, WR, true>, dim3(grid), dim3(kThreads), lds, L.stream, a);
-    return launch_kernel(&tree_attention_wide<DT, WR, false>, dim3(grid), dim3(kThreads), lds, L.stream, a);
+        return launch_kernel(&tree_attention_wide<DT, WR, MT, true>, dim3(grid), dim3(kThreads), lds, L.stream, a);
+    return launch_kernel(&tree_attention_wide<DT, WR, MT, false>, dim3(grid), dim3(kThreads), lds, L.stream, a);
 }
 
 template <int DT>
 hipError_t launch_dim(Args& a, int rows) {
-    if constexpr (DT < 256)
-        if (rows <= Shape<DT, 2>::ROWS) return launch_shape<DT, 2>(a);
-    return rows <= Shape<DT, 4>::ROWS ? launch_shape<DT, 4>(a) : launch_shape<DT, 8>(a);
+    if (rows <= 64) return launch_shape<DT, 4, 1>(a);
+    if constexpr (DT == 256) return launch_shape<DT, 8, 1>(a);
+    else return rows <= 128 ? launch_shape<DT, 4, 2>(a) : launch_shape<DT, 8, 2>(a);
 }
 
 }  // namespace
