@@ -1,6 +1,6 @@
 // tree_attention.hip -- osd_tree_attention: drafted tokens attend to the context
-// in the paged cache, to their ancestors and to themselves.  Few rows (and all of
-// fp32): keys and values go from memory to registers.  Of V a lane reads whole 16-byte
+// in the paged cache, to their ancestors and to themselves.  Up to 16 rows of a kv
+// head (single tokens): keys and values go from memory to registers.  Of V a lane reads whole 16-byte
 // pieces of the keys that it holds, and picks the halves of each pair of keys apart,
 // which is the transposition that the second product's A operand needs.
 #include "tree_attention.hpp"
@@ -13,13 +13,14 @@ using namespace attention;
 constexpr int kWaves = 4;  // of a workgroup: each takes its own keys of a tile
 constexpr int kThreads = kWaves * kWave;
 
-// DT: head_dim rounded up; MT: row tiles of 16; GEN: pages that end inside tiles of
+// DT: head_dim rounded up; GEN: pages that end inside tiles of
 // 16 keys, or head_dim < DT.  A step is 16 or 32 keys of a wave, a tile those of the
 // workgroup's four; the next step's keys and values are on their way while one is
 // worked on, 16 KB a wave of DT = 128.
-template <typename Ops, int DT, int MT, bool GEN>
+template <typename Ops, int DT, bool GEN>
 __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_kernel(Args a) {
     using Fmt = typename Ops::Fmt;
+    constexpr int MT = 1;
     using R = Rows<Ops, DT, MT, kPiece<Ops, DT>>;
     using Value = typename Ops::template Value<R::VW>;
     const TreeAttentionLaunch& L = a.L;
@@ -37,31 +38,16 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
     __shared__ uint64_t s_sees[ROWS];
     __shared__ int s_odd[kWaves];
 
-    const Share share = divide<kThreads, TILE>(a, s_tiles);
-    const int64_t w = int64_t(blockIdx.x);
-    if (w >= share.W) return;
-    const int64_t first = share.begin(w), end = share.begin(w + 1);
+    Division<kThreads, TILE> share;
+    share.init(a, s_tiles, 1);
+    const int64_t w = int64_t(blockIdx.x), first = share.begin(w), end = share.begin(w + 1);
 
     for (int64_t pos = first; pos < end;) {
-        const Piece p = find_piece<ROWS>(a, s_tiles, pos, end);
+        const Piece p = share.template find<ROWS>(a, pos, end);
         const int len = p.seq.len, T = p.T;
         chunk_t q[MT][CHUNKS];
         R rows;
         bool bad = p.seq.state == 2;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) rows.sees[mt] = 0;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) load_queries<Ops, CHUNKS, !GEN>(a, p, mt * 16 + col, D, q[mt]);
-        if (p.t1 * TILE > len && T > 0) {
-            bool tree;
-            const uint64_t all = wave_ancestors(L.parent ? L.parent + int64_t(p.b) * L.N : nullptr, p.seq.n, &tree);
-            bad = bad || !tree;
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                const int node = (p.row0 + mt * 16 + col) / a.group;
-                rows.sees[mt] = uint64_t(__shfl(static_cast<unsigned long long>(all), node & (kWave - 1)));
-            }
-        }
 
         // Byte offsets of the tiles of 16 keys to come (!GEN), KT lanes a step, or of
         // the keys of the next step (GEN); out of the cache: its first.
@@ -158,11 +144,33 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
             rows.add(v, pr);
             if (more) load_v(step + 1);
         };
-        rows.clear();
-        for (bool again = false; steps > 0; again = true) {
+        if (steps > 0) {
             fill(0);
             load_k(0);
             load_v(0);
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            load_queries<Ops, CHUNKS, !GEN>(a, p, mt * 16 + col, D, q[mt]);
+            rows.sees[mt] = 0;
+        }
+        if (p.t1 * TILE > len && T > 0) {
+            bool tree;
+            const uint64_t all = wave_ancestors(L.parent ? L.parent + int64_t(p.b) * L.N : nullptr, p.seq.n, &tree);
+            bad = bad || !tree;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const int node = (p.row0 + mt * 16 + col) / a.group;
+                rows.sees[mt] = uint64_t(__shfl(static_cast<unsigned long long>(all), node & (kWave - 1)));
+            }
+        }
+        rows.clear();
+        for (bool again = false; steps > 0; again = true) {
+            if (again) {
+                fill(0);
+                load_k(0);
+                load_v(0);
+            }
             float most[MT];
             if (!again) {
                 f32x4_t s[MT][KT];
@@ -232,31 +240,30 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
     }
 }
 
-template <typename Ops, int DT, int MT>
-hipError_t launch_tiles(Args& a) {
+template <typename Ops, int DT>
+hipError_t launch_dim(Args& a) {
     const TreeAttentionLaunch& L = a.L;
-    a.blocks = (L.N * a.group + 16 * MT - 1) / (16 * MT);
+    a.blocks = 1;
     int grid = L.cus * 2;
     if (grid > kMaxGroups) grid = kMaxGroups;
     const size_t lds = size_t(L.B + 1) * sizeof(int);
     if (L.pages.page_size % 16 || L.head_dim != DT)
-        return launch_kernel(&tree_attention_kernel<Ops, DT, MT, true>, dim3(grid), dim3(kThreads), lds, L.stream, a);
-    return launch_kernel(&tree_attention_kernel<Ops, DT, MT, false>, dim3(grid), dim3(kThreads), lds, L.stream, a);
+        return launch_kernel(&tree_attention_kernel<Ops, DT, true>, dim3(grid), dim3(kThreads), lds, L.stream, a);
+    return launch_kernel(&tree_attention_kernel<Ops, DT, false>, dim3(grid), dim3(kThreads), lds, L.stream, a);
 }
 
-// Rows of a workgroup.  fp32 keeps to 32 (16 of DT = 256): its matrix products are what
-// bounds it from there on.
+// Rows of a workgroup.
 int block_rows(int rows, int DT, int dtype) {
     if (rows <= 16) return 16;
-    if (dtype != OSD_BF16) return DT == 256 ? 16 : 32;
-    return rows <= 64 ? 64 : rows <= 128 || DT == 256 ? 128 : 256;
+    if (rows <= 64 || (dtype != OSD_BF16 && DT == 256)) return 64;
+    return rows <= 128 || DT == 256 || dtype != OSD_BF16 ? 128 : 256;
 }
 
 struct Workspace {
     size_t stats, parts, total;
 };
 Workspace layout(int rows, int DT, int dtype) {
-    const size_t R = size_t(block_rows(rows, DT, dtype)), slots = 2 * kMaxGroups / (R > 32 ? 2 : 1);
+    const size_t R = size_t(block_rows(rows, DT, dtype)), slots = 2 * kMaxGroups / (R > 16 ? 2 : 1);
     Workspace w;
     w.stats = kMaxGroups * sizeof(uint32_t);
     w.parts = w.stats + slots * R * 2 * sizeof(float);
@@ -264,19 +271,12 @@ Workspace layout(int rows, int DT, int dtype) {
     return w;
 }
 
-template <typename Ops, int DT>
-hipError_t launch_dim(Args& a, int rows) {
-    if constexpr (DT < 256 && Ops::Fmt::kBytes == 4)
-        if (rows > 16) return launch_tiles<Ops, DT, 2>(a);
-    return launch_tiles<Ops, DT, 1>(a);
-}
-
 template <typename Ops>
-hipError_t launch_ops(Args& a, int rows) {
+hipError_t launch_ops(Args& a) {
     switch (padded_dim(a.L.head_dim)) {
-        case 64: return launch_dim<Ops, 64>(a, rows);
-        case 128: return launch_dim<Ops, 128>(a, rows);
-        default: return launch_dim<Ops, 256>(a, rows);
+        case 64: return launch_dim<Ops, 64>(a);
+        case 128: return launch_dim<Ops, 128>(a);
+        default: return launch_dim<Ops, 256>(a);
     }
 }
 
@@ -300,9 +300,8 @@ hipError_t launch_tree_attention(const TreeAttentionLaunch& L) {
     a.parts = reinterpret_cast<float*>(L.workspace + w.parts);
     a.stats_bytes = uint32_t(w.parts - w.stats);
     a.parts_bytes = uint32_t(w.total - w.parts);
-    if (L.dtype != OSD_BF16) return launch_ops<F32Ops>(a, R);
-    if (R > 32) return launch_wide(a, R);
-    return launch_ops<Bf16Ops>(a, R);
+    if (R > 16) return launch_wide(a, R);
+    return L.dtype == OSD_BF16 ? launch_ops<Bf16Ops>(a) : launch_ops<F32Ops>(a);
 }
 
 }  // namespace osd

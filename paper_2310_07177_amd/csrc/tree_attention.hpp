@@ -92,6 +92,18 @@ struct Bf16Ops {
     __device__ static f32x4_t pv(const Value<VW> (&v)[8], int t, const Probs& p, f32x4_t o) {
         return qk(column(v, t), p.x, o);
     }
+    __device__ static f32x4_t pv(const chunk_t& v, const Probs& p, f32x4_t o) { return qk(v, p.x, o); }
+    // Of an operand of the second product: what is not finite to 0, whether there is any.
+    __device__ static bool clean(chunk_t& v) {
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = pair_finite(v[i]);
+            odd = odd || x != v[i];
+            v[i] = x;
+        }
+        return odd;
+    }
     __device__ static uint32_t half_finite(uint32_t h) { return (h & 0x7F80u) == 0x7F80u ? 0u : h; }
     __device__ static uint32_t pair_finite(uint32_t h) { return half_finite(h & 0xFFFFu) | half_finite(h >> 16) << 16; }
     template <int VW>
@@ -132,6 +144,22 @@ struct F32Ops {
         for (int i = 0; i < 4; ++i) o = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i].x[t], p.x[i], o, 0, 0, 0);
         return o;
     }
+    // (Element i of an operand: the lane's key i of 4.)
+    __device__ static f32x4_t pv(const chunk_t& v, const Probs& p, f32x4_t o) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[i]), p.x[i], o, 0, 0, 0);
+        return o;
+    }
+    __device__ static bool clean(chunk_t& v) {
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool bad = (v[i] & 0x7F800000u) == 0x7F800000u;
+            odd = odd || bad;
+            v[i] = bad ? 0u : v[i];
+        }
+        return odd;
+    }
     template <int VW>
     __device__ static void clean(Value<VW>& v) {
 #pragma unroll
@@ -161,60 +189,18 @@ struct Args {
 struct Seq {
     int len, n, state;
 };
+__device__ inline int state_of(const TreeAttentionLaunch& L, int len, int n) {
+    return len < 0 || n == 0 ? 1 : cache_fits(L.pages, len, n, L.N) ? 0 : 2;
+}
 __device__ inline Seq sequence(const TreeAttentionLaunch& L, int b) {
     Seq s{L.seq_len[b], L.new_len ? L.new_len[b] : L.N, 0};
-    if (s.len < 0 || s.n == 0) s.state = 1;
-    else if (!cache_fits(L.pages, s.len, s.n, L.N)) s.state = 2;
+    s.state = state_of(L, s.len, s.n);
     return s;
 }
 
-// Work is counted in tiles of keys.  A unit is one row block of one kv head of one
-// sequence, all its keys; units lie one after another, and workgroup w of W takes
-// the tiles from w * total / W on: equal shares whatever the lengths, at most two
-// pieces of which are parts of units (the others it has alone).
-struct Share {
-    int64_t total, W;
-    __device__ int64_t begin(int64_t w) const { return w * total / W; }
-    __device__ int64_t owner(int64_t tile) const { return ((tile + 1) * W - 1) / total; }
-};
-
-// Tiles of all sequences before each (s_tiles [B + 1]), and the shares.
-template <int THREADS, int TILE>
-__device__ inline Share divide(const Args& a, int* s_tiles) {
-    constexpr int WAVES = THREADS / kWave;
-    __shared__ int s_scan[WAVES];
-    const TreeAttentionLaunch& L = a.L;
-    const int tid = int(threadIdx.x), lane = tid & (kWave - 1), wave = tid / kWave;
-    const int each = (L.B + THREADS - 1) / THREADS, first = tid * each;
-    int mine = 0;
-    for (int b = first; b < first + each && b < L.B; ++b) {
-        const Seq s = sequence(L, b);
-        const int tiles = s.state ? 1 : (s.len + s.n - 1) / TILE + 1;
-        s_tiles[b] = tiles;
-        mine += tiles;
-    }
-    int sum = mine;
-#pragma unroll
-    for (int o = 1; o < kWave; o *= 2) {
-        const int up = __shfl_up(sum, o);
-        if (lane >= o) sum += up;
-    }
-    if (lane == kWave - 1) s_scan[wave] = sum;
-    __syncthreads();
-    int before = sum - mine;
-    for (int w = 0; w < wave; ++w) before += s_scan[w];
-    for (int b = first; b < first + each && b < L.B; ++b) {
-        const int tiles = s_tiles[b];
-        s_tiles[b] = before;
-        before += tiles;
-        if (b == L.B - 1) s_tiles[L.B] = before;
-    }
-    __syncthreads();
-    const int64_t units = int64_t(L.kv_heads) * a.blocks;
-    Share s{s_tiles[L.B] * units, int64_t(gridDim.x)};
-    if (s.W > L.B * units * kMaxPieces) s.W = L.B * units * kMaxPieces;
-    if (s.W > s.total) s.W = s.total;
-    return s;
+__device__ inline int64_t quotient(int64_t a, int64_t b) {
+    if ((uint64_t(a | b) >> 32) == 0) return int64_t(uint32_t(a) / uint32_t(b));  // a tenth of the instructions
+    return a / b;
 }
 
 // A workgroup's part of one unit.
@@ -225,24 +211,110 @@ struct Piece {
     int T;                 // keys
     __device__ bool whole() const { return t0 == 0 && t1 == tiles; }
 };
+// Work is counted in tiles of keys.  A unit is one row block of one kv head of one
+// sequence, all its keys; units lie one after another, and every workgroup takes the
+// same number of tiles whatever the lengths, at most two pieces of which are parts of
+// units (the others it has alone).  Sequences' lengths are in registers of each wave
+// (up to 64 of them) or in LDS.
+template <int THREADS, int TILE>
+struct Division {
+    int* s_before;         // [B + 1] tiles of the sequences before each, of one unit (more than 64)
+    int upto, len, n;      // (up to 64) lane b: tiles up to and with sequence b, and the sequence
+    int64_t total, each;   // tiles of all units, of a workgroup
+
+    __device__ static int tiles_of(const Seq& s) { return s.state ? 1 : (s.len + s.n - 1) / TILE + 1; }
+
+    // least: tiles of a workgroup.
+    __device__ void init(const Args& a, int* room, int least) {
+        const TreeAttentionLaunch& L = a.L;
+        const int tid = int(threadIdx.x), lane = tid & (kWave - 1);
+        int all;
+        s_before = room;
+        if (L.B <= kWave) {
+            Seq s{-1, 0, 1};
+            if (lane < L.B) s = sequence(L, lane);
+            len = s.len;
+            n = s.n;
+            upto = lane < L.B ? tiles_of(s) : 0;
+#pragma unroll
+            for (int o = 1; o < kWave; o *= 2) {
+                const int up = __shfl_up(upto, o);
+                upto += lane >= o ? up : 0;
+            }
+            all = __builtin_amdgcn_readlane(upto, kWave - 1);
+        } else {
+            constexpr int WAVES = THREADS / kWave;
+            __shared__ int s_scan[WAVES];
+            const int wave = tid / kWave, each = (L.B + THREADS - 1) / THREADS, first = tid * each;
+            int mine = 0;
+            for (int b = first; b < first + each && b < L.B; ++b) {
+                const int tiles = tiles_of(sequence(L, b));
+                s_before[b] = tiles;
+                mine += tiles;
+            }
+            int sum = mine;
+#pragma unroll
+            for (int o = 1; o < kWave; o *= 2) {
+                const int up = __shfl_up(sum, o);
+                sum += lane >= o ? up : 0;
+            }
+            if (lane == kWave - 1) s_scan[wave] = sum;
+            __syncthreads();
+            int before = sum - mine;
+            for (int w = 0; w < wave; ++w) before += s_scan[w];
+            for (int b = first; b < first + each && b < L.B; ++b) {
+                const int tiles = s_before[b];
+                s_before[b] = before;
+                before += tiles;
+                if (b == L.B - 1) s_before[L.B] = before;
+            }
+            __syncthreads();
+            all = __builtin_amdgcn_readfirstlane(s_before[L.B]);
+        }
+        const int64_t units = int64_t(L.kv_heads) * a.blocks;
+        total = all * units;
+        int64_t W = int64_t(gridDim.x);
+        if (W > L.B * units * kMaxPieces) W = L.B * units * kMaxPieces;
+        each = quotient(total + W - 1, W);
+        if (each < least) each = least;
+    }
+    __device__ int64_t begin(int64_t w) const { return w * each < total ? w * each : total; }
+    __device__ int owner(int64_t tile) const { return int(quotient(tile, each)); }
+
+    template <int ROWS>
+    __device__ Piece find(const Args& a, int64_t pos, int64_t end) const;
+};
+
+template <int THREADS, int TILE>
 template <int ROWS>
-__device__ inline Piece find_piece(const Args& a, const int* s_tiles, int64_t pos, int64_t end) {
+__device__ inline Piece Division<THREADS, TILE>::find(const Args& a, int64_t pos, int64_t end) const {
     const TreeAttentionLaunch& L = a.L;
     const int64_t units = int64_t(L.kv_heads) * a.blocks;
-    int b = 0;
-    for (int hi = L.B; hi - b > 1;) {
-        const int mid = (b + hi) / 2;
-        if (s_tiles[mid] * units <= pos) b = mid;
-        else hi = mid;
-    }
     Piece p;
-    p.b = __builtin_amdgcn_readfirstlane(b);
-    p.seq = sequence(L, p.b);
-    p.tiles = __builtin_amdgcn_readfirstlane(s_tiles[p.b + 1] - s_tiles[p.b]);
-    const int64_t in_b = pos - s_tiles[p.b] * units;
-    const int unit = __builtin_amdgcn_readfirstlane(int(in_b / p.tiles));
-    p.t0 = __builtin_amdgcn_readfirstlane(int(in_b - int64_t(unit) * p.tiles));
-    p.t1 = __builtin_amdgcn_readfirstlane(int(end - pos < p.tiles - p.t0 ? p.t0 + (end - pos) : p.tiles));
+    int before;
+    if (L.B <= kWave) {
+        const int lane = int(threadIdx.x) & (kWave - 1);
+        p.b = __ffsll(static_cast<unsigned long long>(__ballot(lane < L.B && upto * units > pos))) - 1;
+        before = p.b ? __builtin_amdgcn_readlane(upto, p.b - 1) : 0;
+        p.tiles = __builtin_amdgcn_readlane(upto, p.b) - before;
+        p.seq = Seq{__builtin_amdgcn_readlane(len, p.b), __builtin_amdgcn_readlane(n, p.b), 0};
+        p.seq.state = state_of(L, p.seq.len, p.seq.n);
+    } else {
+        int b = 0;
+        for (int hi = L.B; hi - b > 1;) {
+            const int mid = (b + hi) / 2;
+            if (s_before[mid] * units <= pos) b = mid;
+            else hi = mid;
+        }
+        p.b = __builtin_amdgcn_readfirstlane(b);
+        before = __builtin_amdgcn_readfirstlane(s_before[p.b]);
+        p.tiles = __builtin_amdgcn_readfirstlane(s_before[p.b + 1]) - before;
+        p.seq = sequence(L, p.b);
+    }
+    const int64_t in_b = pos - before * units;
+    const int unit = int(quotient(in_b, p.tiles));
+    p.t0 = int(in_b - int64_t(unit) * p.tiles);
+    p.t1 = int(end - pos < p.tiles - p.t0 ? p.t0 + (end - pos) : p.tiles);
     p.h = unit / a.blocks;
     p.row0 = (unit - p.h * a.blocks) * ROWS;
     p.rows = L.N * a.group - p.row0 < ROWS ? L.N * a.group - p.row0 : ROWS;
@@ -508,29 +580,31 @@ __device__ inline void join_parts(const Args& a, const Piece& p, int first_slot,
 
 // A workgroup has posted its part of a unit (all its threads call this); the last of
 // the unit's joins them, in their order.
-template <typename Fmt, int THREADS, int ROWS, int DT>
-__device__ inline void join(const Args& a, const Piece& p, const Share& share, int64_t pos, int D) {
+template <typename Fmt, int THREADS, int ROWS, int DT, typename Division>
+__device__ inline void join(const Args& a, const Piece& p, const Division& share, int64_t pos, int D) {
     __shared__ uint32_t s_arrived;
     const int tid = int(threadIdx.x);
-    const int64_t u0 = pos - p.t0, w0 = share.owner(u0), w1 = share.owner(u0 + p.tiles - 1);
+    const int64_t u0 = pos - p.t0;
+    const int w0 = share.owner(u0), w1 = share.owner(u0 + p.tiles - 1);
     wait_memory();
     __syncthreads();
     if (tid == 0) s_arrived = arrive(&a.counters[w0]);
     __syncthreads();
     if (s_arrived != uint32_t(w1 - w0)) return;
-    const int count = int(w1 - w0) + 1;
-    const int first_slot = 2 * int(w0) + (share.begin(w0) == u0 ? 0 : 1);
+    const int count = w1 - w0 + 1;
+    const int first_slot = 2 * w0 + (share.begin(w0) == u0 ? 0 : 1);
     // A read takes about 2 us, so as many as registers allow are in flight.
-    if (count <= 2) join_parts<Fmt, THREADS, ROWS, DT, 8, 2>(a, p, first_slot, int(w0), count, D);
-    else if (count <= 4) join_parts<Fmt, THREADS, ROWS, DT, 4, 4>(a, p, first_slot, int(w0), count, D);
-    else join_parts<Fmt, THREADS, ROWS, DT, 2, 8>(a, p, first_slot, int(w0), count, D);
+    if (count <= 2) join_parts<Fmt, THREADS, ROWS, DT, 8, 2>(a, p, first_slot, w0, count, D);
+    else if (count <= 4) join_parts<Fmt, THREADS, ROWS, DT, 4, 4>(a, p, first_slot, w0, count, D);
+    else if (count <= 8) join_parts<Fmt, THREADS, ROWS, DT, 2, 8>(a, p, first_slot, w0, count, D);
+    else join_parts<Fmt, THREADS, ROWS, DT, 1, 16>(a, p, first_slot, w0, count, D);
     if (tid == 0) __hip_atomic_store(&a.counters[w0], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // Rows of one workgroup, of the kernel that serves `rows` rows of a kv head.
 inline int padded_dim(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
-hipError_t launch_wide(const Args& a, int rows);  // tree_attention_wide.hip: bf16
+hipError_t launch_wide(const Args& a, int rows);  // tree_attention_wide.hip
 
 }  // namespace attention
 }  // namespace osd

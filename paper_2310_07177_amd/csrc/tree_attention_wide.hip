@@ -1,5 +1,5 @@
-// tree_attention_wide.hip -- osd_tree_attention of many bf16 rows: eight waves of 32
-// rows each read keys and values from LDS, where they arrive directly from memory.
+// tree_attention_wide.hip -- osd_tree_attention of many rows: eight waves read keys
+// and values from LDS, where they arrive directly from memory.
 #include "tree_attention.hpp"
 
 namespace osd {
@@ -16,6 +16,11 @@ constexpr int kPageWindow = 512;  // pages looked up at once
 __device__ inline void load_lds(const char* from, uint32_t to) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
 }
+// All but the wave's LEFT newest loads are there, then those of all waves.
+template <int LEFT>
+__device__ inline void wait_stage() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
 // The transposing read: 16 lanes give the places of 4 keys' pieces of 16 elements (8 bytes
 // a lane, four lanes a key) and get an element of the 4 keys each.
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
@@ -23,39 +28,33 @@ __device__ inline u32x2_t transposed(const char* at) {
     return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                                            (__attribute__((address_space(3))) s16x4_t*)(const_cast<char*>(at))));
 }
-template <int LEFT>
-__device__ inline void wait_stage() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
-}
 
 // WR waves share the rows, 16 MT each, WK = 8 / WR the keys of a stage.  The ring of
-// stages in LDS is filled NST - 1 ahead.  A row's 16-byte chunks lie permuted
-// (chunk ^ key), so that 16 lanes that read one chunk of 16 keys meet 16 different
-// banks; the DMA writes lanes one after another, so the permutation is in what they
-// read.
-template <int DT, int WR, int MT>
+// stages in LDS is filled NST - 1 ahead.
+template <typename Ops, int DT, int WR, int MT>
 struct Shape {
-    static constexpr int WK = kWaves / WR, STAGE = DT == 256 ? 32 * WK : 64, SUB = STAGE / (32 * WK);
+    static constexpr int ES = Ops::Fmt::kBytes, STEP = 16 * Ops::kKT, ROW = DT * ES;
+    static constexpr int WK = kWaves / WR, FIT = 16384 / ROW < 64 ? 16384 / ROW : 64;
+    static constexpr int STAGE = FIT > STEP * WK ? FIT : STEP * WK;
     static constexpr int ROWS = 16 * MT * WR, PITCH = DT + 4;
-    static constexpr int TILE_BYTES = STAGE * DT * 2;  // of K, and of V
+    static constexpr int TILE_BYTES = STAGE * ROW;  // of K, and of V
     static constexpr int NST = TILE_BYTES > 16384 ? 2 : 4;
     static constexpr int RING = NST * 2 * TILE_BYTES, MERGE = kWaves * 16 * PITCH * 4;
     static constexpr int LDS = RING > MERGE ? RING : MERGE;
     static constexpr int LOADS = TILE_BYTES / 1024 / kWaves;  // of K, and of V, of a wave for a stage
+    static constexpr int CPR = ROW / 16;                      // 16-byte chunks of a row
 };
 
-template <int DT, int WR, int MT, bool FULL>
+template <typename Ops, int DT, int WR, int MT, bool FULL>
 __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
-    using Ops = Bf16Ops;
-    using Fmt = BF16;
-    using S = Shape<DT, WR, MT>;
-    constexpr int ES = 2;
+    using Fmt = typename Ops::Fmt;
+    using S = Shape<Ops, DT, WR, MT>;
     using R = Rows<Ops, DT, MT, 1>;
-    constexpr int CHUNKS = R::CHUNKS, KT = R::KT;
-    constexpr int WK = S::WK, STAGE = S::STAGE, ROWS = S::ROWS, PITCH = S::PITCH, CPR = DT / 8;
+    constexpr int ES = S::ES, CHUNKS = R::CHUNKS, KT = R::KT, STEP = S::STEP, STAGE = S::STAGE, ROWS = S::ROWS;
+    constexpr int PITCH = S::PITCH, CPR = S::CPR, ROW = S::ROW;
     const TreeAttentionLaunch& L = a.L;
     const int tid = int(threadIdx.x), lane = tid & (kWave - 1), col = lane & 15, grp = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave), wr = wave % WR, wk = wave / WR;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int D = FULL ? DT : L.head_dim;
 
     extern __shared__ int s_tiles[];  // [B + 1]
@@ -67,33 +66,30 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
     float(*s_acc)[16][PITCH] = reinterpret_cast<float(*)[16][PITCH]>(s_ring);
     const uint32_t ring = uint32_t(uintptr_t((__attribute__((address_space(3))) char*)s_ring));
 
-    const Share share = divide<kThreads, STAGE>(a, s_tiles);
-    const int64_t w = int64_t(blockIdx.x);
-    if (w >= share.W) return;
-    const int64_t first = share.begin(w), end = share.begin(w + 1);
-    // XOR of a row's chunks, of period 16: rows of 128 bytes lie two to 64 banks.
-    const auto swizzle = [](int key) { return DT == 64 ? (key >> 1) & 7 : key & 15; };
+    Division<kThreads, STAGE> share;
+    share.init(a, s_tiles, 1);
+    const int64_t w = int64_t(blockIdx.x), first = share.begin(w), end = share.begin(w + 1);
+
+    // A row's chunks lie permuted (chunk ^ key, of period 16; rows of 128 bytes lie two to
+    // 64 banks), so that 16 lanes that read one chunk of 16 keys meet 16 different
+    // places; the DMA writes lanes one after another, so the permutation is in what they read.
+    const auto swizzle = [](int key) { return CPR == 8 ? (key >> 1) & 7 : key & 15; };
+    // Of each of the wave's loads: its first key in the stage (of 1024 / ROW), and the lane's place from there.
+    int lane_key[S::LOADS], lane_chunk[S::LOADS];
+#pragma unroll
+    for (int x = 0; x < S::LOADS; ++x) {
+        const int at = (wave * S::LOADS + x) * kWave + lane, key = at / CPR;
+        lane_key[x] = lane / CPR;
+        lane_chunk[x] = (at % CPR) ^ swizzle(key);
+        if (!FULL && lane_chunk[x] * 16 >= D * ES) lane_chunk[x] = 0;
+    }
+    const bool even_pages = L.pages.page_size % 8 == 0;  // a load's keys (8 at most) lie on one page
 
     for (int64_t pos = first; pos < end;) {
-        const Piece p = find_piece<ROWS>(a, s_tiles, pos, end);
+        const Piece p = share.template find<ROWS>(a, pos, end);
         const int len = p.seq.len, T = p.T;
-        chunk_t q[MT][CHUNKS];
-        R rows;
         bool bad = p.seq.state == 2;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) rows.sees[mt] = 0;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) load_queries<Ops, CHUNKS, FULL>(a, p, (wr * MT + mt) * 16 + col, D, q[mt]);
-        if (p.t1 * STAGE > len && T > 0) {
-            bool tree;
-            const uint64_t all = wave_ancestors(L.parent ? L.parent + int64_t(p.b) * L.N : nullptr, p.seq.n, &tree);
-            bad = bad || !tree;
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                const int node = (p.row0 + (wr * MT + mt) * 16 + col) / a.group;
-                rows.sees[mt] = uint64_t(__shfl(static_cast<unsigned long long>(all), node & (kWave - 1)));
-            }
-        }
+        const int64_t head = int64_t(p.h) * L.pages.head_bytes;
 
         // The pages from page0 on; a stage's keys behind the last stand for the last.
         const int stages = T > 0 ? p.t1 - p.t0 : 0;
@@ -123,31 +119,69 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
             const uint32_t to = ring + uint32_t(st % S::NST) * (2 * S::TILE_BYTES);
 #pragma unroll
             for (int x = 0; x < S::LOADS; ++x) {
-                const int at = (wave * S::LOADS + x) * kWave + lane, key = at / CPR;
-                int chunk = (at % CPR) ^ swizzle(key);
-                if (!FULL && chunk * 8 >= D) chunk = 0;
-                int j = (p.t0 + st) * STAGE + key;
-                j = j < T ? j : T - 1;
-                const int in = page_of(j);
-                const int64_t from = int64_t(s_page[in - page0]) * L.pages.page_bytes + int64_t(p.h) * L.pages.head_bytes +
-                                     int64_t(j - in * L.pages.page_size) * (D * ES) + chunk * 16;
+                constexpr int KEYS_OF = 1024 / ROW > 0 ? 1024 / ROW : 1;
+                const int key0 = (p.t0 + st) * STAGE + (wave * S::LOADS + x) * KEYS_OF;
+                int64_t from;
+                if (even_pages) {
+                    const int last = (T - 1) / KEYS_OF * KEYS_OF, j = key0 < last ? key0 : last, in = page_of(j);
+                    const int page = __builtin_amdgcn_readfirstlane(s_page[in - page0]);
+                    from = int64_t(page) * L.pages.page_bytes + head + int64_t(j - in * L.pages.page_size) * (D * ES) +
+                           (lane_key[x] * (D * ES) + lane_chunk[x] * 16);
+                } else {
+                    int j = key0 + lane_key[x];
+                    j = j < T ? j : T - 1;
+                    const int in = page_of(j);
+                    from = int64_t(s_page[in - page0]) * L.pages.page_bytes + head +
+                           int64_t(j - in * L.pages.page_size) * (D * ES) + lane_chunk[x] * 16;
+                }
                 const uint32_t unit = to + uint32_t(wave * S::LOADS + x) * 1024u;
                 load_lds(L.k_cache + from, unit);
                 load_lds(L.v_cache + from, unit + S::TILE_BYTES);
             }
         };
+        for (int st = 0; st < S::NST - 1 && st < stages; ++st) issue(st);
+
+        // Half of the rows in use (a batch's smaller trees): the waves without rows take half of the keys.
+        constexpr bool HALVES = WR == kWaves && STAGE / STEP % 2 == 0;
+        const int half = HALVES && p.live * 2 <= ROWS ? 1 : 0;
+        const int row_waves = WR >> half, wr = wave & (row_waves - 1), wk = wave / row_waves, key_waves = kWaves / row_waves;
         const bool alive = wr * MT * 16 < p.live;  // (of padding alone: a wave helps to fill the ring)
-        bool fresh = true;                         // no reference yet
-        auto take = [&](int st, int sub, auto tail) {
+        chunk_t q[MT][CHUNKS];
+        R rows;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            load_queries<Ops, CHUNKS, FULL>(a, p, (wr * MT + mt) * 16 + col, D, q[mt]);
+            rows.sees[mt] = 0;
+        }
+        if (p.t1 * STAGE > len && T > 0) {
+            bool tree;
+            const uint64_t all = wave_ancestors(L.parent ? L.parent + int64_t(p.b) * L.N : nullptr, p.seq.n, &tree);
+            bad = bad || !tree;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const int node = (p.row0 + (wr * MT + mt) * 16 + col) / a.group;
+                rows.sees[mt] = uint64_t(__shfl(static_cast<unsigned long long>(all), node & (kWave - 1)));
+            }
+        }
+
+        bool fresh = true;  // no reference yet
+        auto take = [&](int st, int k0, auto tail) {
             constexpr bool TAIL = decltype(tail)::value;
-            const int k0 = (sub * WK + wk) * 32, j0 = (p.t0 + st) * STAGE + k0;
-            const char* k_row = s_ring + (st % S::NST) * (2 * S::TILE_BYTES) + (k0 + col) * (DT * ES);
+            const int j0 = (p.t0 + st) * STAGE + k0;
+            const char* k_row = s_ring + (st % S::NST) * (2 * S::TILE_BYTES) + (k0 + col) * ROW;
             // (A chunk's place is a XOR of the lane's part and a constant; computed each time, as all of
             // them together would hold 30 registers.)
             int k_lane = (grp ^ swizzle(col)) * 16;
-            const int from = grp * 4 + (col >> 2);  // the key whose piece of V this lane reads for the others
-            const char* v_row = s_ring + (st % S::NST) * (2 * S::TILE_BYTES) + S::TILE_BYTES + (k0 + from) * (DT * ES) + (col & 1) * 8;
-            int v_lane = (((col & 3) >> 1) ^ swizzle(from)) * 16;
+            const char* v_row;
+            int v_lane;
+            if constexpr (ES == 2) {  // the key whose piece of V this lane reads for the others
+                const int from = grp * 4 + (col >> 2);
+                v_row = k_row + S::TILE_BYTES + (from - col) * ROW + (col & 1) * 8;
+                v_lane = (((col & 3) >> 1) ^ swizzle(from)) * 16;
+            } else {
+                v_row = k_row + S::TILE_BYTES + (grp * 4 - col) * ROW + (col & 3) * 4;
+                v_lane = ((col >> 2) ^ swizzle(grp * 4)) * 16;
+            }
             asm volatile("" : "+v"(k_lane), "+v"(v_lane));
             f32x4_t s[MT][KT];
 #pragma unroll
@@ -157,8 +191,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c) {
                     if (!FULL && c * Ops::kChunk >= D) continue;
-                    chunk_t k = *reinterpret_cast<const chunk_t*>(k_row + kt * 16 * (DT * ES) + (k_lane ^ c * 64));
-                    if (!FULL && c * Ops::kChunk + grp * 8 >= D) k = chunk_t{0, 0, 0, 0};
+                    chunk_t k = *reinterpret_cast<const chunk_t*>(k_row + kt * 16 * ROW + (k_lane ^ c * 64));
+                    if (!FULL && c * Ops::kChunk + grp * (16 / ES) >= D) k = chunk_t{0, 0, 0, 0};
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) s[mt][kt] = Ops::qk(k, q[mt][c], s[mt][kt]);
                 }
@@ -174,48 +208,50 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
             }
             typename Ops::Probs pr[MT];
             rows.template soften<TAIL>(s, a.c2, pr);
-            // Pairs of halves of the lane's 8 keys that are keys.
+            // The lane's keys that are keys.
             chunk_t in;
             if constexpr (TAIL) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int j = j0 + (i / 2) * 16 + grp * 4 + (i & 1) * 2;
-                    in[i] = (j < T ? 0xFFFFu : 0u) | (j + 1 < T ? 0xFFFF0000u : 0u);
+                    const int j = j0 + (ES == 2 ? (i / 2) * 16 + grp * 4 + (i & 1) * 2 : grp * 4 + i);
+                    in[i] = ES == 2 ? (j < T ? 0xFFFFu : 0u) | (j + 1 < T ? 0xFFFF0000u : 0u) : j < T ? ~0u : 0u;
                 }
             }
 #pragma unroll
             for (int t = 0; t < DT / 16; ++t) {
+                if (!FULL && t * 16 >= D) continue;
                 chunk_t v;
+                if constexpr (ES == 2) {
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt) {
-                    const u32x2_t half = transposed(v_row + kt * 16 * (DT * ES) + (v_lane ^ t * 32));
-                    v[2 * kt] = half.x;
-                    v[2 * kt + 1] = half.y;
+                    for (int kt = 0; kt < KT; ++kt) {
+                        const u32x2_t half_of = transposed(v_row + kt * 16 * ROW + (v_lane ^ t * 32));
+                        v[2 * kt] = half_of.x;
+                        v[2 * kt + 1] = half_of.y;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint32_t*>(v_row + i * ROW + (v_lane ^ (i * 16) ^ t * 64));
                 }
                 if constexpr (TAIL) {
-                    chunk_t clean;
                     v &= in;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) clean[i] = Ops::pair_finite(v[i]);
-                    rows.odd = rows.odd || __any(clean[0] != v[0] || clean[1] != v[1] || clean[2] != v[2] || clean[3] != v[3]);
-                    v = clean;
+                    const bool odd = Ops::clean(v);
+                    rows.odd = rows.odd || __any(odd);
                 }
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) rows.acc[mt][t][0] = Ops::qk(v, pr[mt].x, rows.acc[mt][t][0]);
+                for (int mt = 0; mt < MT; ++mt) rows.acc[mt][t][0] = Ops::pv(v, pr[mt], rows.acc[mt][t][0]);
             }
         };
         rows.clear();
         for (bool again = false;; again = true) {
-            __syncthreads();  // the ring is free
             if (again) {
                 float most[MT];
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) most[mt] = rows.seen[mt];
                 rows.clear();
                 rows.refer(most, a.c2);
+                page_end = 0;
+                for (int st = 0; st < S::NST - 1 && st < stages; ++st) issue(st);
             }
-            page_end = 0;
-            for (int st = 0; st < S::NST - 1 && st < stages; ++st) issue(st);
             for (int st = 0; st < stages; ++st) {
                 // This stage is there; the ones behind it may be on their way.
                 if (S::NST > 2 && st + 2 < stages) wait_stage<(S::NST > 2 ? 4 * S::LOADS : 0)>();
@@ -223,11 +259,11 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                 else wait_stage<0>();
                 if (st + S::NST - 1 < stages) issue(st + S::NST - 1);
 #pragma unroll
-                for (int sub = 0; sub < S::SUB; ++sub) {
-                    const int j0 = (p.t0 + st) * STAGE + (sub * WK + wk) * 32;
-                    if (j0 >= T || !alive) continue;
-                    if (j0 + 32 <= len) take(st, sub, no_t{});
-                    else take(st, sub, yes_t{});
+                for (int sub = 0; sub < STAGE / STEP / S::WK; ++sub) {
+                    const int k0 = (sub * key_waves + wk) * STEP, j0 = (p.t0 + st) * STAGE + k0;
+                    if (j0 >= T || !alive || k0 >= STAGE) continue;
+                    if (j0 + STEP <= len) take(st, k0, no_t{});
+                    else take(st, k0, yes_t{});
                 }
             }
             // All waves share the stages, so that one that needs them again has all go through them.
@@ -263,25 +299,25 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             float all = kNegInf;
-#pragma unroll
-            for (int i = 0; i < WK; ++i) all = fmaxf(all, s_stat[i * WR + wr][mt * 16 + col][0]);
+            for (int i = 0; i < key_waves; ++i) all = fmaxf(all, s_stat[i * row_waves + wr][mt * 16 + col][0]);
             rows.template store<PITCH>(mt, rescale(rows.ref[mt], all), s_acc[wave][col]);
             __syncthreads();
+            // (With half of the rows in use the other half is padding: zeros.)
             for (int i = tid; i < WR * 16 * (DT / 4); i += kThreads) {
                 const int rr = i / (DT / 4), d = i % (DT / 4) * 4, x = rr / 16, r = rr % 16, row = (x * MT + mt) * 16 + r;
                 if (row >= p.rows || d >= D) continue;
-                f32x4_t o = *reinterpret_cast<const f32x4_t*>(&s_acc[x][r][d]);
-                float most = s_stat[x][mt * 16 + r][0], total = 0.0f;
-#pragma unroll
-                for (int y = 1; y < WK; ++y) {
-                    o += *reinterpret_cast<const f32x4_t*>(&s_acc[y * WR + x][r][d]);
-                    most = fmaxf(most, s_stat[y * WR + x][mt * 16 + r][0]);
-                }
-                if ((flags & 2) && row < p.live) add_odd<Fmt>(L, p.b, p.h, d, len, T, len / 32 * 32, s_sees[row], o);
-#pragma unroll
-                for (int y = 0; y < WK; ++y) {
-                    const float s = s_stat[y * WR + x][mt * 16 + r][1];
-                    total += s == s ? s * rescale(s_stat[y * WR + x][mt * 16 + r][0], most) : s;
+                f32x4_t o = {0, 0, 0, 0};
+                float most = kNegInf, total = 0.0f;
+                if (x < row_waves) {
+                    for (int y = 0; y < key_waves; ++y) {
+                        o += *reinterpret_cast<const f32x4_t*>(&s_acc[y * row_waves + x][r][d]);
+                        most = fmaxf(most, s_stat[y * row_waves + x][mt * 16 + r][0]);
+                    }
+                    if ((flags & 2) && row < p.live) add_odd<Fmt>(L, p.b, p.h, d, len, T, len / STEP * STEP, s_sees[row], o);
+                    for (int y = 0; y < key_waves; ++y) {
+                        const float s = s_stat[y * row_waves + x][mt * 16 + r][1];
+                        total += s == s ? s * rescale(s_stat[y * row_waves + x][mt * 16 + r][0], most) : s;
+                    }
                 }
                 if (flags & 1) total = __builtin_nanf("");
                 if (whole) write_row<Fmt>(a, p, row, d, D, o, total);
@@ -291,37 +327,46 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
         }
         if (!whole) join<Fmt, kThreads, ROWS, DT>(a, p, share, pos, D);
         pos += p.t1 - p.t0;
+        __syncthreads();  // the ring and the pages are free
     }
 }
 
-template <int DT, int WR, int MT>
+template <typename Ops, int DT, int WR, int MT>
 hipError_t launch_shape(Args& a) {
     const TreeAttentionLaunch& L = a.L;
-    constexpr int ROWS = Shape<DT, WR, MT>::ROWS;
+    constexpr int ROWS = Shape<Ops, DT, WR, MT>::ROWS;
     a.blocks = (L.N * a.group + ROWS - 1) / ROWS;
     const int grid = L.cus < kMaxGroups / 2 ? L.cus : kMaxGroups / 2;
     const size_t lds = size_t(L.B + 1) * sizeof(int);
     if (L.head_dim == DT)
-        return launch_kernel(&tree_attention_wide<DT, WR, MT, true>, dim3(grid), dim3(kThreads), lds, L.stream, a);
-    return launch_kernel(&tree_attention_wide<DT, WR, MT, false>, dim3(grid), dim3(kThreads), lds, L.stream, a);
+        return launch_kernel(&tree_attention_wide<Ops, DT, WR, MT, true>, dim3(grid), dim3(kThreads), lds, L.stream, a);
+    return launch_kernel(&tree_attention_wide<Ops, DT, WR, MT, false>, dim3(grid), dim3(kThreads), lds, L.stream, a);
 }
 
-template <int DT>
+// (A wave's sums of 32 rows of DT = 256, or of fp32, would fill its registers.)
+template <typename Ops, int DT>
 hipError_t launch_dim(Args& a, int rows) {
-    if (rows <= 64) return launch_shape<DT, 4, 1>(a);
-    if constexpr (DT == 256) return launch_shape<DT, 8, 1>(a);
-    else return rows <= 128 ? launch_shape<DT, 4, 2>(a) : launch_shape<DT, 8, 2>(a);
+    if (rows <= 64) return launch_shape<Ops, DT, 4, 1>(a);
+    if constexpr (Ops::Fmt::kBytes == 2 && DT < 256)
+        return rows <= 128 ? launch_shape<Ops, DT, 4, 2>(a) : launch_shape<Ops, DT, 8, 2>(a);
+    else if constexpr (Ops::Fmt::kBytes == 2 || DT < 256) return launch_shape<Ops, DT, 8, 1>(a);
+    else return hipErrorInvalidValue;
+}
+
+template <typename Ops>
+hipError_t launch_ops(Args& a, int rows) {
+    switch (padded_dim(a.L.head_dim)) {
+        case 64: return launch_dim<Ops, 64>(a, rows);
+        case 128: return launch_dim<Ops, 128>(a, rows);
+        default: return launch_dim<Ops, 256>(a, rows);
+    }
 }
 
 }  // namespace
 
 hipError_t launch_wide(const Args& args, int rows) {
     Args a = args;
-    switch (padded_dim(a.L.head_dim)) {
-        case 64: return launch_dim<64>(a, rows);
-        case 128: return launch_dim<128>(a, rows);
-        default: return launch_dim<256>(a, rows);
-    }
+    return a.L.dtype == OSD_BF16 ? launch_ops<Bf16Ops>(a, rows) : launch_ops<F32Ops>(a, rows);
 }
 
 }  // namespace attention
