@@ -491,8 +491,9 @@ int osd_verify_topk(const void* target_logits, const int32_t* draft_ids, const v
  * [pages, kv_heads, page_size, head_dim] in `dtype`, with page_stride elements
  * between pages (so that K and V may share one allocation).  A sequence's
  * tokens lie on the pages that its row of page_table names: token j on page
- * page_table[b, j / page_size], slot j % page_size.  Arguments shared by the
- * three operators:
+ * page_table[b, j / page_size], slot j % page_size.  These calls have many
+ * arguments, so they take them in a struct in host memory, which they have read
+ * when they return.  osd_cache is what the three share:
  *
  * k_cache, v_cache   the caches
  * page_stride        elements between pages, >= kv_heads * page_size * head_dim
@@ -504,6 +505,9 @@ int osd_verify_topk(const void* target_logits, const int32_t* draft_ids, const v
  *                    (a padded batch)
  * N                  new tokens of a sequence: node n of sequence b is token
  *                    c_b + n of the cache
+ *
+ * and two of them the tree:
+ *
  * parent             [B, N] int32 as in osd_verify_tree (node 0 is the root,
  *                    0 <= parent[n] < n), or NULL: a chain, every node's parent
  *                    the one before it.  N <= OSD_MAX_TREE_NODES with a tree
@@ -520,7 +524,14 @@ int osd_verify_topk(const void* target_logits, const int32_t* draft_ids, const v
 #define OSD_MAX_HEAD_DIM 256
 #define OSD_MAX_CACHE_BATCH 4096
 
-typedef enum { OSD_ROTATE_HALVES = 0, OSD_ROTATE_PAIRS = 1 } osd_rotation;
+typedef struct {
+    void* k_cache;
+    void* v_cache;
+    int64_t page_stride;
+    const int32_t* page_table;
+    const int32_t* seq_len;
+    int32_t pages, page_size, kv_heads, head_dim, dtype, table_len, B, N;
+} osd_cache;
 
 /*
  * osd_cache_append -- new tokens' keys and values into the pages behind the
@@ -549,12 +560,23 @@ typedef enum { OSD_ROTATE_HALVES = 0, OSD_ROTATE_PAIRS = 1 } osd_rotation;
  * an invalid tree), and all of a sequence whose n_b is outside 0 .. N, is not
  * written to the cache; its q_out is NaN.
  */
-int osd_cache_append(void* k_cache, void* v_cache, int64_t page_stride, int pages, int page_size, int kv_heads,
-                     int head_dim, int dtype, const int32_t* page_table, int table_len, const int32_t* seq_len,
-                     const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, int q_heads,
-                     const void* k, int64_t k_stride, const void* v, int64_t v_stride, int B, int N,
-                     const int32_t* parent, const int32_t* new_len, const float* rotation, int rotation_rows,
-                     int rotary_dim, int rotation_style, void* stream);
+typedef enum { OSD_ROTATE_HALVES = 0, OSD_ROTATE_PAIRS = 1 } osd_rotation;
+typedef struct {
+    osd_cache cache;
+    const void* q;
+    int64_t q_stride;
+    void* q_out;
+    int64_t q_out_stride;
+    const void* k;
+    int64_t k_stride;
+    const void* v;
+    int64_t v_stride;
+    const int32_t* parent;
+    const int32_t* new_len;
+    const float* rotation;
+    int32_t q_heads, rotation_rows, rotary_dim, rotation_style;
+} osd_append;
+int osd_cache_append(const osd_append* call, void* stream);
 
 /*
  * osd_tree_attention -- attention of the drafted tokens: node n sees the context,
@@ -580,12 +602,20 @@ int osd_cache_append(void* k_cache, void* v_cache, int64_t page_stride, int page
  * captured call serves any lengths; how it is divided, and with it the last bits,
  * depends on all of the batch.  Equal calls give equal bits.
  */
+typedef struct {
+    osd_cache cache;
+    const void* q;
+    int64_t q_stride;
+    const int32_t* parent;
+    const int32_t* new_len;
+    void* out;
+    void* workspace;
+    size_t workspace_bytes;
+    int32_t q_heads;
+    float scale;
+} osd_attention;
 size_t osd_tree_attention_workspace_bytes(int B, int N, int q_heads, int kv_heads, int head_dim);
-int osd_tree_attention(const void* q, int64_t q_stride, int q_heads, const void* k_cache, const void* v_cache,
-                       int64_t page_stride, int pages, int page_size, int kv_heads, int head_dim, int dtype,
-                       const int32_t* page_table, int table_len, const int32_t* seq_len, int B, int N,
-                       const int32_t* parent, const int32_t* new_len, float scale, void* out, void* workspace,
-                       size_t workspace_bytes, void* stream);
+int osd_tree_attention(const osd_attention* call, void* stream);
 
 /*
  * osd_cache_keep -- the accepted path's keys and values move to where the context
@@ -603,10 +633,15 @@ int osd_tree_attention(const void* q, int64_t q_stride, int q_heads, const void*
  * (-1: an invalid tree), the path is no ascending list of nodes in 1 .. N - 1, or
  * the root or a node on the path has no place.
  */
-int osd_cache_keep(void* k_cache, void* v_cache, int64_t page_stride, int pages, int page_size, int kv_heads,
-                   int head_dim, int dtype, int layers, int64_t layer_stride, const int32_t* page_table,
-                   int table_len, const int32_t* seq_len, int B, int N, const int32_t* path_nodes,
-                   const int32_t* accepted_len, int32_t* new_seq_len, void* stream);
+typedef struct {
+    osd_cache cache;
+    int64_t layer_stride;
+    const int32_t* path_nodes;
+    const int32_t* accepted_len;
+    int32_t* new_seq_len;
+    int32_t layers, reserved;
+} osd_keep;
+int osd_cache_keep(const osd_keep* call, void* stream);
 
 /*
  * Vocabulary-sharded verification.  When the target and draft LM heads are

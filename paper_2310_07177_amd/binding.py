@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 import threading
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -113,17 +114,11 @@ def lib():
             L.osd_verify_topk.restype = i32
             L.osd_verify_topk.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, f32, vp, vp, vp, vp,
                                           sz, vp]
-            L.osd_cache_append.restype = i32
-            L.osd_cache_append.argtypes = [vp, vp, i64, i32, i32, i32, i32, i32, vp, i32, vp, vp, i64, vp, i64, i32,
-                                           vp, i64, vp, i64, i32, i32, vp, vp, vp, i32, i32, i32, vp]
+            for f in (L.osd_cache_append, L.osd_tree_attention, L.osd_cache_keep):
+                f.restype = i32
+                f.argtypes = [ctypes.c_char_p, vp]
             L.osd_tree_attention_workspace_bytes.restype = sz
             L.osd_tree_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
-            L.osd_tree_attention.restype = i32
-            L.osd_tree_attention.argtypes = [vp, i64, i32, vp, vp, i64, i32, i32, i32, i32, i32, vp, i32, vp, i32,
-                                             i32, vp, vp, f32, vp, vp, sz, vp]
-            L.osd_cache_keep.restype = i32
-            L.osd_cache_keep.argtypes = [vp, vp, i64, i32, i32, i32, i32, i32, i32, i64, vp, i32, vp, i32, i32, vp,
-                                         vp, vp, vp]
             _lib = L
     return _lib
 
@@ -713,24 +708,32 @@ def osd_verify_topk(target_logits, draft_ids, draft_top, draft_tokens, u_accept,
     return acc, toks, rmask
 
 
-def _cache_args(k_cache, v_cache, page_table, seq_len, layers=False):
-    """The C ABI's description of a paged cache, checked."""
+# The structs of the calls on the paged cache (osd_append, osd_attention and osd_keep in
+# include/osd.h), packed at once: an argument of a ctypes call costs 0.1 us.
+_CACHE = "=5q8i"
+_APPEND = struct.Struct(_CACHE + "11q4i")
+_ATTENTION = struct.Struct(_CACHE + "7qif")
+_KEEP = struct.Struct(_CACHE + "4q2i")
+
+
+def _cache_args(k_cache, v_cache, page_table, seq_len, layers):
+    """The C ABI's description of a paged cache, checked; `layers`: its leading axes."""
     torch = _torch()
-    if k_cache.dim() != 4 + layers or v_cache.shape != k_cache.shape:
+    shape, stride = k_cache.shape, k_cache.stride()
+    if len(shape) != 4 + layers or v_cache.shape != shape:
         raise ValueError("the caches must be two " + ("[layers, " if layers else "[")
                          + "pages, kv_heads, page_size, head_dim] tensors of one shape")
     if v_cache.dtype != k_cache.dtype:
         raise TypeError("the caches must share a dtype")
-    P, H, S, D = k_cache.shape[layers:]
-    stride = k_cache.stride()[layers:]
-    if v_cache.stride() != k_cache.stride() or stride[3] != 1 or stride[2] != D or stride[1] != S * D:
+    P, H, S, D = shape[layers:]
+    if v_cache.stride() != stride or stride[-3:] != (S * D, D, 1):
         raise ValueError("a page must be contiguous, and the caches' strides the same")
-    if page_table.dim() != 2:
-        raise ValueError("page_table must be [B, pages of a sequence]")
-    B, table_len = page_table.shape
-    _check_out(page_table, (B, table_len), torch.int32, "page_table")
-    _check_out(seq_len, (B,), torch.int32, "seq_len")
-    return B, table_len, stride[0], P, H, S, D, _dtype_code(k_cache)
+    int32 = torch.int32
+    at = page_table.shape
+    if len(at) != 2 or page_table.dtype != int32 or not page_table.is_contiguous():
+        raise ValueError("page_table must be a contiguous int32 tensor [B, pages of a sequence]")
+    _check_out(seq_len, at[:1], int32, "seq_len")
+    return at[0], at[1], stride[layers], P, H, S, D, _dtype_code(k_cache)
 
 
 def _token_stride(t, B, N, H, D, dtype, name):
@@ -742,6 +745,30 @@ def _token_stride(t, B, N, H, D, dtype, name):
     if s[3] != 1 or (H > 1 and s[2] != D) or (B > 1 and s[0] != N * step):
         raise ValueError(f"{name}: a token's heads must lie one after another, tokens at one distance")
     return step
+
+
+def _one_gpu(*ts):
+    """The GPU that all tensors given live on (its index)."""
+    at = ts[0].get_device()
+    for t in ts:
+        if t is not None and t.get_device() != at:
+            at = -1
+    if at < 0:
+        raise ValueError("every tensor argument must live on one GPU")
+    return at
+
+
+def _cache_call(name, call, at):
+    """One of the calls on the cache, on the GPU `at`, on its current stream."""
+    c = _torch()._C
+    fn = getattr(lib(), name)
+    if c._cuda_getDevice() == at:
+        st = fn(call, c._cuda_getCurrentRawStream(at))
+    else:
+        with _torch().cuda.device(at):
+            st = fn(call, c._cuda_getCurrentRawStream(at))
+    if st != OSD_OK:
+        raise OsdError(name, st)
 
 
 def osd_cache_append(k, v, k_cache, v_cache, page_table, seq_len, q=None, rotation=None, pairs=False, parent=None,
@@ -759,39 +786,36 @@ def osd_cache_append(k, v, k_cache, v_cache, page_table, seq_len, q=None, rotati
     [B, N] int32 as osd_verify_tree takes it, or None: a chain.  new_len [B]
     int32: how many of the N tokens a sequence has.  Returns the rotated
     queries (new, or `q_out`, which may be q) or None."""
-    torch = _torch()
-    B, table_len, page_stride, P, H, S, D, code = _cache_args(k_cache, v_cache, page_table, seq_len)
-    dev = k_cache.device
-    _check_same_device(dev, k, v, k_cache, v_cache, page_table, seq_len, q, rotation, parent, new_len, q_out)
+    B, table_len, page_stride, P, H, S, D, code = _cache_args(k_cache, v_cache, page_table, seq_len, 0)
+    at = _one_gpu(k_cache, v_cache, k, v, page_table, seq_len, q, rotation, parent, new_len, q_out)
     if k.dim() != 4 or (q is not None and q.dim() != 4):
         raise ValueError("k, v and q must be [B, N, heads, head_dim]")
     N, dt = k.shape[1], k_cache.dtype
     k_step, v_step = _token_stride(k, B, N, H, D, dt, "k"), _token_stride(v, B, N, H, D, dt, "v")
-    Hq = q_step = out_step = 0
+    Hq = q_step = out_step = qp = op = rows = R = rp = 0
     if q is not None:
         Hq = q.shape[2]
-        q_step = _token_stride(q, B, N, Hq, D, dt, "q")
+        q_step, qp = _token_stride(q, B, N, Hq, D, dt, "q"), q.data_ptr()
         if q_out is None:
-            q_out = torch.empty(B, N, Hq, D, dtype=dt, device=dev)
+            q_out = q.new_empty((B, N, Hq, D))
             out_step = Hq * D
         else:
             out_step = _token_stride(q_out, B, N, Hq, D, dt, "q_out")
+        op = q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("q_out without q")
-    rows = R = 0
     if rotation is not None:
         if rotation.dim() != 2:
             raise ValueError("rotation must be [positions, rotary_dim]")
         rows, R = rotation.shape
-        _check_out(rotation, (rows, R), torch.float32, "rotation")
-    _check_out(parent, (B, N), torch.int32, "parent")
-    _check_out(new_len, (B,), torch.int32, "new_len")
-    st = _on_device(dev, lib().osd_cache_append, _ptr(k_cache), _ptr(v_cache), page_stride, P, S, H, D, code,
-                    _ptr(page_table), table_len, _ptr(seq_len), _ptr(q), q_step, _ptr(q_out), out_step, Hq, _ptr(k),
-                    k_step, _ptr(v), v_step, B, N, _ptr(parent), _ptr(new_len), _ptr(rotation), rows, R,
-                    OSD_ROTATE_PAIRS if pairs else OSD_ROTATE_HALVES, _stream_handle(dev))
-    if st != OSD_OK:
-        raise OsdError("osd_cache_append", st)
+        _check_out(rotation, (rows, R), _torch().float32, "rotation")
+        rp = rotation.data_ptr()
+    _check_out(parent, (B, N), _torch().int32, "parent")
+    _check_out(new_len, (B,), _torch().int32, "new_len")
+    _cache_call("osd_cache_append", _APPEND.pack(
+        k_cache.data_ptr(), v_cache.data_ptr(), page_stride, page_table.data_ptr(), seq_len.data_ptr(), P, S, H, D,
+        code, table_len, B, N, qp, q_step, op, out_step, k.data_ptr(), k_step, v.data_ptr(), v_step, _ptr(parent) or 0,
+        _ptr(new_len) or 0, rp, Hq, rows, R, OSD_ROTATE_PAIRS if pairs else OSD_ROTATE_HALVES), at)
     return q_out
 
 
@@ -803,28 +827,23 @@ def osd_tree_attention(q, k_cache, v_cache, page_table, seq_len, parent=None, ne
     q [B, N, q_heads, head_dim] (any distance between tokens), the other
     arguments as osd_cache_append; scale: 1 / sqrt(head_dim) by default.
     Returns [B, N, q_heads, head_dim] as a new (or the given `out`) tensor."""
-    torch = _torch()
-    B, table_len, page_stride, P, H, S, D, code = _cache_args(k_cache, v_cache, page_table, seq_len)
-    dev = q.device
-    _check_same_device(dev, q, k_cache, v_cache, page_table, seq_len, parent, new_len, out)
+    B, table_len, page_stride, P, H, S, D, code = _cache_args(k_cache, v_cache, page_table, seq_len, 0)
+    at = _one_gpu(q, k_cache, v_cache, page_table, seq_len, parent, new_len, out)
     if q.dim() != 4:
         raise ValueError("q must be [B, N, q_heads, head_dim]")
-    N, Hq = q.shape[1], q.shape[2]
+    N, Hq = q.shape[1:3]
     step = _token_stride(q, B, N, Hq, D, k_cache.dtype, "q")
-    _check_out(parent, (B, N), torch.int32, "parent")
-    _check_out(new_len, (B,), torch.int32, "new_len")
+    _check_out(parent, (B, N), _torch().int32, "parent")
+    _check_out(new_len, (B,), _torch().int32, "new_len")
     if out is None:
-        out = torch.empty(B, N, Hq, D, dtype=q.dtype, device=dev)
+        out = q.new_empty((B, N, Hq, D))
     else:
         _check_out(out, (B, N, Hq, D), q.dtype, "out")
-    L = lib()
-    ws = workspace("tree_attention", L.osd_tree_attention_workspace_bytes(B, N, Hq, H, D), dev, _scratch)
-    st = _on_device(dev, L.osd_tree_attention, _ptr(q), step, Hq, _ptr(k_cache), _ptr(v_cache), page_stride, P, S, H,
-                    D, code, _ptr(page_table), table_len, _ptr(seq_len), B, N, _ptr(parent), _ptr(new_len),
-                    D ** -0.5 if scale is None else float(scale), _ptr(out), _ptr(ws), ws.numel(),
-                    _stream_handle(dev))
-    if st != OSD_OK:
-        raise OsdError("osd_tree_attention", st)
+    ws = workspace("tree_attention", lib().osd_tree_attention_workspace_bytes(B, N, Hq, H, D), q.device, _scratch)
+    _cache_call("osd_tree_attention", _ATTENTION.pack(
+        k_cache.data_ptr(), v_cache.data_ptr(), page_stride, page_table.data_ptr(), seq_len.data_ptr(), P, S, H, D,
+        code, table_len, B, N, q.data_ptr(), step, _ptr(parent) or 0, _ptr(new_len) or 0, out.data_ptr(),
+        ws.data_ptr(), ws.numel(), Hq, D ** -0.5 if scale is None else float(scale)), at)
     return out
 
 
@@ -836,24 +855,25 @@ def osd_cache_keep(k_cache, v_cache, page_table, seq_len, path_nodes, accepted_l
     layer: without the first axis), path_nodes [B, N] and accepted_len [B]
     int32 as osd_verify_tree returns them.  Returns the new context lengths [B]
     int32 (a new tensor, or the given `out`, not seq_len itself)."""
-    torch = _torch()
     if k_cache.dim() == 4:
-        k_cache, v_cache = k_cache.unsqueeze(0), v_cache.unsqueeze(0)
-    B, table_len, page_stride, P, H, S, D, code = _cache_args(k_cache, v_cache, page_table, seq_len, layers=True)
-    dev = k_cache.device
-    _check_same_device(dev, k_cache, v_cache, page_table, seq_len, path_nodes, accepted_len, out)
+        layers = 1
+        B, table_len, page_stride, P, H, S, D, code = _cache_args(k_cache, v_cache, page_table, seq_len, 0)
+        layer_stride = 0
+    else:
+        B, table_len, page_stride, P, H, S, D, code = _cache_args(k_cache, v_cache, page_table, seq_len, 1)
+        layers, layer_stride = k_cache.shape[0], k_cache.stride(0)
+    at = _one_gpu(k_cache, v_cache, page_table, seq_len, path_nodes, accepted_len, out)
     if path_nodes.dim() != 2:
         raise ValueError("path_nodes must be [B, N]")
     N = path_nodes.shape[1]
-    _check_out(path_nodes, (B, N), torch.int32, "path_nodes")
-    _check_out(accepted_len, (B,), torch.int32, "accepted_len")
+    _check_out(path_nodes, (B, N), _torch().int32, "path_nodes")
+    _check_out(accepted_len, (B,), _torch().int32, "accepted_len")
     if out is None:
-        out = torch.empty(B, dtype=torch.int32, device=dev)
+        out = seq_len.new_empty((B,))
     else:
-        _check_out(out, (B,), torch.int32, "out")
-    st = _on_device(dev, lib().osd_cache_keep, _ptr(k_cache), _ptr(v_cache), page_stride, P, S, H, D, code,
-                    k_cache.shape[0], k_cache.stride(0), _ptr(page_table), table_len, _ptr(seq_len), B, N,
-                    _ptr(path_nodes), _ptr(accepted_len), _ptr(out), _stream_handle(dev))
-    if st != OSD_OK:
-        raise OsdError("osd_cache_keep", st)
+        _check_out(out, (B,), _torch().int32, "out")
+    _cache_call("osd_cache_keep", _KEEP.pack(
+        k_cache.data_ptr(), v_cache.data_ptr(), page_stride, page_table.data_ptr(), seq_len.data_ptr(), P, S, H, D,
+        code, table_len, B, N, layer_stride, path_nodes.data_ptr(), accepted_len.data_ptr(), out.data_ptr(), layers, 0),
+        at)
     return out

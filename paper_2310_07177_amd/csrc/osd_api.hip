@@ -823,43 +823,41 @@ constexpr int64_t kMaxStride = int64_t(1) << 40, kMaxTokenStride = int64_t(1) <<
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// The cache arguments that the three operators share.
-int check_cache(const void* k_cache, const void* v_cache, int64_t page_stride, int pages, int page_size, int kv_heads,
-                int head_dim, int dtype, const int32_t* page_table, int table_len, const int32_t* seq_len, int B,
-                int N) {
-    if (dtype != OSD_F32 && dtype != OSD_BF16) return OSD_ERR_INVALID_ARG;
-    if (pages <= 0 || page_size <= 0 || kv_heads <= 0 || head_dim <= 0 || table_len <= 0 || B <= 0 || N <= 0)
+// The arguments that the three operators share.
+int check_cache(const osd_cache& c) {
+    if (c.dtype != OSD_F32 && c.dtype != OSD_BF16) return OSD_ERR_INVALID_ARG;
+    if (c.pages <= 0 || c.page_size <= 0 || c.kv_heads <= 0 || c.head_dim <= 0 || c.table_len <= 0 || c.B <= 0 || c.N <= 0)
         return OSD_ERR_INVALID_ARG;
-    if (!k_cache || !v_cache || !page_table || !seq_len) return OSD_ERR_INVALID_ARG;
-    if (head_dim % 8 || head_dim > OSD_MAX_HEAD_DIM || B > OSD_MAX_CACHE_BATCH) return OSD_ERR_UNSUPPORTED;
-    const int64_t es = dtype == OSD_BF16 ? 2 : 4;
-    if (int64_t(table_len) * page_size > (int64_t(1) << 30) ||
-        int64_t(table_len) * page_size * B > (int64_t(1) << 36) || int64_t(page_size) * head_dim * es > 0x7FFFFFFFll)
+    if (!c.k_cache || !c.v_cache || !c.page_table || !c.seq_len) return OSD_ERR_INVALID_ARG;
+    if (c.head_dim % 8 || c.head_dim > OSD_MAX_HEAD_DIM || c.B > OSD_MAX_CACHE_BATCH) return OSD_ERR_UNSUPPORTED;
+    const int64_t es = c.dtype == OSD_BF16 ? 2 : 4, covered = int64_t(c.table_len) * c.page_size;
+    if (covered > (int64_t(1) << 30) || covered * c.B > (int64_t(1) << 36) ||
+        int64_t(c.page_size) * c.head_dim * es > 0x7FFFFFFFll)
         return OSD_ERR_INVALID_ARG;
-    if (kv_heads > 65535 || page_stride < int64_t(kv_heads) * page_size * head_dim ||
-        page_stride > kMaxStride || page_stride * es % 16)
+    if (c.kv_heads > 65535 || c.page_stride < int64_t(c.kv_heads) * c.page_size * c.head_dim ||
+        c.page_stride > kMaxStride || c.page_stride * es % 16)
         return OSD_ERR_INVALID_ARG;
-    if (!aligned16(k_cache) || !aligned16(v_cache)) return OSD_ERR_INVALID_ARG;
+    if (!aligned16(c.k_cache) || !aligned16(c.v_cache)) return OSD_ERR_INVALID_ARG;
     return OSD_OK;
 }
 
-osd::CachePages cache_pages(int64_t page_stride, int pages, int page_size, int head_dim, int dtype,
-                            const int32_t* page_table, int table_len) {
-    const int64_t es = dtype == OSD_BF16 ? 2 : 4;
+osd::CachePages cache_pages(const osd_cache& cache) {
+    const int64_t es = cache.dtype == OSD_BF16 ? 2 : 4;
+    const int page_size = cache.page_size;
     osd::CachePages c;
-    c.table = page_table;
-    c.table_len = table_len;
-    c.pages = pages;
+    c.table = cache.page_table;
+    c.table_len = cache.table_len;
+    c.pages = cache.pages;
     c.page_size = page_size;
-    c.capacity = table_len * page_size;
+    c.capacity = cache.table_len * page_size;
     // With l = ceil(log2 S), m = ceil(2^(31 + l) / S) < 2^32: j m / 2^(31 + l) is above j / S by less
     // than j / 2^(31 + l) < 2^-l <= 1 / S for j < 2^31, so it does not reach the next whole number.
     int l = 0;
     while ((int64_t(1) << l) < page_size) ++l;
     c.shift = uint32_t(31 + l);
     c.magic = uint32_t(((uint64_t(1) << c.shift) + uint64_t(page_size) - 1) / uint64_t(page_size));
-    c.page_bytes = page_stride * es;
-    c.row_bytes = int(head_dim * es);
+    c.page_bytes = cache.page_stride * es;
+    c.row_bytes = int(cache.head_dim * es);
     c.head_bytes = int64_t(page_size) * c.row_bytes;
     return c;
 }
@@ -873,59 +871,58 @@ bool stride_ok(int64_t stride, int heads, int head_dim, int64_t es) {
 
 extern "C" {
 
-int osd_cache_append(void* k_cache, void* v_cache, int64_t page_stride, int pages, int page_size, int kv_heads,
-                     int head_dim, int dtype, const int32_t* page_table, int table_len, const int32_t* seq_len,
-                     const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, int q_heads,
-                     const void* k, int64_t k_stride, const void* v, int64_t v_stride, int B, int N,
-                     const int32_t* parent, const int32_t* new_len, const float* rotation, int rotation_rows,
-                     int rotary_dim, int rotation_style, void* stream) {
-    const int st = check_cache(k_cache, v_cache, page_stride, pages, page_size, kv_heads, head_dim, dtype, page_table,
-                               table_len, seq_len, B, N);
+int osd_cache_append(const osd_append* call, void* stream) {
+    if (!call) return OSD_ERR_INVALID_ARG;
+    const osd_append& c = *call;
+    const osd_cache& m = c.cache;
+    const int st = check_cache(m);
     if (st != OSD_OK) return st;
-    if (int64_t(B) * N > 0x7FFFFFFFll || (parent && N > OSD_MAX_TREE_NODES)) return OSD_ERR_INVALID_ARG;
-    const int64_t es = dtype == OSD_BF16 ? 2 : 4, tokens = int64_t(B) * N;
-    if (!k || !v || !aligned16(k) || !aligned16(v) || (!q) != (!q_out)) return OSD_ERR_INVALID_ARG;
-    if (!stride_ok(k_stride, kv_heads, head_dim, es) || !stride_ok(v_stride, kv_heads, head_dim, es))
+    if (int64_t(m.B) * m.N > 0x7FFFFFFFll || (c.parent && m.N > OSD_MAX_TREE_NODES)) return OSD_ERR_INVALID_ARG;
+    const int64_t es = m.dtype == OSD_BF16 ? 2 : 4, tokens = int64_t(m.B) * m.N;
+    if (!c.k || !c.v || !aligned16(c.k) || !aligned16(c.v) || (!c.q) != (!c.q_out)) return OSD_ERR_INVALID_ARG;
+    if (!stride_ok(c.k_stride, m.kv_heads, m.head_dim, es) || !stride_ok(c.v_stride, m.kv_heads, m.head_dim, es))
         return OSD_ERR_INVALID_ARG;
-    if (q) {
-        if (q_heads <= 0 || q_heads > 65535 || !aligned16(q) || !aligned16(q_out)) return OSD_ERR_INVALID_ARG;
-        if (!stride_ok(q_stride, q_heads, head_dim, es) || !stride_ok(q_out_stride, q_heads, head_dim, es))
+    if (c.q) {
+        if (c.q_heads <= 0 || c.q_heads > 65535 || !aligned16(c.q) || !aligned16(c.q_out)) return OSD_ERR_INVALID_ARG;
+        if (!stride_ok(c.q_stride, c.q_heads, m.head_dim, es) || !stride_ok(c.q_out_stride, c.q_heads, m.head_dim, es))
             return OSD_ERR_INVALID_ARG;
-        const uint64_t row = uint64_t(q_heads) * head_dim * es;
-        if (!(q_out == q && q_out_stride == q_stride) &&
-            meets(q, uint64_t((tokens - 1) * q_stride * es) + row, q_out, uint64_t((tokens - 1) * q_out_stride * es) + row))
+        const uint64_t row = uint64_t(c.q_heads) * m.head_dim * es;
+        if (!(c.q_out == c.q && c.q_out_stride == c.q_stride) &&
+            meets(c.q, uint64_t((tokens - 1) * c.q_stride * es) + row, c.q_out,
+                  uint64_t((tokens - 1) * c.q_out_stride * es) + row))
             return OSD_ERR_INVALID_ARG;
     }
-    if (rotation) {
-        if (rotation_rows <= 0 || rotary_dim <= 0 || rotary_dim % 2 || rotary_dim > head_dim) return OSD_ERR_INVALID_ARG;
-        if (rotation_style != OSD_ROTATE_HALVES && rotation_style != OSD_ROTATE_PAIRS) return OSD_ERR_INVALID_ARG;
-        if (!aligned16(rotation)) return OSD_ERR_INVALID_ARG;
+    if (c.rotation) {
+        if (c.rotation_rows <= 0 || c.rotary_dim <= 0 || c.rotary_dim % 2 || c.rotary_dim > m.head_dim)
+            return OSD_ERR_INVALID_ARG;
+        if (c.rotation_style != OSD_ROTATE_HALVES && c.rotation_style != OSD_ROTATE_PAIRS) return OSD_ERR_INVALID_ARG;
+        if (!aligned16(c.rotation)) return OSD_ERR_INVALID_ARG;
     }
     osd::AppendLaunch L;
-    L.k_cache = static_cast<char*>(k_cache);
-    L.v_cache = static_cast<char*>(v_cache);
-    L.pages = cache_pages(page_stride, pages, page_size, head_dim, dtype, page_table, table_len);
-    L.seq_len = seq_len;
-    L.q = static_cast<const char*>(q);
-    L.q_out = static_cast<char*>(q_out);
-    L.k = static_cast<const char*>(k);
-    L.v = static_cast<const char*>(v);
-    L.q_stride = q_stride * es;
-    L.q_out_stride = q_out_stride * es;
-    L.k_stride = k_stride * es;
-    L.v_stride = v_stride * es;
-    L.dtype = dtype;
-    L.B = B;
-    L.N = N;
-    L.q_heads = q ? q_heads : 0;
-    L.kv_heads = kv_heads;
-    L.head_dim = head_dim;
-    L.parent = parent;
-    L.new_len = new_len;
-    L.rotation = rotation;
-    L.rotation_rows = rotation ? rotation_rows : 0;
-    L.rotary_dim = rotation ? rotary_dim : 0;
-    L.style = rotation_style;
+    L.k_cache = static_cast<char*>(m.k_cache);
+    L.v_cache = static_cast<char*>(m.v_cache);
+    L.pages = cache_pages(m);
+    L.seq_len = m.seq_len;
+    L.q = static_cast<const char*>(c.q);
+    L.q_out = static_cast<char*>(c.q_out);
+    L.k = static_cast<const char*>(c.k);
+    L.v = static_cast<const char*>(c.v);
+    L.q_stride = c.q_stride * es;
+    L.q_out_stride = c.q_out_stride * es;
+    L.k_stride = c.k_stride * es;
+    L.v_stride = c.v_stride * es;
+    L.dtype = m.dtype;
+    L.B = m.B;
+    L.N = m.N;
+    L.q_heads = c.q ? c.q_heads : 0;
+    L.kv_heads = m.kv_heads;
+    L.head_dim = m.head_dim;
+    L.parent = c.parent;
+    L.new_len = c.new_len;
+    L.rotation = c.rotation;
+    L.rotation_rows = c.rotation ? c.rotation_rows : 0;
+    L.rotary_dim = c.rotation ? c.rotary_dim : 0;
+    L.style = c.rotation_style;
     L.stream = static_cast<hipStream_t>(stream);
     return osd::launch_append(L) == hipSuccess ? OSD_OK : OSD_ERR_DEVICE;
 }
@@ -937,73 +934,71 @@ size_t osd_tree_attention_workspace_bytes(int B, int N, int q_heads, int kv_head
     return round_up(osd::tree_attention_workspace(N, q_heads, kv_heads, head_dim), kAlign);
 }
 
-int osd_tree_attention(const void* q, int64_t q_stride, int q_heads, const void* k_cache, const void* v_cache,
-                       int64_t page_stride, int pages, int page_size, int kv_heads, int head_dim, int dtype,
-                       const int32_t* page_table, int table_len, const int32_t* seq_len, int B, int N,
-                       const int32_t* parent, const int32_t* new_len, float scale, void* out, void* workspace,
-                       size_t workspace_bytes, void* stream) {
-    const int st = check_cache(k_cache, v_cache, page_stride, pages, page_size, kv_heads, head_dim, dtype, page_table,
-                               table_len, seq_len, B, N);
+int osd_tree_attention(const osd_attention* call, void* stream) {
+    if (!call) return OSD_ERR_INVALID_ARG;
+    const osd_attention& c = *call;
+    const osd_cache& m = c.cache;
+    const int st = check_cache(m);
     if (st != OSD_OK) return st;
-    if (N > OSD_MAX_TREE_NODES || q_heads <= 0 || q_heads > 65535 || q_heads % kv_heads) return OSD_ERR_INVALID_ARG;
-    const int64_t es = dtype == OSD_BF16 ? 2 : 4;
-    if (!q || !out || !aligned16(q) || !aligned16(out)) return OSD_ERR_INVALID_ARG;
-    if (!stride_ok(q_stride, q_heads, head_dim, es)) return OSD_ERR_INVALID_ARG;
-    if (!(scale - scale == 0.0f)) return OSD_ERR_INVALID_ARG;  // NaN, infinite
-    const uint64_t row = uint64_t(q_heads) * head_dim * es, tokens = uint64_t(B) * N;
-    if (meets(q, (tokens - 1) * uint64_t(q_stride * es) + row, out, tokens * row)) return OSD_ERR_INVALID_ARG;
-    if (!workspace || workspace_bytes < osd_tree_attention_workspace_bytes(B, N, q_heads, kv_heads, head_dim) ||
-        !aligned16(workspace))
+    if (m.N > OSD_MAX_TREE_NODES || c.q_heads <= 0 || c.q_heads > 65535 || c.q_heads % m.kv_heads)
+        return OSD_ERR_INVALID_ARG;
+    const int64_t es = m.dtype == OSD_BF16 ? 2 : 4;
+    if (!c.q || !c.out || !aligned16(c.q) || !aligned16(c.out)) return OSD_ERR_INVALID_ARG;
+    if (!stride_ok(c.q_stride, c.q_heads, m.head_dim, es)) return OSD_ERR_INVALID_ARG;
+    if (!(c.scale - c.scale == 0.0f)) return OSD_ERR_INVALID_ARG;  // NaN, infinite
+    const uint64_t row = uint64_t(c.q_heads) * m.head_dim * es, tokens = uint64_t(m.B) * m.N;
+    if (meets(c.q, (tokens - 1) * uint64_t(c.q_stride * es) + row, c.out, tokens * row)) return OSD_ERR_INVALID_ARG;
+    if (!c.workspace || !aligned16(c.workspace) ||
+        c.workspace_bytes < osd_tree_attention_workspace_bytes(m.B, m.N, c.q_heads, m.kv_heads, m.head_dim))
         return OSD_ERR_WORKSPACE;
     osd::TreeAttentionLaunch L;
-    L.q = static_cast<const char*>(q);
-    L.q_stride = q_stride * es;
-    L.k_cache = static_cast<const char*>(k_cache);
-    L.v_cache = static_cast<const char*>(v_cache);
-    L.pages = cache_pages(page_stride, pages, page_size, head_dim, dtype, page_table, table_len);
-    L.seq_len = seq_len;
-    L.dtype = dtype;
-    L.B = B;
-    L.N = N;
-    L.q_heads = q_heads;
-    L.kv_heads = kv_heads;
-    L.head_dim = head_dim;
-    L.parent = parent;
-    L.new_len = new_len;
-    L.scale = scale;
-    L.out = static_cast<char*>(out);
-    L.workspace = static_cast<char*>(workspace);
+    L.q = static_cast<const char*>(c.q);
+    L.q_stride = c.q_stride * es;
+    L.k_cache = static_cast<const char*>(m.k_cache);
+    L.v_cache = static_cast<const char*>(m.v_cache);
+    L.pages = cache_pages(m);
+    L.seq_len = m.seq_len;
+    L.dtype = m.dtype;
+    L.B = m.B;
+    L.N = m.N;
+    L.q_heads = c.q_heads;
+    L.kv_heads = m.kv_heads;
+    L.head_dim = m.head_dim;
+    L.parent = c.parent;
+    L.new_len = c.new_len;
+    L.scale = c.scale;
+    L.out = static_cast<char*>(c.out);
+    L.workspace = static_cast<char*>(c.workspace);
     L.stream = static_cast<hipStream_t>(stream);
     L.cus = device_cus(L.stream);
     return osd::launch_tree_attention(L) == hipSuccess ? OSD_OK : OSD_ERR_DEVICE;
 }
 
-int osd_cache_keep(void* k_cache, void* v_cache, int64_t page_stride, int pages, int page_size, int kv_heads,
-                   int head_dim, int dtype, int layers, int64_t layer_stride, const int32_t* page_table,
-                   int table_len, const int32_t* seq_len, int B, int N, const int32_t* path_nodes,
-                   const int32_t* accepted_len, int32_t* new_seq_len, void* stream) {
-    const int st = check_cache(k_cache, v_cache, page_stride, pages, page_size, kv_heads, head_dim, dtype, page_table,
-                               table_len, seq_len, B, N);
+int osd_cache_keep(const osd_keep* call, void* stream) {
+    if (!call) return OSD_ERR_INVALID_ARG;
+    const osd_keep& c = *call;
+    const osd_cache& m = c.cache;
+    const int st = check_cache(m);
     if (st != OSD_OK) return st;
-    const int64_t es = dtype == OSD_BF16 ? 2 : 4;
-    if (N > OSD_MAX_TREE_NODES || layers <= 0 || layers > 65535 || layer_stride < 0 || layer_stride > kMaxStride ||
-        layer_stride * es % 16)
+    const int64_t es = m.dtype == OSD_BF16 ? 2 : 4;
+    if (m.N > OSD_MAX_TREE_NODES || c.layers <= 0 || c.layers > 65535 || c.layer_stride < 0 ||
+        c.layer_stride > kMaxStride || c.layer_stride * es % 16)
         return OSD_ERR_INVALID_ARG;
-    if (!path_nodes || !accepted_len || !new_seq_len) return OSD_ERR_INVALID_ARG;
-    if (meets(seq_len, uint64_t(B) * 4, new_seq_len, uint64_t(B) * 4)) return OSD_ERR_INVALID_ARG;
+    if (!c.path_nodes || !c.accepted_len || !c.new_seq_len) return OSD_ERR_INVALID_ARG;
+    if (meets(m.seq_len, uint64_t(m.B) * 4, c.new_seq_len, uint64_t(m.B) * 4)) return OSD_ERR_INVALID_ARG;
     osd::KeepLaunch L;
-    L.k_cache = static_cast<char*>(k_cache);
-    L.v_cache = static_cast<char*>(v_cache);
-    L.pages = cache_pages(page_stride, pages, page_size, head_dim, dtype, page_table, table_len);
-    L.layer_bytes = layer_stride * es;
-    L.layers = layers;
-    L.seq_len = seq_len;
-    L.B = B;
-    L.N = N;
-    L.kv_heads = kv_heads;
-    L.path_nodes = path_nodes;
-    L.accepted_len = accepted_len;
-    L.new_seq_len = new_seq_len;
+    L.k_cache = static_cast<char*>(m.k_cache);
+    L.v_cache = static_cast<char*>(m.v_cache);
+    L.pages = cache_pages(m);
+    L.layer_bytes = c.layer_stride * es;
+    L.layers = c.layers;
+    L.seq_len = m.seq_len;
+    L.B = m.B;
+    L.N = m.N;
+    L.kv_heads = m.kv_heads;
+    L.path_nodes = c.path_nodes;
+    L.accepted_len = c.accepted_len;
+    L.new_seq_len = c.new_seq_len;
     L.stream = static_cast<hipStream_t>(stream);
     return osd::launch_keep(L) == hipSuccess ? OSD_OK : OSD_ERR_DEVICE;
 }

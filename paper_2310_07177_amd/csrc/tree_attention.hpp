@@ -596,7 +596,7 @@ __device__ inline void join(const Args& a, const Piece& p, const Division& share
     // A read takes about 2 us, so as many as registers allow are in flight.
     if (count <= 2) join_parts<Fmt, THREADS, ROWS, DT, 8, 2>(a, p, first_slot, w0, count, D);
     else if (count <= 4) join_parts<Fmt, THREADS, ROWS, DT, 4, 4>(a, p, first_slot, w0, count, D);
-    else if (count <= 8) join_parts<Fmt, THREADS, ROWS, DT, 2, 8>(a, p, first_slot, w0, count, D);
+    else if (p.rows * (DT / 4) > THREADS) join_parts<Fmt, THREADS, ROWS, DT, 2, 8>(a, p, first_slot, w0, count, D);
     else join_parts<Fmt, THREADS, ROWS, DT, 1, 16>(a, p, first_slot, w0, count, D);
     if (tid == 0) __hip_atomic_store(&a.counters[w0], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }

@@ -5,6 +5,7 @@ import ctypes
 import pytest
 
 import paper_2310_07177_amd as osd
+from paper_2310_07177_amd import binding
 
 P = ctypes.c_void_p
 FAKE, ODD = P(0x10000), P(0x10008)  # never dereferenced: every call below fails validation
@@ -20,14 +21,19 @@ BAD_CACHE = [
 ]
 
 
+def call(name, layout, a, fields):
+    """A call's struct, in the header's order."""
+    v = [a[x] for x in ("kc", "vc", "ps", "table", "len", "pages", "S", "H", "D", "dtype", "T", "B", "N") + fields]
+    v = [(x.value or 0) if isinstance(x, P) else 0 if x is None else x for x in v]
+    return getattr(osd.lib(), name)(layout.pack(*v), None)
+
+
 def append(**kw):
     a = dict(CACHE, q=FAKE, qs=4 * 64, qo=P(0x90000), qos=4 * 64, Hq=4, k=FAKE, ks=128, v=FAKE, vs=128, B=2, N=3,
              parent=None, new=None, rot=FAKE, rows=100, R=64, style=0)
     a.update(kw)
-    return osd.lib().osd_cache_append(a["kc"], a["vc"], a["ps"], a["pages"], a["S"], a["H"], a["D"], a["dtype"],
-                                      a["table"], a["T"], a["len"], a["q"], a["qs"], a["qo"], a["qos"], a["Hq"], a["k"],
-                                      a["ks"], a["v"], a["vs"], a["B"], a["N"], a["parent"], a["new"], a["rot"],
-                                      a["rows"], a["R"], a["style"], None)
+    return call("osd_cache_append", binding._APPEND, a, ("q", "qs", "qo", "qos", "k", "ks", "v", "vs", "parent", "new", "rot",
+                                                         "Hq", "rows", "R", "style"))
 
 
 @pytest.mark.parametrize("kw,status", BAD_CACHE + [
@@ -48,9 +54,7 @@ def attention(**kw):
     a = dict(CACHE, q=FAKE, qs=256, Hq=4, B=2, N=3, parent=None, new=None, scale=0.1, out=P(0x90000), ws=FAKE,
              wsb=1 << 34)
     a.update(kw)
-    return osd.lib().osd_tree_attention(a["q"], a["qs"], a["Hq"], a["kc"], a["vc"], a["ps"], a["pages"], a["S"],
-                                        a["H"], a["D"], a["dtype"], a["table"], a["T"], a["len"], a["B"], a["N"],
-                                        a["parent"], a["new"], a["scale"], a["out"], a["ws"], a["wsb"], None)
+    return call("osd_tree_attention", binding._ATTENTION, a, ("q", "qs", "parent", "new", "out", "ws", "wsb", "Hq", "scale"))
 
 
 @pytest.mark.parametrize("kw,status", BAD_CACHE + [
@@ -64,11 +68,9 @@ def test_attention_rejects_bad_arguments(kw, status):
 
 
 def keep(**kw):
-    a = dict(CACHE, layers=2, ls=1 << 20, B=2, N=3, path=FAKE, acc=FAKE, new=P(0x90000))
+    a = dict(CACHE, layers=2, ls=1 << 20, B=2, N=3, path=FAKE, acc=FAKE, new=P(0x90000), reserved=0)
     a.update(kw)
-    return osd.lib().osd_cache_keep(a["kc"], a["vc"], a["ps"], a["pages"], a["S"], a["H"], a["D"], a["dtype"],
-                                    a["layers"], a["ls"], a["table"], a["T"], a["len"], a["B"], a["N"], a["path"],
-                                    a["acc"], a["new"], None)
+    return call("osd_cache_keep", binding._KEEP, a, ("ls", "path", "acc", "new", "layers", "reserved"))
 
 
 @pytest.mark.parametrize("kw,status", BAD_CACHE + [
@@ -78,6 +80,24 @@ def keep(**kw):
 ])
 def test_keep_rejects_bad_arguments(kw, status):
     assert keep(**kw) == status
+
+
+def test_no_call_is_refused():
+    L = osd.lib()
+    assert L.osd_cache_append(None, None) == L.osd_tree_attention(None, None) == L.osd_cache_keep(None, None) == -1
+
+
+def test_structs_are_the_headers(tmp_path):
+    """The binding packs the structs as C lays them out."""
+    import os
+    import subprocess
+    src = tmp_path / "sizes.c"
+    src.write_text('#include <stdio.h>\n#include "osd.h"\nint main(void) { printf("%zu %zu %zu", sizeof(osd_append), '
+                   'sizeof(osd_attention), sizeof(osd_keep)); return 0; }\n')
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run(["gcc", "-I", os.path.join(root, "include"), str(src), "-o", str(tmp_path / "sizes")], check=True)
+    got = subprocess.run([str(tmp_path / "sizes")], capture_output=True, text=True, check=True).stdout.split()
+    assert [int(x) for x in got] == [binding._APPEND.size, binding._ATTENTION.size, binding._KEEP.size]
 
 
 def test_workspace_sizes():
@@ -114,7 +134,6 @@ def test_binding_refuses_shapes_types_and_cpu_tensors():
 
 def test_binding_refuses_distances_that_are_not_one():
     import torch
-    from paper_2310_07177_amd import binding
     f = lambda t: binding._token_stride(t, *t.shape, t.dtype, "q")
     x = torch.zeros(2, 3, 8, 64)
     assert f(x) == 512 and f(x[:, :, 2:4]) == 512 and f(x[:, :1, :4]) == 3 * 512
