@@ -39,11 +39,11 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
     __shared__ int s_odd[kWaves];
 
     Division<kThreads, TILE> share;
-    share.init(a, s_tiles, 1);
-    const int64_t w = int64_t(blockIdx.x), first = share.begin(w), end = share.begin(w + 1);
+    share.init(a, s_tiles);
+    const int64_t w = int64_t(blockIdx.x), first = share.begin(w), end = share.end(a, w);
 
     for (int64_t pos = first; pos < end;) {
-        const Piece p = share.template find<ROWS>(a, pos, end);
+        const Piece p = share.template find<ROWS>(a, w, pos, first, end);
         const int len = p.seq.len, T = p.T;
         chunk_t q[MT][CHUNKS];
         R rows;
@@ -205,9 +205,7 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
         }
         if (lane == 0) s_odd[wave] = rows.odd;
         __syncthreads();
-        const bool whole = p.whole(), odd = s_odd[0] || s_odd[1] || s_odd[2] || s_odd[3];
-        // Where this piece's part goes: a unit that an earlier workgroup began, or one that begins here.
-        const int64_t slot = 2 * w + (pos == first ? 0 : 1);
+        const bool odd = s_odd[0] || s_odd[1] || s_odd[2] || s_odd[3];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             float all = kNegInf;
@@ -230,13 +228,13 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
                     const float s = s_stat[x][row][1];
                     total += s == s ? s * rescale(s_stat[x][row][0], most) : s;
                 }
-                if (whole) write_row<Fmt>(a, p, row, d, D, o, total);
-                else post_part<ROWS, DT>(a, slot, row, d, o, most, total);
+                if (p.whole) write_row<Fmt>(a, p, row, d, D, o, total);
+                else post_part<ROWS, DT>(a, p.slot, row, d, o, most, total);
             }
             __syncthreads();
         }
-        if (!whole) join<Fmt, kThreads, ROWS, DT>(a, p, share, pos, D);
-        pos += p.t1 - p.t0;
+        if (!p.whole) join<Fmt, kThreads, ROWS, DT>(a, p, share.apart, D);
+        pos += share.step(p);
     }
 }
 
@@ -265,7 +263,7 @@ struct Workspace {
 Workspace layout(int rows, int DT, int dtype) {
     const size_t R = size_t(block_rows(rows, DT, dtype)), slots = 2 * kMaxGroups / (R > 16 ? 2 : 1);
     Workspace w;
-    w.stats = kMaxGroups * sizeof(uint32_t);
+    w.stats = kMaxGroups * 3 * sizeof(uint32_t);
     w.parts = w.stats + slots * R * 2 * sizeof(float);
     w.total = w.parts + slots * R * DT * sizeof(float);
     return w;

@@ -179,7 +179,7 @@ struct Args {
     float c2;            // |scale| * log2(e)
     int group;           // query heads of a kv head
     int blocks;          // row blocks of a kv head
-    uint32_t* counters;  // [kMaxGroups] zero on entry and exit: arrivals of the unit that begins in a workgroup
+    uint32_t* counters;  // [kMaxGroups, 3] zero on entry and exit: of the unit that begins in a workgroup
     float* stats;        // [2 * kMaxGroups, rows, 2] maximum (times c2) and sum
     float* parts;        // [2 * kMaxGroups, rows, DT] sums of p v
     uint32_t stats_bytes, parts_bytes;
@@ -209,94 +209,125 @@ struct Piece {
     int b, h, tiles, t0, t1;
     int row0, rows, live;  // of the row block: its first row, its rows, those before padding
     int T;                 // keys
-    __device__ bool whole() const { return t0 == 0 && t1 == tiles; }
+    bool whole;
+    // Otherwise: the unit's first workgroup, how many there are, and where in the workspace
+    // their parts are (the first's; those of the others are at 2 * workgroup) and this one's.
+    int w0, count, first_slot, slot;
 };
 // Work is counted in tiles of keys.  A unit is one row block of one kv head of one
-// sequence, all its keys; units lie one after another, and every workgroup takes the
-// same number of tiles whatever the lengths, at most two pieces of which are parts of
-// units (the others it has alone).  Sequences' lengths are in registers of each wave
-// (up to 64 of them) or in LDS.
+// sequence, all its keys.  There are two ways to divide them, neither of which asks the host for
+// lengths:
+//   apart     every unit is cut into equal parts, one workgroup each.  For few units;
+//   in a row  units lie one after another, and every workgroup takes the same number of
+//             tiles: at most two pieces of units that others share, the rest alone.
+// A workgroup that ends one piece and begins another loses about 5 us (its loads run dry), so
+// units are cut apart wherever that costs at most kSlack tiles of the longest.  Sequences'
+// lengths are in registers of each wave (up to 64 of them) or in LDS.
+constexpr int kSlack = 4;
+
 template <int THREADS, int TILE>
 struct Division {
-    int* s_before;         // [B + 1] tiles of the sequences before each, of one unit (more than 64)
-    int upto, len, n;      // (up to 64) lane b: tiles up to and with sequence b, and the sequence
-    int64_t total, each;   // tiles of all units, of a workgroup
+    int* s_before;          // [B + 1] tiles of the sequences before each, of one unit (more than 64)
+    int tiles, len, n;      // (up to 64) lane b: a unit's tiles, and the sequence
+    int upto;               // (up to 64) lane b: tiles (in a row) or parts (apart) up to and with sequence b
+    int64_t total, each;    // tiles of all units, of a workgroup
+    bool apart;
 
     __device__ static int tiles_of(const Seq& s) { return s.state ? 1 : (s.len + s.n - 1) / TILE + 1; }
+    // Sums over the lanes up to each.
+    __device__ static int scan(int x) {
+        const int lane = int(threadIdx.x) & (kWave - 1);
+#pragma unroll
+        for (int o = 1; o < kWave; o *= 2) {
+            const int up = __shfl_up(x, o);
+            x += lane >= o ? up : 0;
+        }
+        return x;
+    }
 
-    // least: tiles of a workgroup.
-    __device__ void init(const Args& a, int* room, int least) {
+    __device__ void init(const Args& a, int* room) {
         const TreeAttentionLaunch& L = a.L;
         const int tid = int(threadIdx.x), lane = tid & (kWave - 1);
+        const int64_t units = int64_t(L.kv_heads) * a.blocks;
         int all;
         s_before = room;
+        apart = false;
         if (L.B <= kWave) {
             Seq s{-1, 0, 1};
             if (lane < L.B) s = sequence(L, lane);
             len = s.len;
             n = s.n;
-            upto = lane < L.B ? tiles_of(s) : 0;
-#pragma unroll
-            for (int o = 1; o < kWave; o *= 2) {
-                const int up = __shfl_up(upto, o);
-                upto += lane >= o ? up : 0;
-            }
+            tiles = lane < L.B ? tiles_of(s) : 0;
+            upto = scan(tiles);
             all = __builtin_amdgcn_readlane(upto, kWave - 1);
         } else {
             constexpr int WAVES = THREADS / kWave;
             __shared__ int s_scan[WAVES];
-            const int wave = tid / kWave, each = (L.B + THREADS - 1) / THREADS, first = tid * each;
+            const int wave = tid / kWave, share = (L.B + THREADS - 1) / THREADS, first = tid * share;
             int mine = 0;
-            for (int b = first; b < first + each && b < L.B; ++b) {
-                const int tiles = tiles_of(sequence(L, b));
-                s_before[b] = tiles;
-                mine += tiles;
+            for (int b = first; b < first + share && b < L.B; ++b) {
+                const int t = tiles_of(sequence(L, b));
+                s_before[b] = t;
+                mine += t;
             }
-            int sum = mine;
-#pragma unroll
-            for (int o = 1; o < kWave; o *= 2) {
-                const int up = __shfl_up(sum, o);
-                sum += lane >= o ? up : 0;
-            }
+            const int sum = scan(mine);
             if (lane == kWave - 1) s_scan[wave] = sum;
             __syncthreads();
             int before = sum - mine;
             for (int w = 0; w < wave; ++w) before += s_scan[w];
-            for (int b = first; b < first + each && b < L.B; ++b) {
-                const int tiles = s_before[b];
+            for (int b = first; b < first + share && b < L.B; ++b) {
+                const int t = s_before[b];
                 s_before[b] = before;
-                before += tiles;
+                before += t;
                 if (b == L.B - 1) s_before[L.B] = before;
             }
             __syncthreads();
             all = __builtin_amdgcn_readfirstlane(s_before[L.B]);
         }
-        const int64_t units = int64_t(L.kv_heads) * a.blocks;
         total = all * units;
         int64_t W = int64_t(gridDim.x);
         if (W > L.B * units * kMaxPieces) W = L.B * units * kMaxPieces;
         each = quotient(total + W - 1, W);
-        if (each < least) each = least;
+        if (L.B <= kWave && L.B * units <= W) {
+            for (int more = 0; more <= kSlack && !apart; more = more ? more * 2 : 1) {
+                const int e = int(each) + more, parts = (tiles + e - 1) / e, to = scan(parts);
+                if (__builtin_amdgcn_readlane(to, kWave - 1) * units > W) continue;
+                apart = true;
+                upto = to;
+            }
+        }
     }
-    __device__ int64_t begin(int64_t w) const { return w * each < total ? w * each : total; }
-    __device__ int owner(int64_t tile) const { return int(quotient(tile, each)); }
+    // The tiles (apart: the workgroup) that workgroup w begins with.
+    __device__ int64_t begin(int64_t w) const {
+        if (apart) return w;
+        return w * each < total ? w * each : total;
+    }
+    __device__ int64_t end(const Args& a, int64_t w) const {
+        if (!apart) return begin(w + 1);
+        const int64_t W = int64_t(__builtin_amdgcn_readlane(upto, kWave - 1)) * a.L.kv_heads * a.blocks;
+        return w < W ? w + 1 : w;
+    }
 
+    // The piece at `pos`, of a workgroup w that has the ones from `first` to `end`.
     template <int ROWS>
-    __device__ Piece find(const Args& a, int64_t pos, int64_t end) const;
+    __device__ Piece find(const Args& a, int64_t w, int64_t pos, int64_t first, int64_t end) const;
+    // What has to be added to `pos` for the next one.
+    __device__ int64_t step(const Piece& p) const { return apart ? 1 : p.t1 - p.t0; }
 };
 
 template <int THREADS, int TILE>
 template <int ROWS>
-__device__ inline Piece Division<THREADS, TILE>::find(const Args& a, int64_t pos, int64_t end) const {
+__device__ inline Piece Division<THREADS, TILE>::find(const Args& a, int64_t w, int64_t pos, int64_t first, int64_t end) const {
     const TreeAttentionLaunch& L = a.L;
     const int64_t units = int64_t(L.kv_heads) * a.blocks;
     Piece p;
-    int before;
+    int before, upto_b;
     if (L.B <= kWave) {
         const int lane = int(threadIdx.x) & (kWave - 1);
         p.b = __ffsll(static_cast<unsigned long long>(__ballot(lane < L.B && upto * units > pos))) - 1;
         before = p.b ? __builtin_amdgcn_readlane(upto, p.b - 1) : 0;
-        p.tiles = __builtin_amdgcn_readlane(upto, p.b) - before;
+        upto_b = __builtin_amdgcn_readlane(upto, p.b);
+        p.tiles = __builtin_amdgcn_readlane(tiles, p.b);
         p.seq = Seq{__builtin_amdgcn_readlane(len, p.b), __builtin_amdgcn_readlane(n, p.b), 0};
         p.seq.state = state_of(L, p.seq.len, p.seq.n);
     } else {
@@ -308,13 +339,33 @@ __device__ inline Piece Division<THREADS, TILE>::find(const Args& a, int64_t pos
         }
         p.b = __builtin_amdgcn_readfirstlane(b);
         before = __builtin_amdgcn_readfirstlane(s_before[p.b]);
-        p.tiles = __builtin_amdgcn_readfirstlane(s_before[p.b + 1]) - before;
+        upto_b = __builtin_amdgcn_readfirstlane(s_before[p.b + 1]);
+        p.tiles = upto_b - before;
         p.seq = sequence(L, p.b);
     }
     const int64_t in_b = pos - before * units;
-    const int unit = int(quotient(in_b, p.tiles));
-    p.t0 = int(in_b - int64_t(unit) * p.tiles);
-    p.t1 = int(end - pos < p.tiles - p.t0 ? p.t0 + (end - pos) : p.tiles);
+    const int length = upto_b - before, unit = int(quotient(in_b, length)), at = int(in_b - int64_t(unit) * length);
+    if (apart) {  // part `at` of `length`
+        p.t0 = int(quotient(int64_t(at) * p.tiles, length));
+        p.t1 = int(quotient(int64_t(at + 1) * p.tiles, length));
+        p.whole = length == 1;
+        p.w0 = int(w) - at;
+        p.count = length;
+        p.first_slot = 2 * p.w0;
+        p.slot = 2 * int(w);
+    } else {
+        p.t0 = at;
+        p.t1 = int(end - pos < p.tiles - at ? at + (end - pos) : p.tiles);
+        p.whole = p.t0 == 0 && p.t1 == p.tiles;
+        p.w0 = p.count = p.first_slot = 0;
+        if (!p.whole) {
+            const int64_t u0 = pos - at;
+            p.w0 = int(quotient(u0, each));
+            p.count = int(quotient(u0 + p.tiles - 1, each)) - p.w0 + 1;
+            p.first_slot = 2 * p.w0 + (p.w0 * each == u0 ? 0 : 1);
+        }
+        p.slot = 2 * int(w) + (pos == first ? 0 : 1);
+    }
     p.h = unit / a.blocks;
     p.row0 = (unit - p.h * a.blocks) * ROWS;
     p.rows = L.N * a.group - p.row0 < ROWS ? L.N * a.group - p.row0 : ROWS;
@@ -514,8 +565,8 @@ __device__ inline auto buffer_of(float* p, uint32_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(p, 0, int(bytes), 0x00027000);
 }
 template <int ROWS, int DT>
-__device__ inline void post_part(const Args& a, int64_t slot, int row, int d, f32x4_t o, float top, float sum) {
-    const int64_t at = slot * ROWS + row;
+__device__ inline void post_part(const Args& a, int slot, int row, int d, f32x4_t o, float top, float sum) {
+    const int64_t at = int64_t(slot) * ROWS + row;
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(chunk_t, o), buffer_of(a.parts, a.parts_bytes),
                                            int(uint32_t(at * DT + d) * 4u), 0, kDeviceScope);
     if (d == 0)
@@ -523,12 +574,13 @@ __device__ inline void post_part(const Args& a, int64_t slot, int row, int d, f3
                                               buffer_of(a.stats, a.stats_bytes), int(uint32_t(at) * 8u), 0, kDeviceScope);
 }
 
-// ITEMS times four values of rows, from PIECES parts in flight each.
+// Rows r0 .. r1-1 of a unit from its parts, in their order: ITEMS times four values of a
+// thread, PIECES parts in flight each.
 template <typename Fmt, int THREADS, int ROWS, int DT, int ITEMS, int PIECES>
-__device__ inline void join_parts(const Args& a, const Piece& p, int first_slot, int w0, int count, int D) {
+__device__ inline void join_parts(const Args& a, const Piece& p, int r0, int r1, int D) {
     const auto stats = buffer_of(a.stats, a.stats_bytes), parts = buffer_of(a.parts, a.parts_bytes);
-    const int items = p.rows * (DT / 4);
-    for (int i0 = int(threadIdx.x); i0 < items; i0 += THREADS * ITEMS) {
+    const int items = r1 * (DT / 4), count = p.count;
+    for (int i0 = r0 * (DT / 4) + int(threadIdx.x); i0 < items; i0 += THREADS * ITEMS) {
         float most[ITEMS], total[ITEMS];
         f32x4_t o[ITEMS];
 #pragma unroll
@@ -540,10 +592,9 @@ __device__ inline void join_parts(const Args& a, const Piece& p, int first_slot,
             for (int x = 0; x < PIECES; ++x)
 #pragma unroll
                 for (int k = 0; k < ITEMS; ++k) {
-                    // (What is not there reads as zeros, and is not used.)
                     const int i = i0 + k * THREADS, row = i / (DT / 4), d = i % (DT / 4) * 4;
                     const bool in = i < items && x0 + x < count && d < D;
-                    const uint32_t at = uint32_t(x0 + x ? 2 * (w0 + x0 + x) : first_slot) * ROWS + row;
+                    const uint32_t at = uint32_t(x0 + x ? 2 * (p.w0 + x0 + x) : p.first_slot) * ROWS + row;
                     st[k][x] = u32x2_t{0, 0};
                     part[k][x] = chunk_t{0, 0, 0, 0};
                     if (in) {
@@ -578,27 +629,63 @@ __device__ inline void join_parts(const Args& a, const Piece& p, int first_slot,
     }
 }
 
-// A workgroup has posted its part of a unit (all its threads call this); the last of
-// the unit's joins them, in their order.
-template <typename Fmt, int THREADS, int ROWS, int DT, typename Division>
-__device__ inline void join(const Args& a, const Piece& p, const Division& share, int64_t pos, int D) {
-    __shared__ uint32_t s_arrived;
+// A workgroup has posted its part of a unit (all its threads call this).  Where the unit's
+// parts are many and large, its workgroups wait for each other and join some rows each: a
+// workgroup alone reads 50 GB/s.  The wait is bounded, and nothing depends on who waits: rows
+// are taken from a counter, and the last to arrive does not wait and takes what is left.
+constexpr int kJoinBytes = 128 << 10;  // of a unit's parts: fewer are joined by the last alone
+constexpr int kJoinPolls = 64;
+
+template <typename Fmt, int THREADS, int ROWS, int DT>
+__device__ inline void join_rows(const Args& a, const Piece& p, int r0, int r1, int D) {
+    // A read takes about 2 us, so as many as registers allow are in flight.
+    if (p.count <= 2) join_parts<Fmt, THREADS, ROWS, DT, 8, 2>(a, p, r0, r1, D);
+    else if (p.count <= 4) join_parts<Fmt, THREADS, ROWS, DT, 4, 4>(a, p, r0, r1, D);
+    else if ((r1 - r0) * (DT / 4) > THREADS) join_parts<Fmt, THREADS, ROWS, DT, 2, 8>(a, p, r0, r1, D);
+    else join_parts<Fmt, THREADS, ROWS, DT, 1, 16>(a, p, r0, r1, D);
+}
+
+template <typename Fmt, int THREADS, int ROWS, int DT>
+__device__ inline void join(const Args& a, const Piece& p, bool together, int D) {
+    __shared__ uint32_t s_word;
     const int tid = int(threadIdx.x);
-    const int64_t u0 = pos - p.t0;
-    const int w0 = share.owner(u0), w1 = share.owner(u0 + p.tiles - 1);
+    uint32_t* arrivals = a.counters + 3 * p.w0;
+    uint32_t* taken = arrivals + 1;
+    uint32_t* gone = arrivals + 2;
+    together = together && int64_t(p.count) * p.rows * DT * 4 > kJoinBytes;
     wait_memory();
     __syncthreads();
-    if (tid == 0) s_arrived = arrive(&a.counters[w0]);
+    if (tid == 0) {
+        bool all = arrive(arrivals) == uint32_t(p.count - 1);
+        for (int i = 0; together && !all && i < kJoinPolls; ++i) {
+            __builtin_amdgcn_s_sleep(8);
+            all = load_relaxed(arrivals) == uint32_t(p.count);
+        }
+        s_word = all;
+    }
     __syncthreads();
-    if (s_arrived != uint32_t(w1 - w0)) return;
-    const int count = w1 - w0 + 1;
-    const int first_slot = 2 * w0 + (share.begin(w0) == u0 ? 0 : 1);
-    // A read takes about 2 us, so as many as registers allow are in flight.
-    if (count <= 2) join_parts<Fmt, THREADS, ROWS, DT, 8, 2>(a, p, first_slot, w0, count, D);
-    else if (count <= 4) join_parts<Fmt, THREADS, ROWS, DT, 4, 4>(a, p, first_slot, w0, count, D);
-    else if (p.rows * (DT / 4) > THREADS) join_parts<Fmt, THREADS, ROWS, DT, 2, 8>(a, p, first_slot, w0, count, D);
-    else join_parts<Fmt, THREADS, ROWS, DT, 1, 16>(a, p, first_slot, w0, count, D);
-    if (tid == 0) __hip_atomic_store(&a.counters[w0], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const bool all = s_word != 0;
+    if (!together) {
+        if (!all) return;
+        join_rows<Fmt, THREADS, ROWS, DT>(a, p, 0, p.rows, D);
+        if (tid == 0) __hip_atomic_store(arrivals, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        return;
+    }
+    const int some = (p.rows + p.count - 1) / p.count;
+    while (all) {
+        __syncthreads();
+        if (tid == 0) s_word = arrive(taken);
+        __syncthreads();
+        const int r0 = int(s_word) * some;
+        if (r0 >= p.rows) break;
+        join_rows<Fmt, THREADS, ROWS, DT>(a, p, r0, r0 + some < p.rows ? r0 + some : p.rows, D);
+    }
+    // The last to leave clears the counters.
+    if (tid == 0 && arrive(gone) == uint32_t(p.count - 1)) {
+        __hip_atomic_store(arrivals, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(taken, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(gone, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
 }
 
 // Rows of one workgroup, of the kernel that serves `rows` rows of a kv head.

@@ -67,8 +67,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
     const uint32_t ring = uint32_t(uintptr_t((__attribute__((address_space(3))) char*)s_ring));
 
     Division<kThreads, STAGE> share;
-    share.init(a, s_tiles, 1);
-    const int64_t w = int64_t(blockIdx.x), first = share.begin(w), end = share.begin(w + 1);
+    share.init(a, s_tiles);
+    const int64_t w = int64_t(blockIdx.x), first = share.begin(w), end = share.end(a, w);
 
     // A row's chunks lie permuted (chunk ^ key, of period 16; rows of 128 bytes lie two to
     // 64 banks), so that 16 lanes that read one chunk of 16 keys meet 16 different
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
     const bool even_pages = L.pages.page_size % 8 == 0;  // a load's keys (8 at most) lie on one page
 
     for (int64_t pos = first; pos < end;) {
-        const Piece p = share.template find<ROWS>(a, pos, end);
+        const Piece p = share.template find<ROWS>(a, w, pos, first, end);
         const int len = p.seq.len, T = p.T;
         bool bad = p.seq.state == 2;
         const int64_t head = int64_t(p.h) * L.pages.head_bytes;
@@ -294,8 +294,6 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
         int flags = 0;
 #pragma unroll
         for (int i = 0; i < kWaves; ++i) flags |= s_flags[i];
-        const bool whole = p.whole();
-        const int64_t slot = 2 * w + (pos == first ? 0 : 1);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             float all = kNegInf;
@@ -320,13 +318,13 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                     }
                 }
                 if (flags & 1) total = __builtin_nanf("");
-                if (whole) write_row<Fmt>(a, p, row, d, D, o, total);
-                else post_part<ROWS, DT>(a, slot, row, d, o, most, total);
+                if (p.whole) write_row<Fmt>(a, p, row, d, D, o, total);
+                else post_part<ROWS, DT>(a, p.slot, row, d, o, most, total);
             }
             __syncthreads();
         }
-        if (!whole) join<Fmt, kThreads, ROWS, DT>(a, p, share, pos, D);
-        pos += p.t1 - p.t0;
+        if (!p.whole) join<Fmt, kThreads, ROWS, DT>(a, p, share.apart, D);
+        pos += share.step(p);
         __syncthreads();  // the ring and the pages are free
     }
 }
