@@ -16,7 +16,7 @@ LIB = os.path.join(HERE, "libosd.so")
 PROBE_LIB = os.path.join(HERE, "libosd_probe.so")
 SOURCES = ["osd_api.hip", "verify.hip", "distill.hip", "verify_greedy.hip", "distill_stream.hip", "verify_distill.hip",
            "sample.hip", "verify_shard.hip", "verify_tree.hip", "topk.hip", "distill_topk.hip", "verify_topk.hip",
-           "cache.hip", "tree_attention.hip", "tree_attention_wide.hip"]
+           "cache.hip", "tree_attention.hip", "tree_attention_wide_bf16.hip", "tree_attention_wide_f32.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -298,7 +298,7 @@ hipError_t launch_tree_attention(const TreeAttentionLaunch& L) {
     a.parts = reinterpret_cast<float*>(L.workspace + w.parts);
     a.stats_bytes = uint32_t(w.parts - w.stats);
     a.parts_bytes = uint32_t(w.total - w.parts);
-    if (R > 16) return launch_wide(a, R);
+    if (R > 16) return L.dtype == OSD_BF16 ? launch_wide_bf16(a, R) : launch_wide_f32(a, R);
     return L.dtype == OSD_BF16 ? launch_ops<Bf16Ops>(a) : launch_ops<F32Ops>(a);
 }
 

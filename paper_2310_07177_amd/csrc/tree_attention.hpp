@@ -234,14 +234,14 @@ struct Division {
     bool apart;
 
     __device__ static int tiles_of(const Seq& s) { return s.state ? 1 : (s.len + s.n - 1) / TILE + 1; }
-    // Sums over the lanes up to each.
+    // Sums over the lanes up to each: within rows of 16, then across them.
     __device__ static int scan(int x) {
-        const int lane = int(threadIdx.x) & (kWave - 1);
-#pragma unroll
-        for (int o = 1; o < kWave; o *= 2) {
-            const int up = __shfl_up(x, o);
-            x += lane >= o ? up : 0;
-        }
+        x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);   // row_shr:1
+        x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);   // row_shr:2
+        x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);   // row_shr:4
+        x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);   // row_shr:8
+        x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // row_bcast:15 into rows 1 and 3
+        x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);  // row_bcast:31 into rows 2 and 3
         return x;
     }
 
@@ -399,7 +399,7 @@ constexpr int kPiece = DT * Ops::Fmt::kBytes >= 256 ? 16 / Ops::Fmt::kBytes : DT
 // a row's values in acc[..][n][t].
 template <typename Ops, int DT, int MT, int VW_>
 struct Rows {
-    static constexpr int ES = Ops::Fmt::kBytes, KT = Ops::kKT, KEYS = 4 * KT, CHUNKS = DT / Ops::kChunk;
+    static constexpr int ES = Ops::Fmt::kBytes, KT = Ops::kKT, KEYS = 4 * KT, CHUNKS = (DT + Ops::kChunk - 1) / Ops::kChunk;
     static constexpr int VW = VW_, BW = 16 * VW, BLOCKS = DT / BW;
     f32x4_t acc[MT][BLOCKS][VW];
     float ref[MT], sum[MT];  // every exponent's reference, and the lane's sum
@@ -691,7 +691,9 @@ __device__ inline void join(const Args& a, const Piece& p, bool together, int D)
 // Rows of one workgroup, of the kernel that serves `rows` rows of a kv head.
 inline int padded_dim(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
-hipError_t launch_wide(const Args& a, int rows);  // tree_attention_wide.hip
+// tree_attention_wide.hpp
+hipError_t launch_wide_bf16(const Args& a, int rows);
+hipError_t launch_wide_f32(const Args& a, int rows);
 
 }  // namespace attention
 }  // namespace osd

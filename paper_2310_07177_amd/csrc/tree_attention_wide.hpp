@@ -1,5 +1,8 @@
-// tree_attention_wide.hip -- osd_tree_attention of many rows: eight waves read keys
-// and values from LDS, where they arrive directly from memory.
+// tree_attention_wide.hpp -- osd_tree_attention of many rows: eight waves read keys
+// and values from LDS, where they arrive directly from memory.  (Compiled once for each
+// type.)
+#pragma once
+
 #include "tree_attention.hpp"
 
 namespace osd {
@@ -45,11 +48,13 @@ struct Shape {
     static constexpr int CPR = ROW / 16;                      // 16-byte chunks of a row
 };
 
-template <typename Ops, int DT, int WR, int MT, bool FULL>
+// DT: head_dim rounded up to a power of two, as rows lie in LDS; NC: tiles of 16 of its
+// values that are computed; FULL: all DT of them.
+template <typename Ops, int DT, int WR, int MT, int NC, bool FULL>
 __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
     using Fmt = typename Ops::Fmt;
     using S = Shape<Ops, DT, WR, MT>;
-    using R = Rows<Ops, DT, MT, 1>;
+    using R = Rows<Ops, NC * 16, MT, 1>;
     constexpr int ES = S::ES, CHUNKS = R::CHUNKS, KT = R::KT, STEP = S::STEP, STAGE = S::STAGE, ROWS = S::ROWS;
     constexpr int PITCH = S::PITCH, CPR = S::CPR, ROW = S::ROW;
     const TreeAttentionLaunch& L = a.L;
@@ -81,7 +86,6 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
         const int at = (wave * S::LOADS + x) * kWave + lane, key = at / CPR;
         lane_key[x] = lane / CPR;
         lane_chunk[x] = (at % CPR) ^ swizzle(key);
-        if (!FULL && lane_chunk[x] * 16 >= D * ES) lane_chunk[x] = 0;
     }
     const bool even_pages = L.pages.page_size % 8 == 0;  // a load's keys (8 at most) lie on one page
 
@@ -135,8 +139,10 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                            int64_t(j - in * L.pages.page_size) * (D * ES) + lane_chunk[x] * 16;
                 }
                 const uint32_t unit = to + uint32_t(wave * S::LOADS + x) * 1024u;
-                load_lds(L.k_cache + from, unit);
-                load_lds(L.v_cache + from, unit + S::TILE_BYTES);
+                if (FULL || lane_chunk[x] * 16 < D * ES) {  // (what lies behind a row in LDS is not used)
+                    load_lds(L.k_cache + from, unit);
+                    load_lds(L.v_cache + from, unit + S::TILE_BYTES);
+                }
             }
         };
         for (int st = 0; st < S::NST - 1 && st < stages; ++st) issue(st);
@@ -190,7 +196,6 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                 for (int mt = 0; mt < MT; ++mt) s[mt][kt] = f32x4_t{0, 0, 0, 0};
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c) {
-                    if (!FULL && c * Ops::kChunk >= D) continue;
                     chunk_t k = *reinterpret_cast<const chunk_t*>(k_row + kt * 16 * ROW + (k_lane ^ c * 64));
                     if (!FULL && c * Ops::kChunk + grp * (16 / ES) >= D) k = chunk_t{0, 0, 0, 0};
 #pragma unroll
@@ -218,8 +223,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                 }
             }
 #pragma unroll
-            for (int t = 0; t < DT / 16; ++t) {
-                if (!FULL && t * 16 >= D) continue;
+            for (int t = 0; t < NC; ++t) {
                 chunk_t v;
                 if constexpr (ES == 2) {
 #pragma unroll
@@ -337,8 +341,14 @@ hipError_t launch_shape(Args& a) {
     const int grid = L.cus < kMaxGroups / 2 ? L.cus : kMaxGroups / 2;
     const size_t lds = size_t(L.B + 1) * sizeof(int);
     if (L.head_dim == DT)
-        return launch_kernel(&tree_attention_wide<Ops, DT, WR, MT, true>, dim3(grid), dim3(kThreads), lds, L.stream, a);
-    return launch_kernel(&tree_attention_wide<Ops, DT, WR, MT, false>, dim3(grid), dim3(kThreads), lds, L.stream, a);
+        return launch_kernel(&tree_attention_wide<Ops, DT, WR, MT, DT / 16, true>, dim3(grid), dim3(kThreads), lds, L.stream, a);
+    if constexpr (DT == 128) {  // heads of 80 and 96 without the products of what they lack
+        if (L.head_dim <= 80)
+            return launch_kernel(&tree_attention_wide<Ops, DT, WR, MT, 5, false>, dim3(grid), dim3(kThreads), lds, L.stream, a);
+        if (L.head_dim <= 96)
+            return launch_kernel(&tree_attention_wide<Ops, DT, WR, MT, 6, false>, dim3(grid), dim3(kThreads), lds, L.stream, a);
+    }
+    return launch_kernel(&tree_attention_wide<Ops, DT, WR, MT, DT / 16, false>, dim3(grid), dim3(kThreads), lds, L.stream, a);
 }
 
 // (A wave's sums of 32 rows of DT = 256, or of fp32, would fill its registers.)
@@ -361,11 +371,5 @@ hipError_t launch_ops(Args& a, int rows) {
 }
 
 }  // namespace
-
-hipError_t launch_wide(const Args& args, int rows) {
-    Args a = args;
-    return a.L.dtype == OSD_BF16 ? launch_ops<Bf16Ops>(a, rows) : launch_ops<F32Ops>(a, rows);
-}
-
 }  // namespace attention
 }  // namespace osd

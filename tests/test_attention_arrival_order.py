@@ -8,7 +8,8 @@ from paper_2310_07177_amd import build
 from tests.test_arrival_order import ARRIVAL, WAIT_ALL, WRITE, assembly
 
 
-@pytest.mark.parametrize("src,least", [("tree_attention.hip", 20), ("tree_attention_wide.hip", 16)])
+@pytest.mark.parametrize("src,least", [("tree_attention.hip", 12), ("tree_attention_wide_bf16.hip", 24),
+                                       ("tree_attention_wide_f32.hip", 16)])
 def test_parts_before_arrival(src, least, tmp_path):
     if not os.path.exists(build.HIPCC):
         pytest.skip("needs hipcc")
