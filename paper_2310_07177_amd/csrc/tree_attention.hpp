@@ -92,7 +92,8 @@ struct Bf16Ops {
     __device__ static f32x4_t pv(const Value<VW> (&v)[8], int t, const Probs& p, f32x4_t o) {
         return qk(column(v, t), p.x, o);
     }
-    __device__ static f32x4_t pv(const chunk_t& v, const Probs& p, f32x4_t o) { return qk(v, p.x, o); }
+    static constexpr int kParts = 1;  // instructions of a product
+    __device__ static f32x4_t pv_part(const chunk_t& v, const Probs& p, int, f32x4_t o) { return qk(v, p.x, o); }
     // Of an operand of the second product: what is not finite to 0, whether there is any.
     __device__ static bool clean(chunk_t& v) {
         bool odd = false;
@@ -144,11 +145,10 @@ struct F32Ops {
         for (int i = 0; i < 4; ++i) o = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i].x[t], p.x[i], o, 0, 0, 0);
         return o;
     }
+    static constexpr int kParts = 4;
     // (Element i of an operand: the lane's key i of 4.)
-    __device__ static f32x4_t pv(const chunk_t& v, const Probs& p, f32x4_t o) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[i]), p.x[i], o, 0, 0, 0);
-        return o;
+    __device__ static f32x4_t pv_part(const chunk_t& v, const Probs& p, int i, f32x4_t o) {
+        return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[i]), p.x[i], o, 0, 0, 0);
     }
     __device__ static bool clean(chunk_t& v) {
         bool odd = false;

@@ -189,19 +189,59 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                 v_lane = ((col >> 2) ^ swizzle(grp * 4)) * 16;
             }
             asm volatile("" : "+v"(k_lane), "+v"(v_lane));
-            f32x4_t s[MT][KT];
+            // All of K's operands are read before the first product, V's a batch ahead of theirs and the first
+            // before the exponentials.  (The compiler would read each where it is used, and every
+            // one of the 24 reads of a step would wait for LDS: 6600 cycles a stage of 256 rows.)
+            chunk_t k[CHUNKS][KT];
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
+            for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) s[mt][kt] = f32x4_t{0, 0, 0, 0};
+                for (int kt = 0; kt < KT; ++kt)
+                    k[c][kt] = *reinterpret_cast<const chunk_t*>(k_row + kt * 16 * ROW + (k_lane ^ c * 64));
+            __builtin_amdgcn_sched_barrier(0);
+            f32x4_t s[MT][KT], odd_chunks[MT][KT];  // (fp32: two sums in turn)
 #pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) {
-                    chunk_t k = *reinterpret_cast<const chunk_t*>(k_row + kt * 16 * ROW + (k_lane ^ c * 64));
-                    if (!FULL && c * Ops::kChunk + grp * (16 / ES) >= D) k = chunk_t{0, 0, 0, 0};
+            for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) s[mt][kt] = Ops::qk(k, q[mt][c], s[mt][kt]);
+                for (int kt = 0; kt < KT; ++kt) s[mt][kt] = odd_chunks[mt][kt] = f32x4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) {
+                    if (!FULL && c * Ops::kChunk + grp * (16 / ES) >= D) k[c][kt] = chunk_t{0, 0, 0, 0};
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        f32x4_t& sum = ES == 4 && (c & 1) ? odd_chunks[mt][kt] : s[mt][kt];
+                        sum = Ops::qk(k[c][kt], q[mt][c], sum);
+                    }
                 }
+            if constexpr (ES == 4) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) s[mt][0] += odd_chunks[mt][0];
             }
+            constexpr int BATCH = 4, BATCHES = (NC + BATCH - 1) / BATCH;  // tiles of V
+            chunk_t v[2][BATCH];
+            auto read_v = [&](int batch) {
+#pragma unroll
+                for (int u = 0; u < BATCH; ++u) {
+                    const int t = batch * BATCH + u;
+                    if (t >= NC) continue;
+                    if constexpr (ES == 2) {
+#pragma unroll
+                        for (int kt = 0; kt < KT; ++kt) {
+                            const u32x2_t half_of = transposed(v_row + kt * 16 * ROW + (v_lane ^ t * 32));
+                            v[batch & 1][u][2 * kt] = half_of.x;
+                            v[batch & 1][u][2 * kt + 1] = half_of.y;
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            v[batch & 1][u][i] = *reinterpret_cast<const uint32_t*>(v_row + i * ROW + (v_lane ^ (i * 16) ^ t * 64));
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            read_v(0);
             if constexpr (TAIL) rows.mask(s, j0, p.seq);
             if (fresh) {
                 fresh = false;
@@ -223,26 +263,27 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                 }
             }
 #pragma unroll
-            for (int t = 0; t < NC; ++t) {
-                chunk_t v;
-                if constexpr (ES == 2) {
-#pragma unroll
-                    for (int kt = 0; kt < KT; ++kt) {
-                        const u32x2_t half_of = transposed(v_row + kt * 16 * ROW + (v_lane ^ t * 32));
-                        v[2 * kt] = half_of.x;
-                        v[2 * kt + 1] = half_of.y;
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint32_t*>(v_row + i * ROW + (v_lane ^ (i * 16) ^ t * 64));
-                }
+            for (int batch = 0; batch < BATCHES; ++batch) {
+                if (batch + 1 < BATCHES) read_v(batch + 1);
                 if constexpr (TAIL) {
-                    v &= in;
-                    const bool odd = Ops::clean(v);
-                    rows.odd = rows.odd || __any(odd);
-                }
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) rows.acc[mt][t][0] = Ops::pv(v, pr[mt], rows.acc[mt][t][0]);
+                    for (int u = 0; u < BATCH; ++u) {
+                        if (batch * BATCH + u >= NC) continue;
+                        v[batch & 1][u] &= in;
+                        const bool odd = Ops::clean(v[batch & 1][u]);
+                        rows.odd = rows.odd || __any(odd);
+                    }
+                }
+                // (Products of several tiles in turn: each of fp32 would wait for the one before it.)
+#pragma unroll
+                for (int i = 0; i < Ops::kParts; ++i)
+#pragma unroll
+                    for (int u = 0; u < BATCH; ++u) {
+                        const int t = batch * BATCH + u;
+                        if (t >= NC) continue;
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) rows.acc[mt][t][0] = Ops::pv_part(v[batch & 1][u], pr[mt], i, rows.acc[mt][t][0]);
+                    }
             }
         };
         rows.clear();
@@ -261,7 +302,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                 if (S::NST > 2 && st + 2 < stages) wait_stage<(S::NST > 2 ? 4 * S::LOADS : 0)>();
                 else if (S::NST > 2 && st + 1 < stages) wait_stage<(S::NST > 2 ? 2 * S::LOADS : 0)>();
                 else wait_stage<0>();
-                if (st + S::NST - 1 < stages) issue(st + S::NST - 1);
+                if (S::NST == 2 && st + 1 < stages) issue(st + 1);
 #pragma unroll
                 for (int sub = 0; sub < STAGE / STEP / S::WK; ++sub) {
                     const int k0 = (sub * key_waves + wk) * STEP, j0 = (p.t0 + st) * STAGE + k0;
@@ -269,6 +310,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                     if (j0 + STEP <= len) take(st, k0, no_t{});
                     else take(st, k0, yes_t{});
                 }
+                // (Sent for here, where the waves have drifted apart, rather than by all at once above.)
+                if (S::NST > 2 && st + S::NST - 1 < stages) issue(st + S::NST - 1);
             }
             // All waves share the stages, so that one that needs them again has all go through them.
             const bool ok = again || fresh || rows.served(a.c2);
