@@ -121,27 +121,37 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
         auto issue = [&](int st) {
             look(st);
             const uint32_t to = ring + uint32_t(st % S::NST) * (2 * S::TILE_BYTES);
+            constexpr int KEYS_OF = 1024 / ROW > 0 ? 1024 / ROW : 1;  // keys of a load
+            int64_t from[S::LOADS];
+            if (even_pages) {
+                int page[S::LOADS], slot[S::LOADS];
 #pragma unroll
-            for (int x = 0; x < S::LOADS; ++x) {
-                constexpr int KEYS_OF = 1024 / ROW > 0 ? 1024 / ROW : 1;
-                const int key0 = (p.t0 + st) * STAGE + (wave * S::LOADS + x) * KEYS_OF;
-                int64_t from;
-                if (even_pages) {
-                    const int last = (T - 1) / KEYS_OF * KEYS_OF, j = key0 < last ? key0 : last, in = page_of(j);
-                    const int page = __builtin_amdgcn_readfirstlane(s_page[in - page0]);
-                    from = int64_t(page) * L.pages.page_bytes + head + int64_t(j - in * L.pages.page_size) * (D * ES) +
-                           (lane_key[x] * (D * ES) + lane_chunk[x] * 16);
-                } else {
-                    int j = key0 + lane_key[x];
+                for (int x = 0; x < S::LOADS; ++x) {
+                    const int key = (p.t0 + st) * STAGE + (wave * S::LOADS + x) * KEYS_OF, last = (T - 1) / KEYS_OF * KEYS_OF;
+                    const int j = key < last ? key : last, in = page_of(j);
+                    page[x] = s_page[in - page0];
+                    slot[x] = j - in * L.pages.page_size;
+                }
+#pragma unroll
+                for (int x = 0; x < S::LOADS; ++x)
+                    from[x] = int64_t(__builtin_amdgcn_readfirstlane(page[x])) * L.pages.page_bytes + head +
+                              int64_t(slot[x]) * (D * ES) + (lane_key[x] * (D * ES) + lane_chunk[x] * 16);
+            } else {
+#pragma unroll
+                for (int x = 0; x < S::LOADS; ++x) {
+                    int j = (p.t0 + st) * STAGE + (wave * S::LOADS + x) * KEYS_OF + lane_key[x];
                     j = j < T ? j : T - 1;
                     const int in = page_of(j);
-                    from = int64_t(s_page[in - page0]) * L.pages.page_bytes + head +
-                           int64_t(j - in * L.pages.page_size) * (D * ES) + lane_chunk[x] * 16;
+                    from[x] = int64_t(s_page[in - page0]) * L.pages.page_bytes + head +
+                              int64_t(j - in * L.pages.page_size) * (D * ES) + lane_chunk[x] * 16;
                 }
+            }
+#pragma unroll
+            for (int x = 0; x < S::LOADS; ++x) {
                 const uint32_t unit = to + uint32_t(wave * S::LOADS + x) * 1024u;
                 if (FULL || lane_chunk[x] * 16 < D * ES) {  // (what lies behind a row in LDS is not used)
-                    load_lds(L.k_cache + from, unit);
-                    load_lds(L.v_cache + from, unit + S::TILE_BYTES);
+                    load_lds(L.k_cache + from[x], unit);
+                    load_lds(L.v_cache + from[x], unit + S::TILE_BYTES);
                 }
             }
         };
@@ -150,7 +160,9 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
         // Half of the rows in use (a batch's smaller trees): the waves without rows take half of the keys.
         constexpr bool HALVES = WR == kWaves && STAGE / STEP % 2 == 0;
         const int half = HALVES && p.live * 2 <= ROWS ? 1 : 0;
-        const int row_waves = WR >> half, wr = wave & (row_waves - 1), wk = wave / row_waves, key_waves = kWaves / row_waves;
+        const int row_waves = WR >> half, key_waves = S::WK << half;
+        // (Waves that share rows are neighbours, so that few rows, too, are spread over all SIMDs.)
+        const int wr = wave / key_waves, wk = wave & (key_waves - 1);
         const bool alive = wr * MT * 16 < p.live;  // (of padding alone: a wave helps to fill the ring)
         chunk_t q[MT][CHUNKS];
         R rows;
@@ -170,25 +182,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
             }
         }
 
-        bool fresh = true;  // no reference yet
-        auto take = [&](int st, int k0, auto tail) {
-            constexpr bool TAIL = decltype(tail)::value;
-            const int j0 = (p.t0 + st) * STAGE + k0;
-            const char* k_row = s_ring + (st % S::NST) * (2 * S::TILE_BYTES) + (k0 + col) * ROW;
-            // (A chunk's place is a XOR of the lane's part and a constant; computed each time, as all of
-            // them together would hold 30 registers.)
-            int k_lane = (grp ^ swizzle(col)) * 16;
-            const char* v_row;
-            int v_lane;
-            if constexpr (ES == 2) {  // the key whose piece of V this lane reads for the others
-                const int from = grp * 4 + (col >> 2);
-                v_row = k_row + S::TILE_BYTES + (from - col) * ROW + (col & 1) * 8;
-                v_lane = (((col & 3) >> 1) ^ swizzle(from)) * 16;
-            } else {
-                v_row = k_row + S::TILE_BYTES + (grp * 4 - col) * ROW + (col & 3) * 4;
-                v_lane = ((col >> 2) ^ swizzle(grp * 4)) * 16;
-            }
-            asm volatile("" : "+v"(k_lane), "+v"(v_lane));
+        auto scores = [&](const char* k_row, int k_lane, f32x4_t (&s)[MT][KT]) {
             // All of K's operands are read before the first product, V's a batch ahead of theirs and the first
             // before the exponentials.  (The compiler would read each where it is used, and every
             // one of the 24 reads of a step would wait for LDS: 6600 cycles a stage of 256 rows.)
@@ -199,7 +193,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                 for (int kt = 0; kt < KT; ++kt)
                     k[c][kt] = *reinterpret_cast<const chunk_t*>(k_row + kt * 16 * ROW + (k_lane ^ c * 64));
             __builtin_amdgcn_sched_barrier(0);
-            f32x4_t s[MT][KT], odd_chunks[MT][KT];  // (fp32: two sums in turn)
+            f32x4_t odd_chunks[MT][KT];  // (fp32: two sums in turn)
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -219,6 +213,27 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) s[mt][0] += odd_chunks[mt][0];
             }
+        };
+        auto take = [&](int st, int k0, auto tail) {
+            constexpr bool TAIL = decltype(tail)::value;
+            const int j0 = (p.t0 + st) * STAGE + k0;
+            const char* k_row = s_ring + (st % S::NST) * (2 * S::TILE_BYTES) + (k0 + col) * ROW;
+            // (A chunk's place is a XOR of the lane's part and a constant; computed each time, as all of
+            // them together would hold 30 registers.)
+            int k_lane = (grp ^ swizzle(col)) * 16;
+            const char* v_row;
+            int v_lane;
+            if constexpr (ES == 2) {  // the key whose piece of V this lane reads for the others
+                const int from = grp * 4 + (col >> 2);
+                v_row = k_row + S::TILE_BYTES + (from - col) * ROW + (col & 1) * 8;
+                v_lane = (((col & 3) >> 1) ^ swizzle(from)) * 16;
+            } else {
+                v_row = k_row + S::TILE_BYTES + (grp * 4 - col) * ROW + (col & 3) * 4;
+                v_lane = ((col >> 2) ^ swizzle(grp * 4)) * 16;
+            }
+            asm volatile("" : "+v"(k_lane), "+v"(v_lane));
+            f32x4_t s[MT][KT];
+            scores(k_row, k_lane, s);
             constexpr int BATCH = 4, BATCHES = (NC + BATCH - 1) / BATCH;  // tiles of V
             chunk_t v[2][BATCH];
             auto read_v = [&](int batch) {
@@ -243,14 +258,6 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
             };
             read_v(0);
             if constexpr (TAIL) rows.mask(s, j0, p.seq);
-            if (fresh) {
-                fresh = false;
-                float most[MT];
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) most[mt] = kNegInf;
-                R::largest(s, most);
-                rows.refer(most, a.c2);
-            }
             typename Ops::Probs pr[MT];
             rows.template soften<TAIL>(s, a.c2, pr);
             // The lane's keys that are keys.
@@ -297,24 +304,48 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                 page_end = 0;
                 for (int st = 0; st < S::NST - 1 && st < stages; ++st) issue(st);
             }
-            for (int st = 0; st < stages; ++st) {
+            auto arrive_at = [&](int st) {
                 // This stage is there; the ones behind it may be on their way.
                 if (S::NST > 2 && st + 2 < stages) wait_stage<(S::NST > 2 ? 4 * S::LOADS : 0)>();
                 else if (S::NST > 2 && st + 1 < stages) wait_stage<(S::NST > 2 ? 2 * S::LOADS : 0)>();
                 else wait_stage<0>();
+            };
+            auto stage = [&](int st, auto tail) {
+                arrive_at(st);
                 if (S::NST == 2 && st + 1 < stages) issue(st + 1);
+                if (alive) {
 #pragma unroll
-                for (int sub = 0; sub < STAGE / STEP / S::WK; ++sub) {
-                    const int k0 = (sub * key_waves + wk) * STEP, j0 = (p.t0 + st) * STAGE + k0;
-                    if (j0 >= T || !alive || k0 >= STAGE) continue;
-                    if (j0 + STEP <= len) take(st, k0, no_t{});
-                    else take(st, k0, yes_t{});
+                    for (int sub = 0; sub < STAGE / STEP / S::WK; ++sub) {
+                        const int k0 = (sub * key_waves + wk) * STEP;
+                        if (HALVES && k0 >= STAGE) continue;
+                        if (!decltype(tail)::value || (p.t0 + st) * STAGE + k0 < T) take(st, k0, tail);
+                    }
                 }
                 // (Sent for here, where the waves have drifted apart, rather than by all at once above.)
                 if (S::NST > 2 && st + S::NST - 1 < stages) issue(st + S::NST - 1);
+            };
+            if (!again) {  // the reference: the wave's first step
+                float most[MT];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) most[mt] = kNegInf;
+                if (stages > 0) {
+                    arrive_at(0);
+                    if (alive) {
+                        f32x4_t s[MT][KT];
+                        scores(s_ring + (wk * STEP + col) * ROW, (grp ^ swizzle(col)) * 16, s);
+                        if (p.t0 * STAGE + wk * STEP + STEP > len) rows.mask(s, p.t0 * STAGE + wk * STEP, p.seq);
+                        R::largest(s, most);
+                    }
+                }
+                rows.refer(most, a.c2);
             }
+            // Stages of the context alone, then those with keys that not every row sees.  (Two loops: where the
+            // two kinds of step met, all sums went through a copy.)
+            int st = 0;
+            for (const int plain = len / STAGE - p.t0 < stages ? len / STAGE - p.t0 : stages; st < plain; ++st) stage(st, no_t{});
+            for (; st < stages; ++st) stage(st, yes_t{});
             // All waves share the stages, so that one that needs them again has all go through them.
-            const bool ok = again || fresh || rows.served(a.c2);
+            const bool ok = again || rows.served(a.c2);
             if (lane == 0) s_flags[wave] = ok;
             __syncthreads();
             int all = 1;
@@ -327,7 +358,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             const float sum = rows_sum(rows.sum[mt]);
-            if (sum == 0.0f || fresh) rows.ref[mt] = kNegInf;
+            if (sum == 0.0f) rows.ref[mt] = kNegInf;
             if (grp == 0) {
                 s_stat[wave][mt * 16 + col][0] = rows.ref[mt];
                 s_stat[wave][mt * 16 + col][1] = sum;
@@ -344,7 +375,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             float all = kNegInf;
-            for (int i = 0; i < key_waves; ++i) all = fmaxf(all, s_stat[i * row_waves + wr][mt * 16 + col][0]);
+            for (int i = 0; i < key_waves; ++i) all = fmaxf(all, s_stat[wr * key_waves + i][mt * 16 + col][0]);
             rows.template store<PITCH>(mt, rescale(rows.ref[mt], all), s_acc[wave][col]);
             __syncthreads();
             // (With half of the rows in use the other half is padding: zeros.)
@@ -355,13 +386,13 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                 float most = kNegInf, total = 0.0f;
                 if (x < row_waves) {
                     for (int y = 0; y < key_waves; ++y) {
-                        o += *reinterpret_cast<const f32x4_t*>(&s_acc[y * row_waves + x][r][d]);
-                        most = fmaxf(most, s_stat[y * row_waves + x][mt * 16 + r][0]);
+                        o += *reinterpret_cast<const f32x4_t*>(&s_acc[x * key_waves + y][r][d]);
+                        most = fmaxf(most, s_stat[x * key_waves + y][mt * 16 + r][0]);
                     }
                     if ((flags & 2) && row < p.live) add_odd<Fmt>(L, p.b, p.h, d, len, T, len / STEP * STEP, s_sees[row], o);
                     for (int y = 0; y < key_waves; ++y) {
-                        const float s = s_stat[y * row_waves + x][mt * 16 + r][1];
-                        total += s == s ? s * rescale(s_stat[y * row_waves + x][mt * 16 + r][0], most) : s;
+                        const float s = s_stat[x * key_waves + y][mt * 16 + r][1];
+                        total += s == s ? s * rescale(s_stat[x * key_waves + y][mt * 16 + r][0], most) : s;
                     }
                 }
                 if (flags & 1) total = __builtin_nanf("");
