@@ -294,6 +294,8 @@ struct Division {
                 if (__builtin_amdgcn_readlane(to, kWave - 1) * units > W) continue;
                 apart = true;
                 upto = to;
+                each = e;
+                break;
             }
         }
     }
@@ -343,17 +345,22 @@ __device__ inline Piece Division<THREADS, TILE>::find(const Args& a, int64_t w, 
         p.tiles = upto_b - before;
         p.seq = sequence(L, p.b);
     }
-    const int64_t in_b = pos - before * units;
-    const int length = upto_b - before, unit = int(quotient(in_b, length)), at = int(in_b - int64_t(unit) * length);
-    if (apart) {  // part `at` of `length`
-        p.t0 = int(quotient(int64_t(at) * p.tiles, length));
-        p.t1 = int(quotient(int64_t(at + 1) * p.tiles, length));
+    int unit;
+    if (apart) {  // (at most kMaxGroups parts: 32 bits)
+        const int length = upto_b - before, in_b = int(pos) - before * int(units);
+        unit = int(uint32_t(in_b) / uint32_t(length));
+        const int at = in_b - unit * length, e = int(each);
+        p.t0 = at * e;
+        p.t1 = p.t0 + e < p.tiles ? p.t0 + e : p.tiles;
         p.whole = length == 1;
         p.w0 = int(w) - at;
         p.count = length;
         p.first_slot = 2 * p.w0;
         p.slot = 2 * int(w);
     } else {
+        const int64_t in_b = pos - before * units;
+        unit = int(quotient(in_b, p.tiles));
+        const int at = int(in_b - int64_t(unit) * p.tiles);
         p.t0 = at;
         p.t1 = int(end - pos < p.tiles - at ? at + (end - pos) : p.tiles);
         p.whole = p.t0 == 0 && p.t1 == p.tiles;

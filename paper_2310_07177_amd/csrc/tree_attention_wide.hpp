@@ -17,7 +17,7 @@ constexpr int kPageWindow = 512;  // pages looked up at once
 // the way.  Counted in vmcnt; the compiler does not know of it, so that reads of LDS
 // wait for it only where wait_stage() says so.
 __device__ inline void load_lds(const char* from, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(from), "s"(to) : "memory");
 }
 // All but the wave's LEFT newest loads are there, then those of all waves.
 template <int LEFT>
