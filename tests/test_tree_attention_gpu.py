@@ -76,6 +76,48 @@ def test_scales(osd, dtype, scale, std):
     parity(osd, np.random.default_rng(3), [500, 64], 9, 4, 1, 64, 16, dtype, True, scale=scale, std=std)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,Hq,H,D", [(1, 4, 1, 64), (16, 4, 2, 128), (64, 4, 1, 128), (30, 8, 2, 256)])
+@pytest.mark.parametrize("order", ["rising", "falling", "one far key", "far tree"])
+def test_scores_far_apart(osd, order, N, Hq, H, D, dtype):
+    """Scores that leave the range of a reference taken from the first keys, in
+    either direction, at any place: several hundred powers of two apart."""
+    import torch
+    g = np.random.default_rng(61)
+    lens = [700, 3, 64]
+    c = Cache(g, lens, N, H, D, 16, dtype)
+    q = queries(g, 3, N, Hq, D, dtype)
+    q[..., 0] = 4.0
+    parent = trees(g, 3, N)
+    for b, n in enumerate(lens):
+        for j in range(n + N):
+            p, s = c.row(b, j)
+            if order == "rising":
+                x = j * 0.5
+            elif order == "falling":
+                x = -j * 0.5
+            elif order == "one far key":
+                x = 200.0 if j == max(n - 2, 0) else 0.0
+            else:
+                x = 150.0 if j == n else -100.0 if j == n + 1 else 0.0
+            c.k[p, :, s, 0] = x
+    got = osd.osd_tree_attention(q, c.k, c.v, c.d_table, c.d_lens, dev(parent), scale=0.5)
+    want, mass, reach = ref.attention(f64(q), f64(c.k), f64(c.v), c.table, lens, 0.5, parent)
+    check_attention(got, want, mass, reach, 700 + N, dtype, order)
+
+
+@pytest.mark.parametrize("lens,N,Hq,H,D", [([9000], 64, 4, 1, 128), ([3000, 40], 64, 16, 2, 64), ([5000], 64, 12, 1, 256),
+                                           ([2000] * 3, 33, 32, 1, 128), ([700] * 70, 3, 8, 4, 64), ([300] * 40, 20, 32, 8, 128)])
+def test_divisions(osd, lens, N, Hq, H, D):
+    """Units cut apart into many parts that are joined together, units in a row, row
+    blocks, more sequences than a wave has lanes."""
+    g = np.random.default_rng(67)
+    new = [int(x) for x in g.integers(1, N + 1, len(lens))]
+    parity(osd, g, lens, N, Hq, H, D, 16, "bf16", True, new=new, label=str((len(lens), N, Hq, H, D)))
+    if D < 256:
+        parity(osd, g, lens[:3], N, Hq, H, D, 8, "f32", True)
+
+
 def test_many_sequences(osd):
     g = np.random.default_rng(5)
     lens = [int(x) for x in g.integers(0, 200, 300)]
