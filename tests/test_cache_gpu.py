@@ -144,6 +144,21 @@ def test_append_at_the_largest_length(osd):
         assert torch.isnan(q).all() and torch.equal(c.k, before)
 
 
+def test_append_of_more_tokens_than_a_launch_has_threads_for(osd):
+    """2^26 + 5 tokens, a wave each: more than 2^32 threads.  All land where the pages say."""
+    import torch
+    N, S = (1 << 26) + 5, 1 << 16
+    pages = -(-N // S)
+    k = torch.randint(-(1 << 15), 1 << 15, (1, N, 1, 8), device="cuda", dtype=torch.int16).view(torch.bfloat16)
+    v = torch.randint(-(1 << 15), 1 << 15, (1, N, 1, 8), device="cuda", dtype=torch.int16).view(torch.bfloat16)
+    k_cache, v_cache = (torch.zeros(pages, 1, S, 8, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    table = torch.arange(pages - 1, -1, -1, device="cuda", dtype=torch.int32)[None]
+    osd.osd_cache_append(k, v, k_cache, v_cache, table, torch.zeros(1, device="cuda", dtype=torch.int32))
+    for cache, x in ((k_cache, k), (v_cache, v)):
+        got = cache.flip(0).view(-1, 8).view(torch.int16)
+        assert torch.equal(got[:N], x.view(N, 8).view(torch.int16)) and not got[N:].any()
+
+
 def test_append_graph(osd):
     import torch
     g = np.random.default_rng(5)
