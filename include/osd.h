@@ -10,7 +10,9 @@
  *   osd_distill_loss_grad  the distillation divergence of Eq. 3 (forward KL,
  *                          reverse KL, JSD[beta]) and its gradient with
  *                          respect to the draft (student) logits (Section 4.1,
- *                          Eq. 2-4).
+ *                          Eq. 2-4);
+ * and what the model does with drafted tokens in every layer between the two, on a
+ * paged cache: osd_cache_append, osd_tree_attention, osd_cache_keep.
  *
  * Conventions shared by every entry point:
  *   - All array arguments are DEVICE pointers owned by the caller; the library
