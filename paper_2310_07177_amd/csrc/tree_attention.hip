@@ -38,6 +38,7 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
     __shared__ float s_stat[kWaves][ROWS][2];
     __shared__ uint64_t s_sees[ROWS];
     __shared__ int s_odd[kWaves];
+    __shared__ int64_t s_place[ROWS];
 
     Division<kThreads, TILE> share;
     share.init(a, s_tiles);
@@ -160,10 +161,11 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
             bool tree;
             const uint64_t all = wave_ancestors(L.parent ? L.parent + int64_t(p.b) * L.N : nullptr, p.seq.n, &tree);
             bad = bad || !tree;
+            const uint64_t nodes = p.seq.n < kWave ? (uint64_t(1) << p.seq.n) - 1 : ~uint64_t(0);
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 const int node = (p.row0 + mt * 16 + col) / a.group;
-                rows.sees[mt] = uint64_t(__shfl(static_cast<unsigned long long>(all), node & (kWave - 1)));
+                rows.sees[mt] = uint64_t(__shfl(static_cast<unsigned long long>(all), node & (kWave - 1))) & nodes;
             }
         }
         rows.clear();
@@ -206,6 +208,7 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
             }
         }
         if (lane == 0) s_odd[wave] = rows.odd;
+        if (tid < p.rows) s_place[tid] = row_place<Fmt>(a, p, tid, D);
         __syncthreads();
         const bool odd = s_odd[0] || s_odd[1] || s_odd[2] || s_odd[3];
 #pragma unroll
@@ -230,12 +233,15 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
                     const float s = s_stat[x][row][1];
                     total += s == s ? s * rescale(s_stat[x][row][0], most) : s;
                 }
-                if (p.whole) write_row<Fmt>(a, p, row, d, D, o, total);
+                if (p.whole) write_row<Fmt>(a, s_place[row], d, o, 1.0f / total);
                 else post_part<ROWS, DT>(a, p.slot, row, d, o, most, total);
             }
             __syncthreads();
         }
-        if (!p.whole) join<Fmt, kThreads, ROWS, DT>(a, p, share.apart, D);
+        if (!p.whole) {
+            join<Fmt, kThreads, ROWS, DT>(a, p, share.apart, D, s_place);
+            __syncthreads();  // the places are free
+        }
         pos += share.step(p);
     }
 }

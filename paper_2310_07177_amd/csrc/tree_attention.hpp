@@ -94,16 +94,18 @@ struct Bf16Ops {
     }
     static constexpr int kParts = 1;  // instructions of a product
     __device__ static f32x4_t pv_part(const chunk_t& v, const Probs& p, int, f32x4_t o) { return qk(v, p.x, o); }
-    // Of an operand of the second product: what is not finite to 0, whether there is any.
-    __device__ static bool clean(chunk_t& v) {
-        bool odd = false;
+    // Of an operand of the second product: nonzero where a value is not finite (an exponent of all ones
+    // carries into the sign's place), and those to 0.
+    static constexpr uint32_t kSigns = 0x80008000u;
+    __device__ static uint32_t carries(const chunk_t& v) {
+        uint32_t c = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t x = pair_finite(v[i]);
-            odd = odd || x != v[i];
-            v[i] = x;
-        }
-        return odd;
+        for (int i = 0; i < 4; ++i) c |= (v[i] & 0x7F807F80u) + 0x00800080u;
+        return c;
+    }
+    __device__ static void clean(chunk_t& v) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = pair_finite(v[i]);
     }
     __device__ static uint32_t half_finite(uint32_t h) { return (h & 0x7F80u) == 0x7F80u ? 0u : h; }
     __device__ static uint32_t pair_finite(uint32_t h) { return half_finite(h & 0xFFFFu) | half_finite(h >> 16) << 16; }
@@ -150,15 +152,16 @@ struct F32Ops {
     __device__ static f32x4_t pv_part(const chunk_t& v, const Probs& p, int i, f32x4_t o) {
         return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[i]), p.x[i], o, 0, 0, 0);
     }
-    __device__ static bool clean(chunk_t& v) {
-        bool odd = false;
+    static constexpr uint32_t kSigns = 0x80000000u;
+    __device__ static uint32_t carries(const chunk_t& v) {
+        uint32_t c = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bool bad = (v[i] & 0x7F800000u) == 0x7F800000u;
-            odd = odd || bad;
-            v[i] = bad ? 0u : v[i];
-        }
-        return odd;
+        for (int i = 0; i < 4; ++i) c |= (v[i] & 0x7F800000u) + 0x00800000u;
+        return c;
+    }
+    __device__ static void clean(chunk_t& v) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (v[i] & 0x7F800000u) == 0x7F800000u ? 0u : v[i];
     }
     template <int VW>
     __device__ static void clean(Value<VW>& v) {
@@ -451,15 +454,20 @@ struct Rows {
     // Where keys that not every row sees begin, j0 their first step's.
     __device__ void mask(f32x4_t (&s)[MT][KT], int j0, const Seq& seq) const {
         const int grp = (int(threadIdx.x) & (kWave - 1)) >> 4;
+        // The lane's first key, counted from the tree's; bit i of `on`: whether the row sees key first + i.
+        // (Without branches: hipcc lost scores where lanes parted here.)
+        const int first = j0 + grp * 4 - seq.len, up = first > 0 ? first : 0, down = first < 0 ? -first : 0;
+        const uint32_t context = down < 32 ? (1u << (down & 31)) - 1u : ~0u;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int mt = 0; mt < MT; ++mt) {
+            uint32_t on = uint32_t((sees[mt] >> (up & 63)) << (down & 31));
+            on = (up < 64 && down < 32 ? on : 0u) | context;
 #pragma unroll
             for (int i = 0; i < KEYS; ++i) {
-                const int j = j0 + (i / 4) * 16 + grp * 4 + (i & 3) - seq.len;
-                // (Without branches: hipcc lost the score where lanes parted here.)
-                const uint32_t on = uint32_t(j < 0) | (uint32_t(j < seq.n) & uint32_t(sees[mt] >> (j & 63)));
-                s[mt][i / 4][i & 3] = (on & 1u) != 0u ? s[mt][i / 4][i & 3] : kNegInf;
+                const uint32_t bit = 1u << ((i / 4) * 16 + (i & 3));
+                s[mt][i / 4][i & 3] = (on & bit) != 0u ? s[mt][i / 4][i & 3] : kNegInf;
             }
+        }
     }
     __device__ static void largest(const f32x4_t (&s)[MT][KT], float (&most)[MT]) {
 #pragma unroll
@@ -551,16 +559,20 @@ __device__ inline void add_odd(const TreeAttentionLaunch& L, int b, int h, int d
     }
 }
 
+// Where a row's values go: a byte offset in the output (a multiple of 16), 1 more for a row of zeros.
+template <typename Fmt>
+__device__ inline int64_t row_place(const Args& a, const Piece& p, int row, int D) {
+    const TreeAttentionLaunch& L = a.L;
+    const int at = p.row0 + row, node = int(uint32_t(at) / uint32_t(a.group)), g = at - node * a.group;
+    const bool on = row < p.live || (p.seq.state == 2 && (p.seq.n < 0 || p.seq.n > node));
+    return ((int64_t(p.b) * L.N + node) * L.q_heads + p.h * a.group + g) * (D * Fmt::kBytes) + (on ? 0 : 1);
+}
 // Four values of a row to the output.
 template <typename Fmt>
-__device__ inline void write_row(const Args& a, const Piece& p, int row, int d, int D, f32x4_t o, float total) {
-    const TreeAttentionLaunch& L = a.L;
-    const int at = p.row0 + row, node = at / a.group, g = at - node * a.group;
-    char* to = L.out + (((int64_t(p.b) * L.N + node) * L.q_heads + p.h * a.group + g) * D + d) * Fmt::kBytes;
-    const float inv = 1.0f / total;
-    const bool on = row < p.live || (p.seq.state == 2 && (p.seq.n < 0 || p.seq.n > node));
+__device__ inline void write_row(const Args& a, int64_t place, int d, f32x4_t o, float inv) {
+    char* to = a.L.out + (place & ~int64_t(1)) + d * Fmt::kBytes;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = on ? o[e] * inv : 0.0f;
+    for (int e = 0; e < 4; ++e) o[e] = (place & 1) == 0 ? o[e] * inv : 0.0f;
     if constexpr (Fmt::kBytes == 2) *reinterpret_cast<u32x2_t*>(to) = u32x2_t{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
     else *reinterpret_cast<f32x4_t*>(to) = o;
 }
@@ -584,7 +596,7 @@ __device__ inline void post_part(const Args& a, int slot, int row, int d, f32x4_
 // Rows r0 .. r1-1 of a unit from its parts, in their order: ITEMS times four values of a
 // thread, PIECES parts in flight each.
 template <typename Fmt, int THREADS, int ROWS, int DT, int ITEMS, int PIECES>
-__device__ inline void join_parts(const Args& a, const Piece& p, int r0, int r1, int D) {
+__device__ inline void join_parts(const Args& a, const Piece& p, int r0, int r1, int D, const int64_t* places) {
     const auto stats = buffer_of(a.stats, a.stats_bytes), parts = buffer_of(a.parts, a.parts_bytes);
     const int items = r1 * (DT / 4), count = p.count;
     for (int i0 = r0 * (DT / 4) + int(threadIdx.x); i0 < items; i0 += THREADS * ITEMS) {
@@ -631,7 +643,7 @@ __device__ inline void join_parts(const Args& a, const Piece& p, int r0, int r1,
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
             const int i = i0 + k * THREADS, row = i / (DT / 4), d = i % (DT / 4) * 4;
-            if (i < items && d < D) write_row<Fmt>(a, p, row, d, D, o[k], total[k]);
+            if (i < items && d < D) write_row<Fmt>(a, places[row], d, o[k], 1.0f / total[k]);
         }
     }
 }
@@ -639,21 +651,22 @@ __device__ inline void join_parts(const Args& a, const Piece& p, int r0, int r1,
 // A workgroup has posted its part of a unit (all its threads call this).  Where the unit's
 // parts are many and large, its workgroups wait for each other and join some rows each: a
 // workgroup alone reads 50 GB/s.  The wait is bounded, and nothing depends on who waits: rows
-// are taken from a counter, and the last to arrive does not wait and takes what is left.
+// are taken from a counter, and the last to arrive does not wait and takes what is left.  (places: of
+// the unit's rows, in LDS.)
 constexpr int kJoinBytes = 128 << 10;  // of a unit's parts: fewer are joined by the last alone
 constexpr int kJoinPolls = 64;
 
 template <typename Fmt, int THREADS, int ROWS, int DT>
-__device__ inline void join_rows(const Args& a, const Piece& p, int r0, int r1, int D) {
+__device__ inline void join_rows(const Args& a, const Piece& p, int r0, int r1, int D, const int64_t* places) {
     // A read takes about 2 us, so as many as registers allow are in flight.
-    if (p.count <= 2) join_parts<Fmt, THREADS, ROWS, DT, 8, 2>(a, p, r0, r1, D);
-    else if (p.count <= 4) join_parts<Fmt, THREADS, ROWS, DT, 4, 4>(a, p, r0, r1, D);
-    else if ((r1 - r0) * (DT / 4) > THREADS) join_parts<Fmt, THREADS, ROWS, DT, 2, 8>(a, p, r0, r1, D);
-    else join_parts<Fmt, THREADS, ROWS, DT, 1, 16>(a, p, r0, r1, D);
+    if (p.count <= 2) join_parts<Fmt, THREADS, ROWS, DT, 8, 2>(a, p, r0, r1, D, places);
+    else if (p.count <= 4) join_parts<Fmt, THREADS, ROWS, DT, 4, 4>(a, p, r0, r1, D, places);
+    else if ((r1 - r0) * (DT / 4) > THREADS) join_parts<Fmt, THREADS, ROWS, DT, 2, 8>(a, p, r0, r1, D, places);
+    else join_parts<Fmt, THREADS, ROWS, DT, 1, 16>(a, p, r0, r1, D, places);
 }
 
 template <typename Fmt, int THREADS, int ROWS, int DT>
-__device__ inline void join(const Args& a, const Piece& p, bool together, int D) {
+__device__ inline void join(const Args& a, const Piece& p, bool together, int D, const int64_t* places) {
     __shared__ uint32_t s_word;
     const int tid = int(threadIdx.x);
     uint32_t* arrivals = a.counters + 3 * p.w0;
@@ -674,7 +687,7 @@ __device__ inline void join(const Args& a, const Piece& p, bool together, int D)
     const bool all = s_word != 0;
     if (!together) {
         if (!all) return;
-        join_rows<Fmt, THREADS, ROWS, DT>(a, p, 0, p.rows, D);
+        join_rows<Fmt, THREADS, ROWS, DT>(a, p, 0, p.rows, D, places);
         if (tid == 0) __hip_atomic_store(arrivals, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         return;
     }
@@ -685,7 +698,7 @@ __device__ inline void join(const Args& a, const Piece& p, bool together, int D)
         __syncthreads();
         const int r0 = int(s_word) * some;
         if (r0 >= p.rows) break;
-        join_rows<Fmt, THREADS, ROWS, DT>(a, p, r0, r0 + some < p.rows ? r0 + some : p.rows, D);
+        join_rows<Fmt, THREADS, ROWS, DT>(a, p, r0, r0 + some < p.rows ? r0 + some : p.rows, D, places);
     }
     // The last to leave clears the counters.
     if (tid == 0 && arrive(gone) == uint32_t(p.count - 1)) {

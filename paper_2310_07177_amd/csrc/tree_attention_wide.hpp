@@ -68,6 +68,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
     __shared__ uint64_t s_sees[ROWS];
     __shared__ int s_flags[kWaves];
     __shared__ int s_page[kPageWindow];
+    __shared__ int64_t s_place[ROWS];
+    __shared__ float s_total[ROWS][2];  // maximum; sum, or its reciprocal
     float(*s_acc)[16][PITCH] = reinterpret_cast<float(*)[16][PITCH]>(s_ring);
     const uint32_t ring = uint32_t(uintptr_t((__attribute__((address_space(3))) char*)s_ring));
 
@@ -175,10 +177,11 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
             bool tree;
             const uint64_t all = wave_ancestors(L.parent ? L.parent + int64_t(p.b) * L.N : nullptr, p.seq.n, &tree);
             bad = bad || !tree;
+            const uint64_t nodes = p.seq.n < kWave ? (uint64_t(1) << p.seq.n) - 1 : ~uint64_t(0);
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 const int node = (p.row0 + (wr * MT + mt) * 16 + col) / a.group;
-                rows.sees[mt] = uint64_t(__shfl(static_cast<unsigned long long>(all), node & (kWave - 1)));
+                rows.sees[mt] = uint64_t(__shfl(static_cast<unsigned long long>(all), node & (kWave - 1))) & nodes;
             }
         }
 
@@ -273,12 +276,18 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
             for (int batch = 0; batch < BATCHES; ++batch) {
                 if (batch + 1 < BATCHES) read_v(batch + 1);
                 if constexpr (TAIL) {
+                    uint32_t carries = 0;
 #pragma unroll
                     for (int u = 0; u < BATCH; ++u) {
                         if (batch * BATCH + u >= NC) continue;
                         v[batch & 1][u] &= in;
-                        const bool odd = Ops::clean(v[batch & 1][u]);
-                        rows.odd = rows.odd || __any(odd);
+                        carries |= Ops::carries(v[batch & 1][u]);
+                    }
+                    if (__any((carries & Ops::kSigns) != 0)) {
+                        rows.odd = true;
+#pragma unroll
+                        for (int u = 0; u < BATCH; ++u)
+                            if (batch * BATCH + u < NC) Ops::clean(v[batch & 1][u]);
                     }
                 }
                 // (Products of several tiles in turn: each of fp32 would wait for the one before it.)
@@ -372,36 +381,44 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
         int flags = 0;
 #pragma unroll
         for (int i = 0; i < kWaves; ++i) flags |= s_flags[i];
+        // What all values of a row share, once for each: its sums (with half of the rows in use the other
+        // half is padding: zeros), where it goes.
+        if (tid < ROWS) {
+            const int x = tid / (16 * MT), at = tid % (16 * MT);
+            float most = kNegInf, total = 0.0f;
+            if (x < row_waves) {
+                for (int y = 0; y < key_waves; ++y) most = fmaxf(most, s_stat[x * key_waves + y][at][0]);
+                for (int y = 0; y < key_waves; ++y) {
+                    const float s = s_stat[x * key_waves + y][at][1];
+                    total += s == s ? s * rescale(s_stat[x * key_waves + y][at][0], most) : s;
+                }
+            }
+            if (flags & 1) total = __builtin_nanf("");
+            s_total[tid][0] = most;
+            s_total[tid][1] = p.whole ? 1.0f / total : total;
+            s_place[tid] = tid < p.rows ? row_place<Fmt>(a, p, tid, D) : -1;
+        }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             float all = kNegInf;
             for (int i = 0; i < key_waves; ++i) all = fmaxf(all, s_stat[wr * key_waves + i][mt * 16 + col][0]);
             rows.template store<PITCH>(mt, rescale(rows.ref[mt], all), s_acc[wave][col]);
             __syncthreads();
-            // (With half of the rows in use the other half is padding: zeros.)
             for (int i = tid; i < WR * 16 * (DT / 4); i += kThreads) {
                 const int rr = i / (DT / 4), d = i % (DT / 4) * 4, x = rr / 16, r = rr % 16, row = (x * MT + mt) * 16 + r;
-                if (row >= p.rows || d >= D) continue;
+                const int64_t place = s_place[row];
+                if (place < 0 || (!FULL && d >= D)) continue;
                 f32x4_t o = {0, 0, 0, 0};
-                float most = kNegInf, total = 0.0f;
                 if (x < row_waves) {
-                    for (int y = 0; y < key_waves; ++y) {
-                        o += *reinterpret_cast<const f32x4_t*>(&s_acc[x * key_waves + y][r][d]);
-                        most = fmaxf(most, s_stat[x * key_waves + y][mt * 16 + r][0]);
-                    }
+                    for (int y = 0; y < key_waves; ++y) o += *reinterpret_cast<const f32x4_t*>(&s_acc[x * key_waves + y][r][d]);
                     if ((flags & 2) && row < p.live) add_odd<Fmt>(L, p.b, p.h, d, len, T, len / STEP * STEP, s_sees[row], o);
-                    for (int y = 0; y < key_waves; ++y) {
-                        const float s = s_stat[x * key_waves + y][mt * 16 + r][1];
-                        total += s == s ? s * rescale(s_stat[x * key_waves + y][mt * 16 + r][0], most) : s;
-                    }
                 }
-                if (flags & 1) total = __builtin_nanf("");
-                if (p.whole) write_row<Fmt>(a, p, row, d, D, o, total);
-                else post_part<ROWS, DT>(a, p.slot, row, d, o, most, total);
+                if (p.whole) write_row<Fmt>(a, place, d, o, s_total[row][1]);
+                else post_part<ROWS, DT>(a, p.slot, row, d, o, s_total[row][0], s_total[row][1]);
             }
             __syncthreads();
         }
-        if (!p.whole) join<Fmt, kThreads, ROWS, DT>(a, p, share.apart, D);
+        if (!p.whole) join<Fmt, kThreads, ROWS, DT>(a, p, share.apart, D, s_place);
         pos += share.step(p);
         __syncthreads();  // the ring and the pages are free
     }
