@@ -216,7 +216,7 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
             float all = kNegInf;
 #pragma unroll
             for (int i = 0; i < kWaves; ++i) all = fmaxf(all, s_stat[i][mt * 16 + col][0]);
-            rows.template store<PITCH>(mt, rescale(rows.ref[mt], all), s_acc[wave][col]);
+            rows.template store<PITCH>(mt, rescale(rows.ref[mt], all), s_acc[wave][col], grp);
             __syncthreads();
             for (int i = tid; i < 16 * (DT / 4); i += kThreads) {
                 const int rr = i / (DT / 4), d = i % (DT / 4) * 4, row = mt * 16 + rr;

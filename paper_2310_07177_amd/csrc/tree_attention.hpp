@@ -44,6 +44,14 @@ __device__ inline float rows_sum(float x) {
 // 2^(a - b), 0 where a is -inf (nothing seen yet).
 __device__ inline float rescale(float a, float b) { return a == kNegInf ? 0.0f : exp2_fast(a - b); }
 
+// x, of which the compiler computes nothing ahead: what is derived from a thread's number for the end of a
+// piece would otherwise be computed before the loop over pieces and lie in scratch memory meanwhile
+// (44 registers of 512 threads of 256 workgroups: 23 MB, 5 us).
+__device__ inline int here(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // The matrix products of one format.  KT tiles of 16 keys make a step.
 //   K: chunk c of a key holds elements c * kChunk + group * (16 / ES) ..
 //   V: a lane holds VW elements of a row for each block of 16 * VW of them.
@@ -389,7 +397,7 @@ template <typename Ops, int CHUNKS, bool FULL>
 __device__ inline void load_queries(const Args& a, const Piece& p, int r, int D, chunk_t (&q)[CHUNKS]) {
     const TreeAttentionLaunch& L = a.L;
     constexpr int ES = Ops::Fmt::kBytes;
-    const int grp = (int(threadIdx.x) & (kWave - 1)) >> 4;
+    const int grp = (here(int(threadIdx.x)) & (kWave - 1)) >> 4;
     const int node = (p.row0 + r) / a.group, g = p.row0 + r - node * a.group;
     const char* at = L.q + (int64_t(p.b) * L.N + node) * L.q_stride + int64_t(p.h * a.group + g) * D * ES + grp * 16;
 #pragma unroll
@@ -526,8 +534,7 @@ struct Rows {
     }
     // The sums of row tile mt, times f, to a row of LDS.
     template <int PITCH>
-    __device__ void store(int mt, float f, float* row) const {
-        const int grp = (int(threadIdx.x) & (kWave - 1)) >> 4;
+    __device__ void store(int mt, float f, float* row, int grp) const {
 #pragma unroll
         for (int n = 0; n < BLOCKS; ++n) {
             if constexpr (VW == 1) {
@@ -599,7 +606,7 @@ template <typename Fmt, int THREADS, int ROWS, int DT, int ITEMS, int PIECES>
 __device__ inline void join_parts(const Args& a, const Piece& p, int r0, int r1, int D, const int64_t* places) {
     const auto stats = buffer_of(a.stats, a.stats_bytes), parts = buffer_of(a.parts, a.parts_bytes);
     const int items = r1 * (DT / 4), count = p.count;
-    for (int i0 = r0 * (DT / 4) + int(threadIdx.x); i0 < items; i0 += THREADS * ITEMS) {
+    for (int i0 = r0 * (DT / 4) + here(int(threadIdx.x)); i0 < items; i0 += THREADS * ITEMS) {
         float most[ITEMS], total[ITEMS];
         f32x4_t o[ITEMS];
 #pragma unroll

@@ -57,6 +57,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
     using R = Rows<Ops, NC * 16, MT, 1>;
     constexpr int ES = S::ES, CHUNKS = R::CHUNKS, KT = R::KT, STEP = S::STEP, STAGE = S::STAGE, ROWS = S::ROWS;
     constexpr int PITCH = S::PITCH, CPR = S::CPR, ROW = S::ROW;
+    static_assert(WR == 4 || WR == kWaves, "two waves share keys, or one, or two with half of the rows");
     const TreeAttentionLaunch& L = a.L;
     const int tid = int(threadIdx.x), lane = tid & (kWave - 1), col = lane & 15, grp = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -383,8 +384,9 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
         for (int i = 0; i < kWaves; ++i) flags |= s_flags[i];
         // What all values of a row share, once for each: its sums (with half of the rows in use the other
         // half is padding: zeros), where it goes.
-        if (tid < ROWS) {
-            const int x = tid / (16 * MT), at = tid % (16 * MT);
+        const int t0 = here(tid), col0 = t0 & 15, grp0 = (t0 & (kWave - 1)) >> 4;
+        if (t0 < ROWS) {
+            const int x = t0 / (16 * MT), at = t0 % (16 * MT);
             float most = kNegInf, total = 0.0f;
             if (x < row_waves) {
                 for (int y = 0; y < key_waves; ++y) most = fmaxf(most, s_stat[x * key_waves + y][at][0]);
@@ -394,27 +396,44 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                 }
             }
             if (flags & 1) total = __builtin_nanf("");
-            s_total[tid][0] = most;
-            s_total[tid][1] = p.whole ? 1.0f / total : total;
-            s_place[tid] = tid < p.rows ? row_place<Fmt>(a, p, tid, D) : -1;
+            s_total[t0][0] = most;
+            s_total[t0][1] = p.whole ? 1.0f / total : total;
+            s_place[t0] = t0 < p.rows ? row_place<Fmt>(a, p, t0, D) : -1;
         }
+        // (A thread's values of ITEMS rows at once: one after another they would wait for LDS.)
+        constexpr int EACH = WR * 16 * (DT / 4) / kThreads, ITEMS = EACH < 4 ? EACH : 4;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             float all = kNegInf;
-            for (int i = 0; i < key_waves; ++i) all = fmaxf(all, s_stat[wr * key_waves + i][mt * 16 + col][0]);
-            rows.template store<PITCH>(mt, rescale(rows.ref[mt], all), s_acc[wave][col]);
+            for (int i = 0; i < key_waves; ++i) all = fmaxf(all, s_stat[wr * key_waves + i][mt * 16 + col0][0]);
+            rows.template store<PITCH>(mt, rescale(rows.ref[mt], all), s_acc[wave][col0], grp0);
             __syncthreads();
-            for (int i = tid; i < WR * 16 * (DT / 4); i += kThreads) {
-                const int rr = i / (DT / 4), d = i % (DT / 4) * 4, x = rr / 16, r = rr % 16, row = (x * MT + mt) * 16 + r;
-                const int64_t place = s_place[row];
-                if (place < 0 || (!FULL && d >= D)) continue;
-                f32x4_t o = {0, 0, 0, 0};
-                if (x < row_waves) {
-                    for (int y = 0; y < key_waves; ++y) o += *reinterpret_cast<const f32x4_t*>(&s_acc[x * key_waves + y][r][d]);
-                    if ((flags & 2) && row < p.live) add_odd<Fmt>(L, p.b, p.h, d, len, T, len / STEP * STEP, s_sees[row], o);
+#pragma nounroll
+            for (int i0 = 0; i0 < EACH; i0 += ITEMS) {
+                f32x4_t o[ITEMS];
+                float most[ITEMS], total[ITEMS];
+                int64_t place[ITEMS];
+#pragma unroll
+                for (int k = 0; k < ITEMS; ++k) {
+                    const int i = (i0 + k) * kThreads + t0, x = i / (16 * (DT / 4)), r = i / (DT / 4) % 16, d = i % (DT / 4) * 4;
+                    const int row = (x * MT + mt) * 16 + r;
+                    place[k] = s_place[row];
+                    most[k] = s_total[row][0];
+                    total[k] = s_total[row][1];
+                    const bool sums = x < row_waves;
+                    o[k] = *reinterpret_cast<const f32x4_t*>(&s_acc[sums ? x * key_waves : 0][r][d]);
+                    if (WR < kWaves || half) o[k] += *reinterpret_cast<const f32x4_t*>(&s_acc[sums ? x * key_waves + 1 : 0][r][d]);
+                    if (!sums) o[k] = f32x4_t{0, 0, 0, 0};
                 }
-                if (p.whole) write_row<Fmt>(a, place, d, o, s_total[row][1]);
-                else post_part<ROWS, DT>(a, p.slot, row, d, o, s_total[row][0], s_total[row][1]);
+#pragma unroll
+                for (int k = 0; k < ITEMS; ++k) {
+                    const int i = (i0 + k) * kThreads + t0, x = i / (16 * (DT / 4)), r = i / (DT / 4) % 16, d = i % (DT / 4) * 4;
+                    const int row = (x * MT + mt) * 16 + r;
+                    if (place[k] < 0 || (!FULL && d >= D)) continue;
+                    if ((flags & 2) && row < p.live) add_odd<Fmt>(L, p.b, p.h, d, len, T, len / STEP * STEP, s_sees[row], o[k]);
+                    if (p.whole) write_row<Fmt>(a, place[k], d, o[k], total[k]);
+                    else post_part<ROWS, DT>(a, p.slot, row, d, o[k], most[k], total[k]);
+                }
             }
             __syncthreads();
         }
