@@ -59,8 +59,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
     constexpr int PITCH = S::PITCH, CPR = S::CPR, ROW = S::ROW;
     static_assert(WR == 4 || WR == kWaves, "two waves share keys, or one, or two with half of the rows");
     const TreeAttentionLaunch& L = a.L;
-    const int tid = int(threadIdx.x), lane = tid & (kWave - 1), col = lane & 15, grp = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave);
     const int D = FULL ? DT : L.head_dim;
 
     extern __shared__ int s_tiles[];  // [B + 1]
@@ -86,13 +85,14 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
     int lane_key[S::LOADS], lane_chunk[S::LOADS];
 #pragma unroll
     for (int x = 0; x < S::LOADS; ++x) {
-        const int at = (wave * S::LOADS + x) * kWave + lane, key = at / CPR;
+        const int lane = int(threadIdx.x) & (kWave - 1), at = (wave * S::LOADS + x) * kWave + lane, key = at / CPR;
         lane_key[x] = lane / CPR;
         lane_chunk[x] = (at % CPR) ^ swizzle(key);
     }
     const bool even_pages = L.pages.page_size % 8 == 0;  // a load's keys (8 at most) lie on one page
 
     for (int64_t pos = first; pos < end;) {
+        const int tid = here(int(threadIdx.x)), lane = tid & (kWave - 1), col = lane & 15, grp = lane >> 4;
         const Piece p = share.template find<ROWS>(a, w, pos, first, end);
         const int len = p.seq.len, T = p.T;
         bool bad = p.seq.state == 2;
