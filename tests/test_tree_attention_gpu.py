@@ -127,6 +127,14 @@ def test_many_sequences(osd):
     parity(osd, g, lens, 1, 2, 1, 8, 16, "f32", False)
 
 
+@pytest.mark.parametrize("N,Hq,D,dtype", [(1, 1, 128, "bf16"), (9, 16, 128, "bf16"), (9, 8, 256, "bf16"), (5, 4, 256, "f32")])
+def test_the_largest_batch(osd, N, Hq, D, dtype):
+    """4096 sequences, most of them padding: the kernels with the most LDS beside the batch's table."""
+    g = np.random.default_rng(N + D)
+    lens = [int(x) if x >= 0 and g.random() < 0.1 else -1 for x in g.integers(0, 40, 4096)]
+    parity(osd, g, lens, N, Hq, 1, D, 16, dtype, N > 1)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_padding_and_invalid_sequences(osd, dtype):
     import torch
