@@ -1,0 +1,60 @@
+"""osd_tree_attention where values are not finite: a row that sees one gets exactly
+that, whatever its key's place in a tile, and however the work is divided."""
+import numpy as np
+import pytest
+
+from oracle import cache_ref as ref
+from tests._cache_helpers import Cache, dev, torch_dtype, trees
+
+pytestmark = pytest.mark.gpu
+
+WHAT = {"nan": float("nan"), "inf": float("inf"), "-inf": -float("inf")}
+
+
+@pytest.fixture(scope="module")
+def osd():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU")
+    import paper_2310_07177_amd as m
+    m.lib()
+    return m
+
+
+def queries(g, B, N, Hq, D, dtype):
+    return dev(g.normal(0, 1, (B, N, Hq, D)).astype(np.float32), torch_dtype(dtype))
+
+
+@pytest.mark.parametrize("what", sorted(WHAT))
+@pytest.mark.parametrize("N,G", [(3, 4), (5, 4), (32, 4), (64, 4)])
+@pytest.mark.parametrize("D", [64, 80, 128, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cut", [False, True])
+def test_the_context_last_tokens(osd, cut, dtype, D, N, G, what):
+    """One value of each of the last 64 tokens of the context in turn, contexts of all
+    residues of a stage, units in a row (few of them shared) or cut apart: all nodes see
+    it, in one value of one kv head's rows, and nothing else changes by a bit."""
+    import torch
+    g = np.random.default_rng(D + N)
+    H = 1 if cut else 12
+    column, head = D - 3, H - 1
+    for lens in (np.arange(130, 194).reshape(-1, 4) if cut else np.arange(66, 130).reshape(1, -1)).tolist():
+        B = len(lens)
+        c = Cache(g, lens, N, H, D, 16, dtype)
+        q, parent = queries(g, B, N, G * H, D, dtype), dev(trees(g, B, N))
+        clean = osd.osd_tree_attention(q, c.k, c.v, c.d_table, c.d_lens, parent)
+        assert torch.isfinite(clean).all()
+        wrong = torch.zeros((), device="cuda", dtype=torch.bool)
+        for back in range(1, 65):
+            j = c.d_lens.long() - back
+            page, slot = c.d_table.long().gather(1, (j // 16)[:, None])[:, 0], j % 16
+            held = c.v[page, head, slot, column].clone()
+            c.v[page, head, slot, column] = WHAT[what]
+            got = osd.osd_tree_attention(q, c.k, c.v, c.d_table, c.d_lens, parent)
+            c.v[page, head, slot, column] = held
+            hit = got[:, :, head * G:, column].clone()
+            wrong |= ~(hit.isnan() if what == "nan" else hit == WHAT[what]).all()
+            got[:, :, head * G:, column] = clean[:, :, head * G:, column]
+            wrong |= ~(got == clean).all()
+            if back % 16 == 0:
+                assert not wrong, (lens[0], back)
