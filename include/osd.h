@@ -598,7 +598,9 @@ int osd_cache_append(const osd_append* call, void* stream);
  * N <= OSD_MAX_TREE_NODES.  Padding, and sequences of length -1, get zeros.  A
  * sequence that is invalid (n_b outside 0 .. N, tokens beyond its table, a page
  * outside the cache, an invalid tree) gets NaN.  What the cache holds in tokens
- * that a node does not see (NaN, too) does not reach its output.  Scores, softmax
+ * that a node does not see (NaN, too) does not reach its output; an infinite value
+ * that it sees gives that infinity, or NaN where its probability is less than fp32
+ * holds (beside a score about 100 larger).  Scores, softmax
  * and sums are fp32; probabilities are rounded to bf16 for the product with bf16
  * values.  Work is divided over the GPU by the lengths in device memory, so a
  * captured call serves any lengths; how it is divided, and with it the last bits,

@@ -212,6 +212,8 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
         if (tid < p.rows) s_place[tid] = row_place<Fmt>(a, p, tid, D);
         __syncthreads();
         const bool odd = s_odd[0] || s_odd[1] || s_odd[2] || s_odd[3];
+        // Keys of the piece in steps that took 0 in the place of values that are not finite.
+        const int odd_from = max(len / STEP * STEP, p.t0 * TILE), odd_to = min(T, p.t1 * TILE);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             float all = kNegInf;
@@ -225,7 +227,7 @@ __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_ke
                 f32x4_t o = *reinterpret_cast<const f32x4_t*>(&s_acc[0][rr][d]);
 #pragma unroll
                 for (int x = 1; x < kWaves; ++x) o += *reinterpret_cast<const f32x4_t*>(&s_acc[x][rr][d]);
-                if (odd && row < p.live) add_odd<Fmt>(L, p.b, p.h, d, len, T, len / STEP * STEP, s_sees[row], o);
+                if (odd && row < p.live) add_odd<Fmt>(L, p.b, p.h, d, len, odd_from, odd_to, s_sees[row], o);
                 float most = kNegInf, total = 0.0f;
 #pragma unroll
                 for (int x = 0; x < kWaves; ++x) most = fmaxf(most, s_stat[x][row][0]);

@@ -553,11 +553,13 @@ struct Rows {
     }
 };
 
-// Adds the values d .. d+3 that are not finite of the keys from `from` on that a row sees.
+// Adds the values d .. d+3 that are not finite of the keys `from` .. `to`-1 that a row sees: those of this
+// workgroup's piece (one that saw none of them would post an infinity beside a maximum of -inf, and
+// the join make NaN of it).
 template <typename Fmt>
-__device__ inline void add_odd(const TreeAttentionLaunch& L, int b, int h, int d, int len, int T, int from, uint64_t sees,
+__device__ inline void add_odd(const TreeAttentionLaunch& L, int b, int h, int d, int len, int from, int to, uint64_t sees,
                                      f32x4_t& o) {
-    for (int j = from; j < T; ++j) {
+    for (int j = from; j < to; ++j) {
         if (j >= len && !(sees >> (j - len) & 1)) continue;
         const int64_t at = cache_place(L.pages, b, j);
         if (at < 0) continue;

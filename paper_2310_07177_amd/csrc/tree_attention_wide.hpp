@@ -433,8 +433,9 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                     const int i = (i0 + k) * kThreads + t0, x = i / (16 * (DT / 4)), r = i / (DT / 4) % 16, d = i % (DT / 4) * 4;
                     const int row = (x * MT + mt) * 16 + r;
                     if (place[k] < 0 || (!FULL && d >= D)) continue;
-                    // (From the first stage on that took values of 0 in the place of those that are not finite.)
-                    if ((flags & 2) && row < p.live) add_odd<Fmt>(L, p.b, p.h, d, len, T, len / STAGE * STAGE, s_sees[row], o[k]);
+                    // (The piece's keys in stages that took 0 in the place of values that are not finite.)
+                    if ((flags & 2) && row < p.live)
+                        add_odd<Fmt>(L, p.b, p.h, d, len, max(len / STAGE * STAGE, p.t0 * STAGE), min(T, p.t1 * STAGE), s_sees[row], o[k]);
                     if (p.whole) write_row<Fmt>(a, place[k], d, o[k], total[k]);
                     else post_part<ROWS, DT>(a, p.slot, row, d, o[k], most[k], total[k]);
                 }

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import cache_ref as ref
-from tests._cache_helpers import Cache, dev, torch_dtype, trees
+from tests._cache_helpers import Cache, check_attention, dev, f64, torch_dtype, trees
 
 pytestmark = pytest.mark.gpu
 
@@ -58,3 +58,24 @@ def test_the_context_last_tokens(osd, cut, dtype, D, N, G, what):
             wrong |= ~(got == clean).all()
             if back % 16 == 0:
                 assert not wrong, (lens[0], back)
+
+
+@pytest.mark.parametrize("N,G,H", [(16, 1, 1), (4, 4, 2), (64, 1, 1), (32, 4, 1), (64, 4, 1), (33, 2, 140)])
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_nodes_on_both_sides_of_a_border(osd, dtype, D, tree, N, G, H):
+    """Nodes of which some lie in one stage and some in the next, which other
+    workgroups may have: a row gets what it sees of both, and of none of them."""
+    g = np.random.default_rng(N + D)
+    for n in range(65, 260, 13 if H < 100 else 97):
+        c = Cache(g, [n, 40], N, H, D, 16, dtype)
+        q, parent = queries(g, 2, N, G * H, D, dtype), trees(g, 2, N) if tree else None
+        early, late = int(g.integers(0, N // 2)), int(g.integers(N // 2, N))
+        for node, values in ((early, {1: "inf", 3: "inf", 4: "nan", 6: "-inf"}), (late, {2: "-inf", 3: "inf", 5: "nan", 6: "inf"})):
+            page, slot = c.row(0, n + node)
+            for column, what in values.items():
+                c.v[page, :, slot, column] = WHAT[what]
+        got = osd.osd_tree_attention(q, c.k, c.v, c.d_table, c.d_lens, None if parent is None else dev(parent))
+        want, mass, reach = ref.attention(f64(q), f64(c.k), f64(c.v), c.table, [n, 40], D ** -0.5, parent)
+        check_attention(got, want, mass, reach, n + N, dtype, f"{n} {early} {late}")
