@@ -78,15 +78,25 @@ struct Bf16Ops {
                                                        0, 0, 0);
     }
     __device__ static chunk_t negate(chunk_t q) { return q ^ 0x80008000u; }
-    // Rounded to bf16, each off by at most 2^-8 of itself, which is what the product takes; the sum that divides them is
-    // of the fp32 ones.  Outputs lie 0.0024 from exact ones (relative, rms) instead of their own rounding's 0.0017.
+    // A probability as two bf16 numbers, its upper half and the rest: together off by at most 2^-15 + 2^-22 of
+    // it, so outputs lie 0.0017 (relative, rms) from exact ones, which is their own rounding.  One
+    // number, off by 2^-8, gives 0.0024 and half of the second product's instructions: 32 even sequences
+    // of 4032 tokens, 64 nodes, 195 us against 237; what memory bounds does not get slower (single tokens of
+    // 64 sequences 221 and 222 us).  The rest is of p (1 + 2^-23), so above 0 wherever p is: with one of 0 an
+    // infinite value would give NaN.
     struct Probs {
-        chunk_t x;
+        chunk_t x[2];
     };
     __device__ static Probs probs(const float (&p)[8]) {
+        constexpr float kUp = 1.00000011920928955078125f;  // 1 + 2^-23
         Probs r;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r.x[i] = pack_bf16x2(p[2 * i], p[2 * i + 1]);
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t a = __float_as_uint(p[2 * i]), b = __float_as_uint(p[2 * i + 1]);
+            r.x[0][i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+            r.x[1][i] = pack_bf16x2(fmaf(p[2 * i], kUp, -__uint_as_float(a & 0xFFFF0000u)),
+                                    fmaf(p[2 * i + 1], kUp, -__uint_as_float(b & 0xFFFF0000u)));
+        }
         return r;
     }
     // Element t of the 8 keys of a lane.
@@ -100,10 +110,11 @@ struct Bf16Ops {
     }
     template <int VW>
     __device__ static f32x4_t pv(const Value<VW> (&v)[8], int t, const Probs& p, f32x4_t o) {
-        return qk(column(v, t), p.x, o);
+        const chunk_t a = column(v, t);
+        return qk(a, p.x[1], qk(a, p.x[0], o));
     }
-    static constexpr int kParts = 1;  // instructions of a product
-    __device__ static f32x4_t pv_part(const chunk_t& v, const Probs& p, int, f32x4_t o) { return qk(v, p.x, o); }
+    static constexpr int kParts = 2;  // instructions of a product
+    __device__ static f32x4_t pv_part(const chunk_t& v, const Probs& p, int i, f32x4_t o) { return qk(v, p.x[i], o); }
     // Of an operand of the second product: nonzero where a value is not finite (an exponent of all ones
     // carries into the sign's place), and those to 0.
     static constexpr uint32_t kSigns = 0x80008000u;
