@@ -600,7 +600,8 @@ int osd_cache_append(const osd_append* call, void* stream);
  * outside the cache, an invalid tree) gets NaN.  What the cache holds in tokens
  * that a node does not see (NaN, too) does not reach its output; an infinite value
  * that it sees gives that infinity, or NaN where its probability is less than fp32
- * holds (beside a score about 100 larger).  Scores, softmax
+ * holds (beside a score about 100 larger).  Finite values give finite outputs where the
+ * |v| that a row sees sum to less than 2^127.  Scores, softmax
  * and sums are fp32; for the product with bf16 values a probability is taken as two
  * bf16 numbers, off by 2^-15 of itself.  Work is divided over the GPU by the lengths in device memory, so a
  * captured call serves any lengths; how it is divided, and with it the last bits,

@@ -462,12 +462,23 @@ struct Rows {
     // Whether the reference served: p up to 2^32 and sums of them are as exact as p up to
     // 1 (no scale is lost in fp32 or bf16), so steps need not agree on a maximum; only
     // where a score turned out further away are all keys taken again, now relative to
-    // the largest.
+    // the largest.  So they are where a sum of p v reached 2^112 (or is not finite): relative to the largest score
+    // it may be smaller, and below 2^112 those of 2^12 waves have a sum.  (Not of a row whose probabilities
+    // are NaN: what only that row sees must not change its neighbours.)
     __device__ bool served(float c2) const {
+        constexpr uint32_t kLarge = 0x77800000u;  // 2^112
         bool ok = true;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            const float m = rows_max(seen[mt]);
+            uint32_t most = 0;
+#pragma unroll
+            for (int n = 0; n < BLOCKS; ++n)
+#pragma unroll
+                for (int t = 0; t < VW; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) most = max(most, __float_as_uint(acc[mt][n][t][e]) & 0x7FFFFFFFu);
+            const float m = rows_max(seen[mt]), all = rows_sum(sum[mt]);
+            ok = ok && (most < kLarge || all != all);
             ok = ok && (m == kNegInf || fabsf(m * c2 - ref[mt]) <= 32.0f);
         }
         return __all(ok);
