@@ -629,7 +629,7 @@ int osd_tree_attention(const osd_attention* call, void* stream);
  * move.
  *
  * layers, layer_stride  the caches are [layers, pages, ...], layer_stride elements
- *                       between layers
+ *                       between layers, which share no memory
  * path_nodes            [B, N] int32 and
  * accepted_len          [B] int32: as osd_verify_tree returns them
  * new_seq_len           out [B] int32: c_b + 1 + accepted_len[b]; not seq_len itself

@@ -862,6 +862,19 @@ osd::CachePages cache_pages(const osd_cache& cache) {
     return c;
 }
 
+// Whether a page of one layer shares memory with one of another.  Two layers lie a multiple x of the distance
+// between layers apart, two pages a multiple of theirs, `page`: they meet where x is less than a page's
+// elements from such a multiple, of pages - 1 at most.
+bool layers_meet(const osd_cache& c, int layers, int64_t distance) {
+    const int64_t page = c.page_stride, elements = int64_t(c.kv_heads) * c.page_size * c.head_dim;
+    for (int64_t x = distance, i = 1; i < layers; x += distance, ++i) {
+        const int64_t below = x / page, rest = x - below * page;
+        if (below >= c.pages) return false;  // (as all that follow are)
+        if (rest < elements || (page - rest < elements && below + 1 < c.pages)) return true;
+    }
+    return false;
+}
+
 // Tokens of `heads` heads at `stride` elements.
 bool stride_ok(int64_t stride, int heads, int head_dim, int64_t es) {
     return stride >= int64_t(heads) * head_dim && stride <= kMaxTokenStride && stride * es % 16 == 0;
@@ -982,7 +995,7 @@ int osd_cache_keep(const osd_keep* call, void* stream) {
     if (st != OSD_OK) return st;
     const int64_t es = m.dtype == OSD_BF16 ? 2 : 4;
     if (m.N > OSD_MAX_TREE_NODES || c.layers <= 0 || c.layers > 65535 || c.layer_stride < 0 ||
-        c.layer_stride > kMaxStride || c.layer_stride * es % 16)
+        c.layer_stride > kMaxStride || c.layer_stride * es % 16 || layers_meet(m, c.layers, c.layer_stride))
         return OSD_ERR_INVALID_ARG;
     if (!c.path_nodes || !c.accepted_len || !c.new_seq_len) return OSD_ERR_INVALID_ARG;
     if (meets(m.seq_len, uint64_t(m.B) * 4, c.new_seq_len, uint64_t(m.B) * 4)) return OSD_ERR_INVALID_ARG;
