@@ -632,7 +632,8 @@ int osd_tree_attention(const osd_attention* call, void* stream);
  *                       between layers, which share no memory
  * path_nodes            [B, N] int32 and
  * accepted_len          [B] int32: as osd_verify_tree returns them
- * new_seq_len           out [B] int32: c_b + 1 + accepted_len[b]; not seq_len itself
+ * new_seq_len           out [B] int32: c_b + 1 + accepted_len[b]; no part of seq_len or of the
+ *                       other int32 arrays
  *
  * Nothing moves, and new_seq_len is c_b, where accepted_len is outside 0 .. N - 1
  * (-1: an invalid tree), the path is no ascending list of nodes in 1 .. N - 1, or

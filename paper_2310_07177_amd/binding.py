@@ -854,7 +854,7 @@ def osd_cache_keep(k_cache, v_cache, page_table, seq_len, path_nodes, accepted_l
     k_cache, v_cache [layers, pages, kv_heads, page_size, head_dim] (one
     layer: without the first axis), path_nodes [B, N] and accepted_len [B]
     int32 as osd_verify_tree returns them.  Returns the new context lengths [B]
-    int32 (a new tensor, or the given `out`, not seq_len itself)."""
+    int32 (a new tensor, or the given `out`, no part of the arguments)."""
     if k_cache.dim() == 4:
         layers = 1
         B, table_len, page_stride, P, H, S, D, code = _cache_args(k_cache, v_cache, page_table, seq_len, 0)

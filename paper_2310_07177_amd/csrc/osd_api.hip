@@ -998,7 +998,12 @@ int osd_cache_keep(const osd_keep* call, void* stream) {
         c.layer_stride > kMaxStride || c.layer_stride * es % 16 || layers_meet(m, c.layers, c.layer_stride))
         return OSD_ERR_INVALID_ARG;
     if (!c.path_nodes || !c.accepted_len || !c.new_seq_len) return OSD_ERR_INVALID_ARG;
-    if (meets(m.seq_len, uint64_t(m.B) * 4, c.new_seq_len, uint64_t(m.B) * 4)) return OSD_ERR_INVALID_ARG;
+    // (A sequence's workgroups read these, one of them writes the new length.)
+    const uint64_t lengths = uint64_t(m.B) * 4;
+    if (meets(m.seq_len, lengths, c.new_seq_len, lengths) || meets(c.accepted_len, lengths, c.new_seq_len, lengths) ||
+        meets(c.path_nodes, lengths * m.N, c.new_seq_len, lengths) ||
+        meets(m.page_table, lengths * m.table_len, c.new_seq_len, lengths))
+        return OSD_ERR_INVALID_ARG;
     osd::KeepLaunch L;
     L.k_cache = static_cast<char*>(m.k_cache);
     L.v_cache = static_cast<char*>(m.v_cache);

@@ -22,3 +22,13 @@ def test_layers_that_share_memory_are_refused(kw):
 def test_an_expanded_tensor_is_refused():
     """The check is the C ABI's: what the binding passes for one memory of three layers."""
     assert keep(vc=P(0x10000000), ls=0, layers=3) == -1
+
+
+@pytest.mark.parametrize("kw", [
+    dict(acc=P(0x90000)), dict(acc=P(0x8fffc)), dict(acc=P(0x90004)),                        # B = 2: 8 bytes each
+    dict(path=P(0x90000)), dict(path=P(0x90000 - 20)), dict(path=P(0x90004)),                # 24 bytes
+    dict(table=P(0x90000)), dict(table=P(0x90000 - 28)),                                     # 32 bytes
+])
+def test_new_lengths_over_what_is_read_are_refused(kw):
+    """One workgroup of a sequence would write them while others have still to read the path."""
+    assert keep(vc=P(0x10000000), **kw) == -1
