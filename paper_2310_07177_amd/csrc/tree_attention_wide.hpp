@@ -15,10 +15,14 @@ constexpr int kPageWindow = 512;  // pages looked up at once
 
 // 16 bytes a lane from memory to LDS at `to` (uniform) + 16 * lane, without a register on
 // the way.  Counted in vmcnt; the compiler does not know of it, so that reads of LDS
-// wait for it only where wait_stage() says so.
+// wait for it only where wait_stage() says so.  (hipcc warns that M0, which it names itself where it needs it, is no
+// register that it keeps for others: nothing here does.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ inline void load_lds(const char* from, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(from), "s"(to) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(from), "s"(to) : "m0", "memory");
 }
+#pragma clang diagnostic pop
 // All but the wave's LEFT newest loads are there, then those of all waves.
 template <int LEFT>
 __device__ inline void wait_stage() {
