@@ -588,7 +588,7 @@ int osd_cache_append(const osd_append* call, void* stream);
  *
  * q             [B, N, q_heads, head_dim], q_stride elements between tokens;
  *               query head h reads kv head h / (q_heads / kv_heads)
- * scale         finite
+ * scale         finite, and so as a float times log2(e), too
  * out           out [B, N, q_heads, head_dim]
  * workspace     osd_tree_attention_workspace_bytes(...) zero-initialised bytes
  *               for this operator alone (counters among them are left zero; the

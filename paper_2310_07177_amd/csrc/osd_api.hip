@@ -958,7 +958,8 @@ int osd_tree_attention(const osd_attention* call, void* stream) {
     const int64_t es = m.dtype == OSD_BF16 ? 2 : 4;
     if (!c.q || !c.out || !aligned16(c.q) || !aligned16(c.out)) return OSD_ERR_INVALID_ARG;
     if (!stride_ok(c.q_stride, c.q_heads, m.head_dim, es)) return OSD_ERR_INVALID_ARG;
-    if (!(c.scale - c.scale == 0.0f)) return OSD_ERR_INVALID_ARG;  // NaN, infinite
+    const float c2 = float(double(c.scale) * 1.4426950408889634);  // as the launch takes it
+    if (!(c2 - c2 == 0.0f)) return OSD_ERR_INVALID_ARG;            // NaN, infinite
     const uint64_t row = uint64_t(c.q_heads) * m.head_dim * es, tokens = uint64_t(m.B) * m.N;
     if (meets(c.q, (tokens - 1) * uint64_t(c.q_stride * es) + row, c.out, tokens * row)) return OSD_ERR_INVALID_ARG;
     if (!c.workspace || !aligned16(c.workspace) ||
