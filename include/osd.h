@@ -517,11 +517,11 @@ int osd_verify_topk(const void* target_logits, const int32_t* draft_ids, const v
  *                    (NULL: N); the nodes behind are padding
  *
  * Base addresses and strides of all arrays but the int32 ones are multiples of
- * 16 bytes; a sequence's table covers at most 2^30 tokens, a batch's 2^36 (otherwise
- * OSD_ERR_INVALID_ARG).  Unsupported head sizes and batches above
- * OSD_MAX_CACHE_BATCH give OSD_ERR_UNSUPPORTED.  Pages that several sequences
- * name are read correctly; a page that a call writes must belong to one
- * sequence alone.  Outputs must not overlap inputs, except as said.
+ * 16 bytes; a sequence's table covers at most 2^30 tokens, a batch's 2^36, and 2^35
+ * for osd_tree_attention (otherwise OSD_ERR_INVALID_ARG).  Unsupported head sizes
+ * and batches above OSD_MAX_CACHE_BATCH give OSD_ERR_UNSUPPORTED.  Pages that
+ * several sequences name are read correctly; a page that a call writes must belong
+ * to one sequence alone.  Outputs must not overlap inputs, except as said.
  */
 #define OSD_MAX_HEAD_DIM 256
 #define OSD_MAX_CACHE_BATCH 4096

@@ -955,6 +955,8 @@ int osd_tree_attention(const osd_attention* call, void* stream) {
     if (st != OSD_OK) return st;
     if (m.N > OSD_MAX_TREE_NODES || c.q_heads <= 0 || c.q_heads > 65535 || c.q_heads % m.kv_heads)
         return OSD_ERR_INVALID_ARG;
+    // The kernels count the batch's tiles, of 32 keys at least, in 31 bits.
+    if (int64_t(m.table_len) * m.page_size * m.B > (int64_t(1) << 35)) return OSD_ERR_INVALID_ARG;
     const int64_t es = m.dtype == OSD_BF16 ? 2 : 4;
     if (!c.q || !c.out || !aligned16(c.q) || !aligned16(c.out)) return OSD_ERR_INVALID_ARG;
     if (!stride_ok(c.q_stride, c.q_heads, m.head_dim, es)) return OSD_ERR_INVALID_ARG;
