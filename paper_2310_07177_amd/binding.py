@@ -716,6 +716,19 @@ _ATTENTION = struct.Struct(_CACHE + "7qif")
 _KEEP = struct.Struct(_CACHE + "4q2i")
 
 
+def _page_strides(t):
+    """Strides of a cache, None if a page is not contiguous.  Those of axes of one
+    element say nothing; they become what a contiguous tensor has."""
+    shape, stride, step = t.shape, list(t.stride()), 1
+    for i in range(len(shape) - 1, -1, -1):
+        if shape[i] == 1:
+            stride[i] = step
+        elif i >= len(shape) - 3 and stride[i] != step:
+            return None
+        step = stride[i] * shape[i]
+    return tuple(stride)
+
+
 def _cache_args(k_cache, v_cache, page_table, seq_len, layers):
     """The C ABI's description of a paged cache, checked; `layers`: its leading axes."""
     torch = _torch()
@@ -726,8 +739,10 @@ def _cache_args(k_cache, v_cache, page_table, seq_len, layers):
     if v_cache.dtype != k_cache.dtype:
         raise TypeError("the caches must share a dtype")
     P, H, S, D = shape[layers:]
-    if v_cache.stride() != stride or stride[-3:] != (S * D, D, 1):
-        raise ValueError("a page must be contiguous, and the caches' strides the same")
+    if v_cache.stride() != stride or stride[-3:] != (S * D, D, 1) or P == 1:
+        stride = _page_strides(k_cache)
+        if stride is None or _page_strides(v_cache) != stride:
+            raise ValueError("a page must be contiguous, and the caches' strides the same")
     int32 = torch.int32
     at = page_table.shape
     if len(at) != 2 or page_table.dtype != int32 or not page_table.is_contiguous():
@@ -861,7 +876,8 @@ def osd_cache_keep(k_cache, v_cache, page_table, seq_len, path_nodes, accepted_l
         layer_stride = 0
     else:
         B, table_len, page_stride, P, H, S, D, code = _cache_args(k_cache, v_cache, page_table, seq_len, 1)
-        layers, layer_stride = k_cache.shape[0], k_cache.stride(0)
+        layers = k_cache.shape[0]
+        layer_stride = k_cache.stride(0) if layers > 1 else 0
     at = _one_gpu(k_cache, v_cache, page_table, seq_len, path_nodes, accepted_len, out)
     if path_nodes.dim() != 2:
         raise ValueError("path_nodes must be [B, N]")

@@ -28,3 +28,23 @@ def test_layers_apart_are_taken(layout):
     new = osd.osd_cache_keep(k, v, dev(table), dev(lens), dev(path), dev(acc))
     assert new.tolist() == ref.keep(wk, wv, table, lens, path, acc).tolist()
     assert np.array_equal(f64(k), wk) and np.array_equal(f64(v), wv)
+
+
+def test_a_head_behind_its_tokens():
+    """One kv head, [pages, page_size, 1, D] seen as [pages, 1, page_size, D]: as the contiguous cache, bit for bit."""
+    import torch
+    import paper_2310_07177_amd as osd
+    S, D = 16, 64
+    k, v = (torch.randn(5, S, 1, D, device="cuda").bfloat16().transpose(1, 2) for _ in range(2))
+    kc, vc = k.reshape(5, 1, S, D).clone(), v.reshape(5, 1, S, D).clone()
+    new, q = torch.randn(2, 3, 1, D, device="cuda").bfloat16(), torch.randn(2, 3, 4, D, device="cuda").bfloat16()
+    table = torch.tensor([[0, 3], [4, 1]], dtype=torch.int32, device="cuda")
+    lens = torch.tensor([14, 9], dtype=torch.int32, device="cuda")
+    path = torch.tensor([[2, -1, -1], [1, 2, -1]], dtype=torch.int32, device="cuda")
+    acc = torch.tensor([1, 2], dtype=torch.int32, device="cuda")
+    got = []
+    for a, b in ((k, v), (kc, vc)):
+        osd.osd_cache_append(new, new, a, b, table, lens)
+        got.append(osd.osd_tree_attention(q, a, b, table, lens))
+        assert osd.osd_cache_keep(a, b, table, lens, path, acc).tolist() == [16, 12]
+    assert torch.equal(got[0], got[1]) and torch.equal(k, kc) and torch.equal(v, vc)
