@@ -551,7 +551,8 @@ typedef struct {
  *               (token (b, n) at (b * N + n) * q_stride); NULL: keys and values
  *               alone
  * q_out         out, as q with q_out_stride between tokens; q itself with the
- *               same stride, or no part of it; NULL iff q is
+ *               same stride, or no part of it (with another stride: apart from the
+ *               first to the last of q's tokens); NULL iff q is
  * k, v          [B, N, kv_heads, head_dim], k_stride and v_stride between tokens
  * rotation      [rotation_rows, rotary_dim] fp32: for each position the cosines
  *               of its rotary_dim / 2 angles, then the sines; NULL: no rotation

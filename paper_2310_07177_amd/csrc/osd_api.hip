@@ -862,16 +862,19 @@ osd::CachePages cache_pages(const osd_cache& cache) {
     return c;
 }
 
-// Whether a page of one layer shares memory with one of another.  Two layers lie a multiple x of the distance
-// between layers apart, two pages a multiple of theirs, `page`: they meet where x is less than a page's
-// elements from such a multiple, of pages - 1 at most.
+// Two arrays of n blocks, each `distance` apart: whether a block of the one, which begins `x` behind the
+// other, shares memory with one of the other.  Blocks lie x +- a multiple of the distance apart, n - 1 times at most.
+bool blocks_meet(int64_t x, int64_t distance, int64_t block, int64_t n) {
+    if (x < 0) x = -x;
+    const int64_t below = x / distance, rest = x - below * distance;
+    return (rest < block && below < n) || (distance - rest < block && below + 1 < n);
+}
+
+// Whether a page of one layer shares memory with one of another.
 bool layers_meet(const osd_cache& c, int layers, int64_t distance) {
-    const int64_t page = c.page_stride, elements = int64_t(c.kv_heads) * c.page_size * c.head_dim;
-    for (int64_t x = distance, i = 1; i < layers; x += distance, ++i) {
-        const int64_t below = x / page, rest = x - below * page;
-        if (below >= c.pages) return false;  // (as all that follow are)
-        if (rest < elements || (page - rest < elements && below + 1 < c.pages)) return true;
-    }
+    const int64_t page = int64_t(c.kv_heads) * c.page_size * c.head_dim;
+    for (int64_t x = distance, i = 1; i < layers && x / c.page_stride < c.pages; x += distance, ++i)
+        if (blocks_meet(x, c.page_stride, page, c.pages)) return true;
     return false;
 }
 
@@ -900,10 +903,13 @@ int osd_cache_append(const osd_append* call, void* stream) {
         if (!stride_ok(c.q_stride, c.q_heads, m.head_dim, es) || !stride_ok(c.q_out_stride, c.q_heads, m.head_dim, es))
             return OSD_ERR_INVALID_ARG;
         const uint64_t row = uint64_t(c.q_heads) * m.head_dim * es;
-        if (!(c.q_out == c.q && c.q_out_stride == c.q_stride) &&
-            meets(c.q, uint64_t((tokens - 1) * c.q_stride * es) + row, c.q_out,
-                  uint64_t((tokens - 1) * c.q_out_stride * es) + row))
-            return OSD_ERR_INVALID_ARG;
+        // Tokens at one distance may lie between the other array's.
+        const int64_t apart = int64_t(reinterpret_cast<uintptr_t>(c.q_out) - reinterpret_cast<uintptr_t>(c.q));
+        const bool over = c.q_out_stride == c.q_stride
+                              ? apart != 0 && blocks_meet(apart, c.q_stride * es, int64_t(row), tokens)
+                              : meets(c.q, uint64_t((tokens - 1) * c.q_stride * es) + row, c.q_out,
+                                      uint64_t((tokens - 1) * c.q_out_stride * es) + row);
+        if (over) return OSD_ERR_INVALID_ARG;
     }
     if (c.rotation) {
         if (c.rotation_rows <= 0 || c.rotary_dim <= 0 || c.rotary_dim % 2 || c.rotary_dim > m.head_dim)

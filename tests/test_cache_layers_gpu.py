@@ -48,3 +48,20 @@ def test_a_head_behind_its_tokens():
         got.append(osd.osd_tree_attention(q, a, b, table, lens))
         assert osd.osd_cache_keep(a, b, table, lens, path, acc).tolist() == [16, 12]
     assert torch.equal(got[0], got[1]) and torch.equal(k, kc) and torch.equal(v, vc)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_rotated_queries_between_the_queries(dtype):
+    """q_out among the same tokens' other heads: no part of q."""
+    import torch
+    import paper_2310_07177_amd as osd
+    x = torch.randn(2, 5, 10, 64, device="cuda").to(getattr(torch, dtype))
+    before, turn = x.clone(), torch.randn(40, 64, device="cuda")
+    k, v = (torch.zeros(4, 1, 16, 64, device="cuda", dtype=x.dtype) for _ in range(2))
+    table = torch.tensor([[0, 3], [2, 1]], dtype=torch.int32, device="cuda")
+    lens = torch.tensor([14, 9], dtype=torch.int32, device="cuda")
+    q, out, new = x[:, :, :4], x[:, :, 5:9], x[:, :, 4:5]
+    want = osd.osd_cache_append(new, new, k, v, table, lens, q=q, rotation=turn)
+    got = osd.osd_cache_append(new, new, k, v, table, lens, q=q, rotation=turn, q_out=out)
+    assert got is out and torch.equal(out, want)
+    assert torch.equal(x[:, :, :5], before[:, :, :5]) and torch.equal(x[:, :, 9:], before[:, :, 9:])
