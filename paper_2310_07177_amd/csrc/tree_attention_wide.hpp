@@ -64,6 +64,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
     using R = Rows<Ops, NC * 16, MT, 1>;
     constexpr int ES = S::ES, CHUNKS = R::CHUNKS, KT = R::KT, STEP = S::STEP, STAGE = S::STAGE, ROWS = S::ROWS;
     constexpr int PITCH = S::PITCH, CPR = S::CPR, ROW = S::ROW;
+    // Tiles that lie in the head whole, whatever its size (of those that launch_shape sends here).
+    constexpr int WHOLE = FULL ? NC : DT == 64 ? 0 : DT == 256 ? 8 : NC == 8 ? 6 : NC - 1;
     static_assert(WR == 4 || WR == kWaves, "two waves share keys, or one, or two with half of the rows");
     const TreeAttentionLaunch& L = a.L;
     const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave);
@@ -289,7 +291,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
                     for (int u = 0; u < BATCH; ++u) {
                         if (batch * BATCH + u >= NC) continue;
                         v[batch & 1][u] &= in;
-                        carries |= Ops::carries(v[batch & 1][u]);
+                        const int t = batch * BATCH + u;
+                        if (t < WHOLE || t * 16 + col < D) carries |= Ops::carries(v[batch & 1][u]);
                     }
                     if (__any((carries & Ops::kSigns) != 0)) {
                         rows.odd = true;
@@ -361,6 +364,14 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
             int st = 0;
             for (const int plain = len / STAGE - p.t0 < stages ? len / STAGE - p.t0 : stages; st < plain; ++st) stage(st, no_t{});
             for (; st < stages; ++st) stage(st, yes_t{});
+            // Columns behind the head's last hold what LDS held, which says nothing about the sums (nor, above, about
+            // values that are not finite: with those counted, heads of 72 took 151 us where those of 80 take 39).
+#pragma unroll
+            for (int t = WHOLE; t < NC; ++t)
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) rows.acc[mt][t][0][e] = t * 16 + grp * 4 + e < D ? rows.acc[mt][t][0][e] : 0.0f;
             // All waves share the stages, so that one that needs them again has all go through them.
             const bool ok = again || rows.served(a.c2);
             if (lane == 0) s_flags[wave] = ok;
