@@ -43,8 +43,8 @@ constexpr int64_t kAppendTokens = 1 << 21;
 // once, by one thread), otherwise two of equal distance.  Products and sums of the
 // rotation are fp32, rounded once to the cache's type.
 // Bound by memory: 8 prompts of 4096 tokens, 48 heads of 128 bf16 values, 822 MB read and
-// written in 149 us (5.5 TB/s; a plain copy of as much reaches 4.9), trees of 32 nodes of 64
-// sequences 51 MB in 12.0 us.  One token takes 2.8 us, the chain of its dependent loads.
+// written in 144 us (5.7 TB/s; a plain copy reaches 4.9), trees of 32 nodes of 64
+// sequences 51 MB in 11.7 us.  One token takes 3.0 us, the chain of its dependent loads.
 template <typename Fmt, int CH, bool PAIRS>
 __global__ __launch_bounds__(1024) void append_kernel(AppendArgs a) {
     const AppendLaunch& L = a.L;
@@ -162,7 +162,7 @@ struct KeepArgs {
 };
 
 // Bound by memory: paths of 64 sequences in 32 layers of 8 heads of 128 bf16 values, 52 MB read
-// and written in 10.8 us (4.8 TB/s, the rate of a copy); one sequence's 3.6 us.
+// and written in 10.3 us (5.0 TB/s, the rate of a copy); one sequence's 3.6 us.
 // A thread holds one 16-byte column of a head and moves the path's rows of it
 // in order.  A node's place on the path is never behind the node itself
 // (path[i] >= i + 1, ascending), so what a thread writes it has read before,

@@ -17,7 +17,7 @@ constexpr int kThreads = kWaves * kWave;
 // 16 keys, or head_dim < DT.  A step is 16 or 32 keys of a wave, a tile those of the
 // workgroup's four; the next step's keys and values are on their way while one is
 // worked on, 16 KB a wave of DT = 128.  Bound by memory: single tokens of 64 sequences of up to 8192
-// tokens, 1.34 GB, 205 to 217 us (6.2 to 6.5 TB/s; 244 us with loads that stay in the caches); one token over 2048
+// tokens, 1.34 GB, 216 us (6.2 TB/s; 244 us with loads that stay in the caches); one token over 2048
 // 11.7 us, a chain of waits (length, page, keys, the join of the parts).
 template <typename Ops, int DT, bool GEN>
 __global__ __launch_bounds__(kThreads, DT == 256 ? 1 : 2) void tree_attention_kernel(Args a) {

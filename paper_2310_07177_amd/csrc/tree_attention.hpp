@@ -21,7 +21,7 @@ namespace osd {
 namespace attention {
 
 constexpr int kMaxGroups = 512;   // workgroups of a launch
-constexpr int kMaxPieces = 64;    // workgroups that share a unit
+constexpr int kMaxPieces = 64;    // workgroups that share a unit, at most, on average (a far longer one has more)
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
@@ -246,7 +246,8 @@ struct Piece {
 //             tiles: at most two pieces of units that others share, the rest alone.
 // A workgroup that ends one piece and begins another loses about 5 us (its loads run dry), so
 // units are cut apart wherever that costs at most kSlack tiles of the longest.  Sequences'
-// lengths are in registers of each wave (up to 64 of them) or in LDS.
+// lengths are in registers of each wave (up to 64 of them; the parts, too, are counted there, so more
+// sequences always lie in a row) or in LDS.
 constexpr int kSlack = 4;
 
 template <int THREADS, int TILE>

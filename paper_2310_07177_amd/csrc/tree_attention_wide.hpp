@@ -38,9 +38,10 @@ __device__ inline u32x2_t transposed(const char* at) {
 
 // WR waves share the rows, 16 MT each, WK = 8 / WR the keys of a stage.  The ring of
 // stages in LDS is filled NST - 1 ahead.  32 sequences of 4032 to 4080 tokens, 8 kv heads of 128 bf16
-// values: 64 rows 95 us (5.6 TB/s), 128 rows 124 us, 256 rows 187 us (734 TFLOP/s), which as two blocks of
-// 128 would take 248.  Few rows are bound by memory, many by products and exponentials in turn.  Eight
-// waves of 32 rows: sixteen of 16 rows read K and V from LDS twice as often, and spilled.
+// values: 64 rows 97 us (5.5 TB/s), 128 rows 143 us, 256 rows 240 us (859 TFLOP/s of executed products),
+// which as two blocks of 128 would take 286.  Few rows are bound by memory, many by products and exponentials in
+// turn.  Eight waves of 32 rows: sixteen of 16 rows read K and V from LDS twice as often, and spilled.  (Of DT = 128
+// waves of 32 rows keep 22 to 34 registers in scratch, those of DT = 256 11 to 52.)
 template <typename Ops, int DT, int WR, int MT>
 struct Shape {
     static constexpr int ES = Ops::Fmt::kBytes, STEP = 16 * Ops::kKT, ROW = DT * ES;
@@ -365,7 +366,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_wide(Args a) {
             for (const int plain = len / STAGE - p.t0 < stages ? len / STAGE - p.t0 : stages; st < plain; ++st) stage(st, no_t{});
             for (; st < stages; ++st) stage(st, yes_t{});
             // Columns behind the head's last hold what LDS held, which says nothing about the sums (nor, above, about
-            // values that are not finite: with those counted, heads of 72 took 151 us where those of 80 take 39).
+            // values that are not finite: with those counted, heads of 72 took 148 us instead of 44).
 #pragma unroll
             for (int t = WHOLE; t < NC; ++t)
 #pragma unroll
@@ -481,7 +482,8 @@ hipError_t launch_shape(Args& a) {
     return launch_kernel(&tree_attention_wide<Ops, DT, WR, MT, DT / 16, false>, dim3(grid), dim3(kThreads), lds, L.stream, a);
 }
 
-// (A wave's sums of 32 rows of DT = 256, or of fp32, would fill its registers.)
+// (Waves of 32 rows: their sums of DT = 256 are 128 registers.  In fp32 sums and queries of DT = 128 are 64 each, of heads
+// up to 96 48 each; whether waves of 32 fp32 rows are faster is not measured.)
 template <typename Ops, int DT>
 hipError_t launch_dim(Args& a, int rows) {
     if (rows <= 64) return launch_shape<Ops, DT, 4, 1>(a);
