@@ -25,15 +25,14 @@ def queries(g, B, N, Hq, D, dtype):
     return dev(g.normal(0, 1, (B, N, Hq, D)).astype(np.float32), torch_dtype(dtype))
 
 
-@pytest.mark.parametrize("what", sorted(WHAT))
 @pytest.mark.parametrize("N,G", [(3, 4), (5, 4), (32, 4), (64, 4)])
 @pytest.mark.parametrize("D", [64, 80, 128, 256])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("cut", [False, True])
-def test_the_context_last_tokens(osd, cut, dtype, D, N, G, what):
-    """One value of each of the last 64 tokens of the context in turn, contexts of all
+def test_the_context_last_tokens(osd, cut, dtype, D, N, G):
+    """Three values of each of the last 64 tokens of the context in turn, contexts of all
     residues of a stage, units in a row (few of them shared) or cut apart: all nodes see
-    it, in one value of one kv head's rows, and nothing else changes but by rounding.
+    them, in three values of one kv head's rows, and nothing else changes but by rounding.
 
     (A sum that is not finite has a workgroup's keys taken again, relative to another score, so
     bits of the other values may change.  Both outputs are off by at most (2 r + n E + 2^-15 + 2^-22) sum p |v| and
@@ -43,7 +42,9 @@ def test_the_context_last_tokens(osd, cut, dtype, D, N, G, what):
     import torch
     g = np.random.default_rng(D + N)
     H = 1 if cut else 12
-    column, head = D - 3, H - 1
+    head, columns = H - 1, {5: "inf", D // 2: "-inf", D - 3: "nan"}
+    at = sorted(columns)
+    values = torch.tensor([WHAT[columns[x]] for x in at], device="cuda")
     for lens in (np.arange(130, 194).reshape(-1, 4) if cut else np.arange(66, 130).reshape(1, -1)).tolist():
         B = len(lens)
         c = Cache(g, lens, N, H, D, 16, dtype)
@@ -58,13 +59,15 @@ def test_the_context_last_tokens(osd, cut, dtype, D, N, G, what):
         for back in range(1, 65):
             j = c.d_lens.long() - back
             page, slot = c.d_table.long().gather(1, (j // 16)[:, None])[:, 0], j % 16
-            held = c.v[page, head, slot, column].clone()
-            c.v[page, head, slot, column] = WHAT[what]
+            held = c.v[page, head, slot].clone()
+            row = held.clone()
+            row[:, at] = values.to(row.dtype)
+            c.v[page, head, slot] = row
             got = osd.osd_tree_attention(q, c.k, c.v, c.d_table, c.d_lens, parent)
-            c.v[page, head, slot, column] = held
-            hit = got[:, :, head * G:, column].clone()
-            wrong |= ~(hit.isnan() if what == "nan" else hit == WHAT[what]).all()
-            got[:, :, head * G:, column] = clean[:, :, head * G:, column]
+            c.v[page, head, slot] = held
+            hit = got[:, :, head * G:].float()[..., at]
+            wrong |= ~torch.where(values.isnan(), hit.isnan(), hit == values).all()
+            got[:, :, head * G:, at] = clean[:, :, head * G:, at]
             wrong |= ~((got.float() - clean.float()).abs() <= tol).all()
             if back % 16 == 0:
                 assert not wrong, (lens[0], back)
@@ -72,13 +75,13 @@ def test_the_context_last_tokens(osd, cut, dtype, D, N, G, what):
 
 @pytest.mark.parametrize("N,G,H", [(16, 1, 1), (4, 4, 2), (64, 1, 1), (32, 4, 1), (64, 4, 1), (33, 2, 140)])
 @pytest.mark.parametrize("tree", [False, True])
-@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("D", [64, 256])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_nodes_on_both_sides_of_a_border(osd, dtype, D, tree, N, G, H):
     """Nodes of which some lie in one stage and some in the next, which other
     workgroups may have: a row gets what it sees of both, and of none of them."""
     g = np.random.default_rng(N + D)
-    for n in range(65, 260, 13 if H < 100 else 97):
+    for n in range(65, 260, 27 if H < 100 else 130):
         c = Cache(g, [n, 40], N, H, D, 16, dtype)
         q, parent = queries(g, 2, N, G * H, D, dtype), trees(g, 2, N) if tree else None
         early, late = int(g.integers(0, N // 2)), int(g.integers(N // 2, N))
@@ -97,11 +100,12 @@ def test_large_values(osd, dtype, N, G, D):
     """Values of 2^100 whose weights relative to a step's first keys reach 2^28.9: outputs are finite."""
     import torch
     g = np.random.default_rng(71)
-    H, lens = 4, [int(x) for x in g.integers(400, 1500, 24)]
+    H, B = 4, 24 if N < 5 else 8
+    lens = [int(x) for x in g.integers(400, 1500, B)]
     c = Cache(g, lens, N, H, D, 16, dtype)
     c.v.mul_(2.0 ** 100)
     c.k.zero_()
-    q = torch.zeros(24, N, G * H, D, device="cuda", dtype=torch_dtype(dtype))
+    q = torch.zeros(B, N, G * H, D, device="cuda", dtype=torch_dtype(dtype))
     q[..., 0] = 4.0
     for b, n in enumerate(lens):
         high = torch.from_numpy(g.random((n + N + 31) // 32) < 0.5).repeat_interleave(32)[:n + N].cuda()
