@@ -30,8 +30,8 @@
  *   - Workspaces: the caller allocates `*_workspace_bytes(...)` bytes of
  *     device memory and fills them with zeros ONCE before first use; every
  *     call leaves its workspace zeroed again when its kernels finish (those of
- *     osd_distill_topk_loss_grad and osd_verify_topk keep scratch beside
- *     counters, and each serves its operator alone).  Calls that may run
+ *     osd_distill_topk_loss_grad, osd_verify_topk and osd_tree_attention keep
+ *     scratch beside counters, and each serves its operator alone).  Calls that may run
  *     concurrently need distinct workspaces.  (A workspace that is not zero --
  *     fresh from an uninitialised allocation, or shared by calls in flight on
  *     two streams -- is not detected: the outputs are then wrong, with no
@@ -601,12 +601,12 @@ int osd_cache_append(const osd_append* call, void* stream);
  * outside the cache, an invalid tree) gets NaN.  What the cache holds in tokens
  * that a node does not see (NaN, too) does not reach its output; an infinite value
  * that it sees gives that infinity, or NaN where its probability is less than fp32
- * holds (beside a score about 100 larger).  Finite values give finite outputs where the
- * |v| that a row sees sum to less than 2^127.  Scores, softmax
- * and sums are fp32; for the product with bf16 values a probability is taken as two
- * bf16 numbers, off by 2^-15 of itself.  Work is divided over the GPU by the lengths in device memory, so a
- * captured call serves any lengths; how it is divided, and with it the last bits,
- * depends on all of the batch.  Equal calls give equal bits.
+ * holds (beside a score about 100 larger).  Finite values give finite outputs where
+ * the |v| that a row sees sum to less than 2^127.  Scores, softmax and sums are
+ * fp32; for the product with bf16 values a probability is taken as two bf16
+ * numbers, off by 2^-15 of itself.  Work is divided over the GPU by the lengths in
+ * device memory, so a captured call serves any lengths; how it is divided, and with
+ * it the last bits, depends on all of the batch.  Equal calls give equal bits.
  */
 typedef struct {
     osd_cache cache;
@@ -633,8 +633,8 @@ int osd_tree_attention(const osd_attention* call, void* stream);
  *                       between layers, which share no memory
  * path_nodes            [B, N] int32 and
  * accepted_len          [B] int32: as osd_verify_tree returns them
- * new_seq_len           out [B] int32: c_b + 1 + accepted_len[b]; no part of seq_len or of the
- *                       other int32 arrays
+ * new_seq_len           out [B] int32: c_b + 1 + accepted_len[b]; no part of seq_len
+ *                       or of the other int32 arrays
  *
  * Nothing moves, and new_seq_len is c_b, where accepted_len is outside 0 .. N - 1
  * (-1: an invalid tree), the path is no ascending list of nodes in 1 .. N - 1, or
